@@ -347,6 +347,180 @@ svm_status svm_tune(const svm_matrix *X, const float *y,
                     int32_t n_grid, const double *C, const double *gamma,
                     const double *epsilon, double *cv_error, int32_t *best);
 
+/* ------------------------------------------------------------------------
+ * Feature maps: the layers whose outputs a model is trained on (random
+ * cosine features for a linear SVM, or a residual network trained under the
+ * SVM's squared hinge loss), with their gradients.
+ *
+ * Conventions of these calls, where they differ from the ones above:
+ *   - Every array is device memory of `device` (on_device = 1; else
+ *     SVM_E_UNSUPPORTED) and is borrowed for the work that the call queues.
+ *   - The work is queued on `stream` (hipStream_t; NULL: the null stream)
+ *     and NOT waited for.  Nothing is allocated or freed and nothing is
+ *     copied to the host, so the calls can be captured into a HIP graph.
+ *   - All arrays of a call have one type (svm_dtype), except where stated.
+ *     Products, sums, statistics and states are held in 32 bits and rounded
+ *     to that type once, when they are written (SVM_F32 products are made
+ *     of three 8-bit parts of each factor: as exact as 32-bit products).
+ *   - Outputs must not overlap inputs or each other, except where stated.
+ *   - work: device memory of the caller, 16-byte aligned, of at least the
+ *     bytes that the call's _workspace function writes to *bytes for the
+ *     same arrays; its contents matter only during the call's work.
+ *   - Results do not depend on earlier calls, and repeat bit for bit. */
+typedef enum { SVM_F32 = 0, SVM_BF16 = 1, SVM_F16 = 2 } svm_dtype;
+
+/* rows x cols values of one type, row i at data + i*ld values, ld >= cols.
+ * Vectors (bias, weight) have rows = 1. */
+typedef struct {
+    void *data;
+    int64_t rows, cols, ld;
+    int32_t dtype;      /* svm_dtype */
+    int32_t on_device;  /* 1 */
+} svm_array;
+
+typedef enum {
+    SVM_ACT_NONE = 0,
+    SVM_ACT_RELU = 1,   /* max(z, 0); its slope at 0 is 0 */
+    SVM_ACT_GELU = 2,   /* z (1 + erf(z / sqrt 2)) / 2 */
+    SVM_ACT_SILU = 3,   /* z / (1 + exp(-z)) */
+    SVM_ACT_TANH = 4,
+    SVM_ACT_COS = 5     /* random Fourier features: with rows of W from
+                           N(0, 2 gamma I), bias from U[0, 2 pi) and n
+                           features, (2/n) phi(u).phi(v) tends to the RBF
+                           kernel (train with SVM_KERNEL_POLY, degree 1,
+                           gamma = 2/n) */
+} svm_act;
+
+/* One layer: Z = X W^T + bias, Y = act(Z) + residual.
+ * X m x k (m >= 0), W n x k, bias 1 x n, residual, Y and Z m x n; bias,
+ * residual and Z are nullable.  Z receives what the gradient needs (for
+ * every act but SVM_ACT_NONE).  residual may be Y itself (same data and
+ * ld).  m < 2^31, n and k in [1, 2^22]. */
+svm_status svm_linear(const svm_array *X, const svm_array *W,
+                      const svm_array *bias, const svm_array *residual,
+                      int32_t act, const svm_array *Y, const svm_array *Z,
+                      void *work, int64_t work_bytes, int32_t device,
+                      void *stream);
+svm_status svm_linear_workspace(const svm_array *X, const svm_array *W,
+                                int64_t *bytes);
+
+/* Its gradients for dY = dL/dY (m x n): with dZ = dY act'(Z),
+ *   dX = dZ W,  dW = dZ^T X,  dbias = sum of the rows of dZ.
+ * The residual's gradient is dY itself.  Z is what svm_linear wrote (may be
+ * NULL for SVM_ACT_NONE).  dX, dW and dbias are nullable: those not asked
+ * for cost nothing.  X may be NULL when dW is, W when dX is.  With m = 0,
+ * dW and dbias are set to 0. */
+svm_status svm_linear_backward(const svm_array *dY, const svm_array *X,
+                               const svm_array *W, const svm_array *Z,
+                               int32_t act, const svm_array *dX,
+                               const svm_array *dW, const svm_array *dbias,
+                               void *work, int64_t work_bytes,
+                               int32_t device, void *stream);
+svm_status svm_linear_backward_workspace(const svm_array *dY,
+                                         const svm_array *X,
+                                         const svm_array *W, int32_t act,
+                                         const svm_array *dX,
+                                         const svm_array *dW,
+                                         const svm_array *dbias,
+                                         int64_t *bytes);
+
+/* Layer norm of each row: y = (x - mean) rstd weight + bias with the row's
+ * mean and rstd = 1 / sqrt(mean of (x - mean)^2 + eps).  weight and bias
+ * (1 x cols) are nullable (1 and 0).  mean and rstd (rows floats each,
+ * nullable) receive the statistics that the gradient needs.  Y may be X
+ * itself (same data and ld).  cols in [1, 2^22]. */
+svm_status svm_layer_norm(const svm_array *X, const svm_array *weight,
+                          const svm_array *bias, double eps,
+                          const svm_array *Y, float *mean, float *rstd,
+                          int32_t device, void *stream);
+
+/* Its gradients: with xh = (x - mean) rstd and a = dY weight,
+ *   dX = rstd (a - mean(a) - xh mean(a xh)) + residual,
+ *   dweight = sum over rows of dY xh,  dbias = sum over rows of dY.
+ * residual (rows x cols, nullable): the gradient that reaches X past the
+ * norm, as in a residual network.  dX, dweight and dbias are nullable; dX
+ * may be dY or the residual itself.  With no rows dweight and dbias are set
+ * to 0. */
+svm_status svm_layer_norm_backward(const svm_array *dY, const svm_array *X,
+                                   const float *mean, const float *rstd,
+                                   const svm_array *weight,
+                                   const svm_array *residual,
+                                   const svm_array *dX,
+                                   const svm_array *dweight,
+                                   const svm_array *dbias, void *work,
+                                   int64_t work_bytes, int32_t device,
+                                   void *stream);
+svm_status svm_layer_norm_backward_workspace(int64_t rows, int64_t cols,
+                                             int64_t *bytes);
+
+/* Squared hinge loss, one class against the rest, and its gradient:
+ *   *loss = scale * sum_ic max(0, 1 - y_ic S_ic)^2,
+ *   dS_ic = -2 scale y_ic max(0, 1 - y_ic S_ic),
+ * y_ic = +1 where c is labels[i], else -1; with one column, label 1 is +1
+ * and label 0 is -1.  A label outside [0, C) (outside {0, 1} with one
+ * column) leaves its row out: it adds nothing and its gradient is 0.  S and
+ * dS rows x C, C in [1, 2^22]; dS is nullable and may be S itself.  labels:
+ * int32, rows of them; loss: one float; both on the device. */
+svm_status svm_hinge_loss(const svm_array *S, const int32_t *labels,
+                          double scale, const svm_array *dS, float *loss,
+                          void *work, int64_t work_bytes, int32_t device,
+                          void *stream);
+svm_status svm_hinge_loss_workspace(int64_t rows, int64_t cols,
+                                    int64_t *bytes);
+
+/* One tensor of svm_adamw_step: n contiguous values and their states.  The
+ * states come in whole blocks of 256 values, B = ceil(n / 256) of them; what
+ * lies past n in the last is updated as with a gradient of 0 (zeros stay
+ * zeros).  In 32 bits m and v are 256 B floats each and the scales NULL.  In
+ * 8 bits m is 256 B int8, v 256 B uint8, each block has a scale in m_scale
+ * and v_scale (B floats each), and they stand for
+ *   m = m_scale (c/127)^2 sign(c),  sqrt(v) = v_scale (c/254)^2,
+ * the square roots giving small values more of the codes; -128 and 255
+ * stand for NaN (a value that is not finite leaves its block's others
+ * alone), a block whose largest magnitude is at most 1e-30 is held as
+ * zeros, and a positive sqrt(v) in any other takes code 1 at least, so that
+ * no value that moves is divided by eps alone.  All zeros are the states to
+ * start from, in either form.  m, v and master are aligned to 16 bytes.
+ * n = 0 is allowed. */
+typedef struct {
+    void *param;         /* dtype; updated in place */
+    const void *grad;    /* grad_dtype */
+    float *master;       /* nullable: the weights in 32 bits (256 B floats),
+                            which the step works on; param receives them
+                            rounded.  Not with SVM_F32 parameters */
+    void *m, *v;
+    float *m_scale, *v_scale;
+    int64_t n;
+    int32_t dtype;       /* svm_dtype of param */
+    int32_t grad_dtype;  /* dtype or SVM_F32 */
+} svm_adamw_tensor;
+
+typedef struct {
+    double lr;            /* finite */
+    double beta1, beta2;  /* in [0, 1) */
+    double eps;           /* >= 0 */
+    double weight_decay;  /* finite */
+    double grad_scale;    /* factor of the gradients (1) */
+    int64_t step;         /* t >= 1, the number of this step */
+    int32_t bits;         /* states: 32 or 8 */
+} svm_adamw_params;
+
+/* One AdamW step (weight decay apart from the gradient) over all tensors of
+ * a host array, read during the call, in as few launches as they fit:
+ *   g = grad_scale grad;  m = b1 m + (1 - b1) g;  v = b2 v + (1 - b2) g^2;
+ *   p = p (1 - lr wd) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
+ * in 32 bits.  No two tensors may overlap. */
+svm_status svm_adamw_step(const svm_adamw_tensor *tensors, int32_t n_tensors,
+                          const svm_adamw_params *params, int32_t device,
+                          void *stream);
+
+/* The values that n 8-bit states stand for, their scales one to 256 (m_out,
+ * v_out: n floats each, nullable), as a checkpoint wants them. */
+svm_status svm_adamw_state(const int8_t *m, const uint8_t *v,
+                           const float *m_scale, const float *v_scale,
+                           int64_t n, float *m_out, float *v_out,
+                           int32_t device, void *stream);
+
 const char *svm_last_error(void);
 
 /* ------------------------------------------------------------------------

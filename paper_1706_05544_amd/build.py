@@ -19,12 +19,13 @@ LIB = os.path.join(HERE, "libmi355svm.so")
 ARCH = "gfx950"
 DEVICE_SOURCES = ["kernels.hip", "rows.hip", "lockstep.hip", "select.hip",
                   "predict.hip", "noalloc.hip", "iterate.hip", "factor.hip",
-                  "resident.hip"]
-HOST_SOURCES = ["solver.cpp", "api.cpp"]
+                  "resident.hip", "linear.hip", "norm.hip", "hinge.hip",
+                  "adamw.hip"]
+HOST_SOURCES = ["solver.cpp", "api.cpp", "layers.cpp"]
 
 # Packed fp32 instructions are disabled for every compilation that has a
 # device pass (hipcc runs one for the .cpp sources too).
-COMMON = ["-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-result",
+COMMON = ["-O3", "-fPIC", "-std=c++20", "-Wall", "-Wno-unused-result",
           "--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang",
           "-packed-fp32-ops", "-I" + INCLUDE]
 DEVICE_FLAGS = ["-x", "hip", "-munsafe-fp-atomics"]

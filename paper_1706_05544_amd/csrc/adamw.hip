@@ -1,0 +1,284 @@
+// One AdamW step over many tensors, states in 32 bits or in 8.
+#include <cmath>
+
+#include "elem.hpp"
+#include "layers.hpp"
+
+namespace msvm {
+
+namespace {
+
+// The tensors of one launch travel in its arguments (no table is copied to
+// the device, nothing outlives the call).
+constexpr int kPerLaunch = 48;
+
+struct AdamTable {
+    void* param[kPerLaunch];
+    const void* grad[kPerLaunch];
+    float* master[kPerLaunch];
+    void *m[kPerLaunch], *v[kPerLaunch];
+    float *ms[kPerLaunch], *vs[kPerLaunch];
+    int64_t n[kPerLaunch];
+    int32_t first[kPerLaunch + 1];  // first block of each tensor
+    int32_t count;
+};
+
+struct AdamConst {
+    float b1, c1, b2, c2;  // c = 1 - b
+    float keep;            // 1 - lr weight_decay
+    float rate;            // lr / (1 - b1^t)
+    float root;            // 1 / sqrt(1 - b2^t)
+    float eps, gscale;
+};
+
+constexpr float kTiny = 1e-30f;
+
+// The value of an 8-bit code; the code past the steps is NaN.  No operation
+// here is contracted: the value depends on the code and the scale alone.
+__device__ __forceinline__ float decode8(int c, float scale, int steps)
+{
+#pragma clang fp contract(off)
+    if (c < -steps || c > steps) return __builtin_nanf("");
+    const float t = (float)c * (1.0f / (float)steps);
+    return (t * fabsf(t)) * scale;
+}
+
+// One step of one value.  Not contracted, so that the states are the same
+// wherever they are computed.
+__device__ __forceinline__ void adam_value(const AdamConst& k, float g,
+                                           float& p, float& m, float& v,
+                                           float& r)
+{
+#pragma clang fp contract(off)
+    g = g * k.gscale;
+    m = m * k.b1 + g * k.c1;
+    v = v * k.b2 + (g * g) * k.c2;
+    r = sqrtf(v);
+    p = p * k.keep - k.rate * (m / (r * k.root + k.eps));
+}
+
+// The code of x (magnitude a) in a block with `by` = steps^2 / largest.
+__device__ __forceinline__ int encode8(float x, float by, bool live, int steps,
+                                       int bad, bool least_one)
+{
+#pragma clang fp contract(off)
+    const float a = fabsf(x);
+    if (!(a <= 3.402823466e38f)) return bad;
+    if (!live) return 0;
+    int c = (int)rintf(sqrtf(a * by));
+    c = c < steps ? c : steps;
+    if (least_one && a > 0.0f && c < 1) c = 1;
+    return x < 0.0f ? -c : c;
+}
+
+// A block of kAdamBlock values to a wave, four of them to a lane.
+template <int PT, int GT, int BITS, bool MASTER>
+__global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int blk = blockIdx.x * 4 + wave;
+    if (blk >= t.first[t.count]) return;
+    int lo = 0, hi = t.count - 1;  // the tensor of this block
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (t.first[mid] <= blk) lo = mid; else hi = mid - 1;
+    }
+    using P = Elem<PT>;
+    using G = Elem<GT>;
+    const int64_t b = blk - t.first[lo];
+    const int64_t at = b * kAdamBlock + lane * 4;
+    const int64_t n = t.n[lo];
+    P* param = (P*)t.param[lo];
+    const G* grad = (const G*)t.grad[lo];
+    float* master = t.master[lo];
+    float m[4], v[4], r[4];
+    float ms = 0.0f, vs = 0.0f;
+    if (BITS == 8) {
+        ms = t.ms[lo][b];
+        vs = t.vs[lo][b];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        // past the tensor's end: its states' last block, with gradient 0
+        const int64_t i = at + e;
+        const bool in = i < n;
+        if (BITS == 8) {
+            m[e] = decode8(((const int8_t*)t.m[lo])[i], ms, 127);
+            r[e] = decode8(((const uint8_t*)t.v[lo])[i], vs, 254);
+            v[e] = r[e] * r[e];
+        } else {
+            m[e] = ((const float*)t.m[lo])[i];
+            v[e] = ((const float*)t.v[lo])[i];
+        }
+        float p = MASTER ? master[i] : in ? (float)param[i] : 0.0f;
+        adam_value(k, in ? (float)grad[i] : 0.0f, p, m[e], v[e], r[e]);
+        if (MASTER) master[i] = p;
+        if (in) param[i] = (P)p;
+        if (BITS == 32) {
+            ((float*)t.m[lo])[i] = m[e];
+            ((float*)t.v[lo])[i] = v[e];
+        }
+    }
+    if (BITS == 8) {
+        float tm = 0.0f, tr = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float am = fabsf(m[e]);
+            if (am <= 3.402823466e38f) tm = fmaxf(tm, am);
+            if (r[e] <= 3.402823466e38f) tr = fmaxf(tr, r[e]);
+        }
+        tm = wave_max(tm);
+        tr = wave_max(tr);
+        const bool lm = tm > kTiny, lr = tr > kTiny;
+        const float bm = lm ? 16129.0f / tm : 0.0f;
+        const float br = lr ? 64516.0f / tr : 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t i = at + e;
+            ((int8_t*)t.m[lo])[i] =
+                (int8_t)encode8(m[e], bm, lm, 127, -128, false);
+            ((uint8_t*)t.v[lo])[i] =
+                (uint8_t)encode8(r[e], br, lr, 254, 255, true);
+        }
+        if (lane == 0) {
+            t.ms[lo][b] = lm ? tm : 0.0f;
+            t.vs[lo][b] = lr ? tr : 0.0f;
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void k_adamw_state(
+    const int8_t* m, const uint8_t* v, const float* ms, const float* vs,
+    int64_t n, float* mo, float* vo)
+{
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    if (mo) mo[i] = decode8(m[i], ms[i / kAdamBlock], 127);
+    if (vo) {
+        const float r = decode8(v[i], vs[i / kAdamBlock], 254);
+        vo[i] = r * r;
+    }
+}
+
+template <int PT, int GT>
+void launch_group(const AdamTable& t, const AdamConst& k, int bits,
+                  bool master, hipStream_t s)
+{
+    const dim3 grid((unsigned)((t.first[t.count] + 3) / 4)), block(256);
+    auto go = [&]<int BITS, bool MASTER>() {
+        hipLaunchKernelGGL((k_adamw<PT, GT, BITS, MASTER>), grid, block, 0, s,
+                           t, k);
+    };
+    if constexpr (PT != SVM_F32) {
+        if (master) {
+            if (bits == 8) go.template operator()<8, true>();
+            else go.template operator()<32, true>();
+            return;
+        }
+    }
+    if (bits == 8) go.template operator()<8, false>();
+    else go.template operator()<32, false>();
+}
+
+}  // namespace
+
+void adamw_step(const svm_adamw_tensor* t, int32_t n,
+                const svm_adamw_params& p, hipStream_t s)
+{
+    AdamConst k;
+    k.b1 = (float)p.beta1;
+    k.c1 = (float)(1.0 - p.beta1);
+    k.b2 = (float)p.beta2;
+    k.c2 = (float)(1.0 - p.beta2);
+    k.keep = (float)(1.0 - p.lr * p.weight_decay);
+    k.rate = (float)(p.lr / (1.0 - std::pow(p.beta1, (double)p.step)));
+    k.root = (float)(1.0 / std::sqrt(1.0 - std::pow(p.beta2, (double)p.step)));
+    k.eps = (float)p.eps;
+    k.gscale = (float)p.grad_scale;
+    AdamTable tab;
+    // one kernel for each combination of types among the tensors
+    for (int pt = SVM_F32; pt <= SVM_F16; ++pt)
+        for (int own = 1; own >= 0; --own)
+            for (int master = 0; master < 2; ++master) {
+                const int gt = own ? pt : SVM_F32;
+                if (pt == SVM_F32 && (!own || master)) continue;
+                tab.count = 0;
+                tab.first[0] = 0;
+                auto flush = [&]() {
+                    if (tab.count == 0) return;
+                    if (pt == SVM_F32)
+                        launch_group<SVM_F32, SVM_F32>(tab, k, p.bits, false,
+                                                       s);
+                    else if (pt == SVM_BF16 && own)
+                        launch_group<SVM_BF16, SVM_BF16>(tab, k, p.bits,
+                                                         master, s);
+                    else if (pt == SVM_BF16)
+                        launch_group<SVM_BF16, SVM_F32>(tab, k, p.bits, master,
+                                                        s);
+                    else if (own)
+                        launch_group<SVM_F16, SVM_F16>(tab, k, p.bits, master,
+                                                       s);
+                    else
+                        launch_group<SVM_F16, SVM_F32>(tab, k, p.bits, master,
+                                                       s);
+                    tab.count = 0;
+                };
+                // values of a tensor in one launch (block numbers are int32)
+                constexpr int64_t kMost = (int64_t)kAdamBlock << 24;
+                for (int32_t i = 0; i < n; ++i) {
+                    if (t[i].dtype != pt || t[i].grad_dtype != gt ||
+                        (t[i].master != nullptr) != (master != 0))
+                        continue;
+                    for (int64_t at = 0; at < t[i].n; at += kMost) {
+                        const int64_t len =
+                            t[i].n - at < kMost ? t[i].n - at : kMost;
+                        const int32_t nb =
+                            (int32_t)((len + kAdamBlock - 1) / kAdamBlock);
+                        if (tab.count == kPerLaunch ||
+                            (tab.count > 0 &&
+                             (int64_t)tab.first[tab.count] + nb > (1 << 25)))
+                            flush();
+                        const int c = tab.count;
+                        const int64_t sb = p.bits == 8 ? 1 : 4;
+                        tab.param[c] =
+                            (char*)t[i].param + at * dtype_bytes(pt);
+                        tab.grad[c] =
+                            (const char*)t[i].grad + at * dtype_bytes(gt);
+                        tab.master[c] = t[i].master ? t[i].master + at
+                                                    : nullptr;
+                        tab.m[c] = (char*)t[i].m + at * sb;
+                        tab.v[c] = (char*)t[i].v + at * sb;
+                        tab.ms[c] = t[i].m_scale
+                                        ? t[i].m_scale + at / kAdamBlock
+                                        : nullptr;
+                        tab.vs[c] = t[i].v_scale
+                                        ? t[i].v_scale + at / kAdamBlock
+                                        : nullptr;
+                        tab.n[c] = len;
+                        if (c == 0) tab.first[0] = 0;
+                        tab.first[c + 1] = tab.first[c] + nb;
+                        tab.count = c + 1;
+                    }
+                }
+                flush();
+            }
+}
+
+void adamw_state(const int8_t* m, const uint8_t* v, const float* ms,
+                 const float* vs, int64_t n, float* mo, float* vo,
+                 hipStream_t s)
+{
+    // at most 2^30 blocks to a launch, each a whole number of scales
+    const int64_t most = (int64_t)256 << 24;
+    for (int64_t at = 0; at < n; at += most) {
+        const int64_t len = n - at < most ? n - at : most;
+        hipLaunchKernelGGL(k_adamw_state,
+                           dim3((unsigned)((len + 255) / 256)), dim3(256), 0,
+                           s, m ? m + at : nullptr, v ? v + at : nullptr,
+                           ms ? ms + at / kAdamBlock : nullptr,
+                           vs ? vs + at / kAdamBlock : nullptr, len,
+                           mo ? mo + at : nullptr, vo ? vo + at : nullptr);
+    }
+}
+
+}  // namespace msvm

@@ -8,17 +8,15 @@
 #include <new>
 #include <string>
 
+#include "entry.hpp"
 #include "solver.hpp"
 
 namespace {
 
 thread_local std::string g_err;
 
-svm_status fail(svm_status st, const std::string& msg)
-{
-    g_err = msg;
-    return st;
-}
+using msvm::check_device;
+using msvm::fail;
 
 bool finite_pos(double v) { return std::isfinite(v) && v > 0.0; }
 
@@ -114,16 +112,6 @@ svm_status check_matrix(const svm_matrix* X, int64_t min_rows)
     return SVM_OK;
 }
 
-svm_status check_device(int dev)
-{
-    int count = 0;
-    hipError_t e = hipGetDeviceCount(&count);
-    if (e != hipSuccess || count <= 0)
-        return fail(SVM_E_DEVICE, "no HIP device available");
-    if (dev >= count) return fail(SVM_E_INVALID, "device ordinal out of range");
-    return SVM_OK;
-}
-
 svm_status check_host_labels(const float* y, int64_t n, int32_t type)
 {
     if (type == SVM_EPS_SVR) {
@@ -176,25 +164,6 @@ void fill_info(svm_model_info& in, const svm_model& m,
     in.select_kernel_launches = r.select_launches;
 }
 
-// Leaves HIP's per-thread last-error slot clean on every exit, so that an
-// error the library handled (or ignored while freeing) is not reported later
-// by a caller's own error check.
-struct ClearHipError {
-    ~ClearHipError() { (void)hipGetLastError(); }
-};
-
-#define GUARD_BEGIN \
-    ClearHipError clear_hip_error_on_exit_; \
-    try {
-#define GUARD_END                                                      \
-    }                                                                  \
-    catch (const msvm::Error& e) { return fail(e.status, e.msg); }     \
-    catch (const std::bad_alloc&) {                                    \
-        return fail(SVM_E_NOMEM, "host allocation failed");            \
-    }                                                                  \
-    catch (const std::exception& e) { return fail(SVM_E_INTERNAL, e.what()); } \
-    catch (...) { return fail(SVM_E_INTERNAL, "unknown error"); }
-
 }  // namespace
 
 namespace msvm {
@@ -202,6 +171,22 @@ void set_error(svm_status st, const std::string& msg)
 {
     (void)st;
     g_err = msg;
+}
+
+svm_status fail(svm_status st, const std::string& msg)
+{
+    set_error(st, msg);
+    return st;
+}
+
+svm_status check_device(int dev)
+{
+    int count = 0;
+    hipError_t e = hipGetDeviceCount(&count);
+    if (e != hipSuccess || count <= 0)
+        return fail(SVM_E_DEVICE, "no HIP device available");
+    if (dev >= count) return fail(SVM_E_INVALID, "device ordinal out of range");
+    return SVM_OK;
 }
 }  // namespace msvm
 

@@ -1,0 +1,41 @@
+// What the C entry points share: status and message of a refusal, the device
+// check, and the guard that lets no C++ exception and no HIP error past the
+// boundary.
+#pragma once
+
+#include <exception>
+#include <new>
+#include <string>
+
+#include "common.hpp"
+
+namespace msvm {
+
+// Sets the thread's message and returns st.
+svm_status fail(svm_status st, const std::string& msg);
+
+// SVM_OK if `dev` is an ordinal of this machine's GPUs.
+svm_status check_device(int dev);
+
+// Leaves HIP's per-thread last-error slot clean on every exit, so that an
+// error the library handled (or ignored while freeing) is not reported later
+// by a caller's own error check.
+struct ClearHipError {
+    ~ClearHipError() { (void)hipGetLastError(); }
+};
+
+}  // namespace msvm
+
+#define GUARD_BEGIN \
+    msvm::ClearHipError clear_hip_error_on_exit_; \
+    try {
+#define GUARD_END                                                      \
+    }                                                                  \
+    catch (const msvm::Error& e) { return msvm::fail(e.status, e.msg); } \
+    catch (const std::bad_alloc&) {                                    \
+        return msvm::fail(SVM_E_NOMEM, "host allocation failed");      \
+    }                                                                  \
+    catch (const std::exception& e) {                                  \
+        return msvm::fail(SVM_E_INTERNAL, e.what());                   \
+    }                                                                  \
+    catch (...) { return msvm::fail(SVM_E_INTERNAL, "unknown error"); }

@@ -31,6 +31,10 @@ SVM_EPS_SVR = 1
 SVM_KERNEL_LINEAR, SVM_KERNEL_POLY, SVM_KERNEL_RBF, SVM_KERNEL_SIGMOID = range(4)
 SVM_DENSE = 0
 SVM_CSR = 1
+SVM_F32, SVM_BF16, SVM_F16 = range(3)
+(SVM_ACT_NONE, SVM_ACT_RELU, SVM_ACT_GELU, SVM_ACT_SILU, SVM_ACT_TANH,
+ SVM_ACT_COS) = range(6)
+SVM_ADAMW_BLOCK = 256  # values that share a scale (states in 8 bits)
 
 # every symbol the header declares
 EXPORTS = [
@@ -42,6 +46,11 @@ EXPORTS = [
     "svm_test_select", "svm_test_rows", "svm_test_subproblem",
     "svm_test_apply", "svm_test_iterate", "svm_test_finish",
     "svm_predict_noalloc", "svm_cache_release",
+    "svm_linear", "svm_linear_workspace", "svm_linear_backward",
+    "svm_linear_backward_workspace", "svm_layer_norm",
+    "svm_layer_norm_backward", "svm_layer_norm_backward_workspace",
+    "svm_hinge_loss", "svm_hinge_loss_workspace", "svm_adamw_step",
+    "svm_adamw_state",
 ]
 
 
@@ -112,6 +121,27 @@ class svm_model_info(ct.Structure):
         return {k: getattr(self, k) for k, _ in self._fields_}
 
 
+class svm_array(ct.Structure):
+    _fields_ = [("data", ct.c_void_p), ("rows", ct.c_int64),
+                ("cols", ct.c_int64), ("ld", ct.c_int64),
+                ("dtype", ct.c_int32), ("on_device", ct.c_int32)]
+
+
+class svm_adamw_tensor(ct.Structure):
+    _fields_ = [("param", ct.c_void_p), ("grad", ct.c_void_p),
+                ("master", ct.c_void_p), ("m", ct.c_void_p),
+                ("v", ct.c_void_p), ("m_scale", ct.c_void_p),
+                ("v_scale", ct.c_void_p), ("n", ct.c_int64),
+                ("dtype", ct.c_int32), ("grad_dtype", ct.c_int32)]
+
+
+class svm_adamw_params(ct.Structure):
+    _fields_ = [("lr", ct.c_double), ("beta1", ct.c_double),
+                ("beta2", ct.c_double), ("eps", ct.c_double),
+                ("weight_decay", ct.c_double), ("grad_scale", ct.c_double),
+                ("step", ct.c_int64), ("bits", ct.c_int32)]
+
+
 _lib = None
 
 
@@ -173,6 +203,23 @@ def load(path: Optional[str] = None):
     lib.svm_test_finish.argtypes = [vp, ct.c_int32, P(ct.c_double),
                                     P(ct.c_double), P(ct.c_double),
                                     P(ct.c_int32)]
+    pa, i64, i32 = P(svm_array), ct.c_int64, ct.c_int32
+    lib.svm_linear.argtypes = [pa, pa, pa, pa, i32, pa, pa, vp, i64, i32, vp]
+    lib.svm_linear_workspace.argtypes = [pa, pa, P(i64)]
+    lib.svm_linear_backward.argtypes = [pa, pa, pa, pa, i32, pa, pa, pa, vp,
+                                        i64, i32, vp]
+    lib.svm_linear_backward_workspace.argtypes = [pa, pa, pa, i32, pa, pa, pa,
+                                                  P(i64)]
+    lib.svm_layer_norm.argtypes = [pa, pa, pa, ct.c_double, pa, vp, vp, i32,
+                                   vp]
+    lib.svm_layer_norm_backward.argtypes = [pa, pa, vp, vp, pa, pa, pa, pa, pa,
+                                            vp, i64, i32, vp]
+    lib.svm_layer_norm_backward_workspace.argtypes = [i64, i64, P(i64)]
+    lib.svm_hinge_loss.argtypes = [pa, vp, ct.c_double, pa, vp, vp, i64, i32,
+                                   vp]
+    lib.svm_hinge_loss_workspace.argtypes = [i64, i64, P(i64)]
+    lib.svm_adamw_step.argtypes = [vp, i32, P(svm_adamw_params), i32, vp]
+    lib.svm_adamw_state.argtypes = [vp, vp, vp, vp, i64, vp, vp, i32, vp]
     for name in EXPORTS:  # fail now, not at first use, if one is missing
         getattr(lib, name)
     _lib = lib
@@ -466,6 +513,419 @@ def svm_model_get(model: Model, output: int = 0, with_alpha: bool = False):
                                 _np_ptr(coef),
                                 _np_ptr(alpha) if alpha is not None else None))
     return idx[:k], coef[:k], alpha
+
+
+# ---------------------------------------------------------------------------
+# Feature maps: layers, their gradients, the loss and the optimiser step.
+# These calls take torch tensors on the GPU (float32, bfloat16 or float16, one
+# type to a call), queue their work on `stream` (torch's current stream when
+# None) and do not wait for it.  A tensor's last dimension is its columns, the
+# rest its rows; inputs whose rows are not at one stride, or whose values in a
+# row are not side by side, are copied first.
+# ---------------------------------------------------------------------------
+
+_ACTS = {"none": SVM_ACT_NONE, "relu": SVM_ACT_RELU, "gelu": SVM_ACT_GELU,
+         "silu": SVM_ACT_SILU, "tanh": SVM_ACT_TANH, "cos": SVM_ACT_COS}
+_DTYPES: dict = {}
+
+
+def _act(act) -> int:
+    if isinstance(act, str):
+        if act not in _ACTS:
+            raise SvmError(SVM_E_INVALID, "unknown activation %r" % act)
+        return _ACTS[act]
+    return act
+
+
+def _dtype(t, what: str) -> int:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: SVM_F32, torch.bfloat16: SVM_BF16,
+                        torch.float16: SVM_F16})
+    d = _DTYPES.get(getattr(t, "dtype", None)) if _is_torch(t) else None
+    if d is None or not t.is_cuda:
+        raise SvmError(SVM_E_UNSUPPORTED, "%s must be a float32, bfloat16 or "
+                       "float16 tensor in device memory" % what)
+    return d
+
+
+def _rows_of(t):
+    """(rows, cols, ld) of a tensor whose rows are at one stride, else
+    None."""
+    nd = t.dim()
+    if nd == 0:
+        return None
+    cols = t.shape[-1]
+    if t.numel() == 0:
+        return (0 if cols else 1), cols, cols
+    st = t.stride()
+    if cols > 1 and st[-1] != 1:
+        return None
+    rows, ld = 1, 0
+    for k in range(nd - 2, -1, -1):
+        size = t.shape[k]
+        if size == 1:
+            continue
+        if rows == 1:
+            ld = st[k]
+        elif st[k] != ld * rows:
+            return None
+        rows *= size
+    if rows == 1:
+        ld = cols
+    if rows and ld < cols:
+        return None
+    return rows, cols, max(ld, cols)
+
+
+def _arr(t, what: str, call, out: bool = False):
+    """svm_array of a tensor; a copy with rows side by side where it is an
+    input that has none (kept alive by the call)."""
+    if t is None:
+        return None
+    d = _dtype(t, what)
+    if t.device != call.device:
+        raise SvmError(SVM_E_INVALID, "%s is on another device" % what)
+    r = _rows_of(t)
+    if r is None:
+        if out:
+            raise SvmError(SVM_E_INVALID, "%s: its rows must be at one "
+                           "stride, the values of a row side by side" % what)
+        t = t.contiguous()
+        r = _rows_of(t)
+        if r is None:
+            raise SvmError(SVM_E_INVALID, "%s must have a dimension" % what)
+    call.keep.append(t)
+    return svm_array(t.data_ptr(), r[0], r[1], r[2], d, 1)
+
+
+def _ref(a):
+    return None if a is None else ct.byref(a)
+
+
+class _Call:
+    """The device and stream of a call, and the memory that its queued work
+    uses."""
+
+    def __init__(self, t, stream):
+        import torch
+        if not _is_torch(t) or not t.is_cuda:
+            raise SvmError(SVM_E_UNSUPPORTED,
+                           "this call takes tensors in device memory")
+        self.device = t.device
+        self.index = t.device.index or 0
+        cur = torch.cuda.current_stream(t.device)
+        self.stream = cur if stream is None else stream
+        self.handle = self.stream.cuda_stream
+        self.other = self.handle != cur.cuda_stream
+        self.keep = []
+
+    def empty(self, shape, dtype):
+        import torch
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        self.keep.append(t)
+        return t
+
+    def work(self, nbytes: int):
+        import torch
+        return self.empty((nbytes,), torch.uint8) if nbytes else None
+
+    def ready(self):
+        """Before the launch: on another stream than torch's current one the
+        work waits for what that one has queued (copies of inputs, earlier
+        users of the memory given out here)."""
+        import torch
+        if self.other:
+            self.stream.wait_stream(torch.cuda.current_stream(self.device))
+
+    def done(self):
+        # memory that torch gave out on its own stream is not handed out
+        # again before the work on the other one is done
+        if self.other:
+            for t in self.keep:
+                t.record_stream(self.stream)
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def svm_linear(X, W, bias=None, residual=None, act="none", save: bool = False,
+               out=None, stream=None):
+    """act(X W^T + bias) + residual -> Y, or (Y, Z) with the pre-activations
+    Z when `save`.  `out` receives Y when given (it may be `residual`)."""
+    lib = load()
+    c = _Call(X, stream)
+    a, w = _arr(X, "X", c), _arr(W, "W", c)
+    shape = X.shape[:-1] + (w.rows,)
+    Y = out if out is not None else c.empty(shape, X.dtype)
+    Z = c.empty(shape, X.dtype) if save else None
+    need = ct.c_int64()
+    _check(lib.svm_linear_workspace(ct.byref(a), ct.byref(w),
+                                    ct.byref(need)))
+    ws = c.work(need.value)
+    c.ready()
+    _check(lib.svm_linear(ct.byref(a), ct.byref(w),
+                          _ref(_arr(bias, "bias", c)),
+                          _ref(_arr(residual, "residual", c)), _act(act),
+                          ct.byref(_arr(Y, "out", c, True)),
+                          _ref(_arr(Z, "Z", c, True)), _ptr(ws), need.value,
+                          c.index, c.handle))
+    c.done()
+    return (Y, Z) if save else Y
+
+
+def svm_linear_backward(dY, X, W, Z=None, act="none", need=(True, True, True),
+                        stream=None):
+    """Gradients (dX, dW, dbias) of svm_linear; None where `need` is false.
+    The residual's gradient is dY itself."""
+    lib = load()
+    c = _Call(dY, stream)
+    g, a, w = _arr(dY, "dY", c), _arr(X, "X", c), _arr(W, "W", c)
+    dX = c.empty(X.shape, dY.dtype) if need[0] else None
+    dW = c.empty(W.shape, dY.dtype) if need[1] else None
+    db = c.empty((g.cols,), dY.dtype) if need[2] else None
+    rx, rw, rb = (_arr(dX, "dX", c, True), _arr(dW, "dW", c, True),
+                  _arr(db, "dbias", c, True))
+    size = ct.c_int64()
+    act = _act(act)
+    _check(lib.svm_linear_backward_workspace(
+        ct.byref(g), _ref(a), _ref(w), act, _ref(rx), _ref(rw), _ref(rb),
+        ct.byref(size)))
+    ws = c.work(size.value)
+    z = _arr(Z, "Z", c)
+    c.ready()
+    _check(lib.svm_linear_backward(
+        ct.byref(g), _ref(a), _ref(w), _ref(z), act, _ref(rx), _ref(rw),
+        _ref(rb), _ptr(ws), size.value, c.index, c.handle))
+    c.done()
+    return dX, dW, db
+
+
+def svm_layer_norm(X, weight=None, bias=None, eps: float = 1e-5,
+                   save: bool = False, out=None, stream=None):
+    """Layer norm over the last dimension -> Y, or (Y, mean, rstd) when
+    `save` (float32, one of each to a row)."""
+    import torch
+    lib = load()
+    c = _Call(X, stream)
+    a = _arr(X, "X", c)
+    Y = out if out is not None else c.empty(X.shape, X.dtype)
+    mean = c.empty(X.shape[:-1], torch.float32) if save else None
+    rstd = c.empty(X.shape[:-1], torch.float32) if save else None
+    w, b = _arr(weight, "weight", c), _arr(bias, "bias", c)
+    c.ready()
+    _check(lib.svm_layer_norm(ct.byref(a), _ref(w), _ref(b), eps,
+                              ct.byref(_arr(Y, "out", c, True)), _ptr(mean),
+                              _ptr(rstd), c.index, c.handle))
+    c.done()
+    return (Y, mean, rstd) if save else Y
+
+
+def _float_rows(t, rows: int, what: str, call):
+    import torch
+    if not _is_torch(t) or not t.is_cuda or t.dtype != torch.float32:
+        raise SvmError(SVM_E_UNSUPPORTED, "%s must be a float32 tensor in "
+                       "device memory" % what)
+    if t.numel() != rows:
+        raise SvmError(SVM_E_INVALID, "%s must have a value for each row"
+                       % what)
+    t = t.contiguous()
+    call.keep.append(t)
+    return t.data_ptr()
+
+
+def svm_layer_norm_backward(dY, X, mean, rstd, weight=None, residual=None,
+                            need=(True, True, True), stream=None):
+    """Gradients (dX, dweight, dbias) of svm_layer_norm; None where `need` is
+    false.  `residual` is added to dX: the gradient that reaches X past the
+    norm."""
+    lib = load()
+    c = _Call(dY, stream)
+    g, a = _arr(dY, "dY", c), _arr(X, "X", c)
+    mp = _float_rows(mean, g.rows, "mean", c)
+    rp = _float_rows(rstd, g.rows, "rstd", c)
+    dX = c.empty(X.shape, dY.dtype) if need[0] else None
+    dw = c.empty((g.cols,), dY.dtype) if need[1] else None
+    db = c.empty((g.cols,), dY.dtype) if need[2] else None
+    size = ct.c_int64()
+    if need[1] or need[2]:
+        _check(lib.svm_layer_norm_backward_workspace(g.rows, g.cols,
+                                                     ct.byref(size)))
+    ws = c.work(size.value)
+    w, r = _arr(weight, "weight", c), _arr(residual, "residual", c)
+    c.ready()
+    _check(lib.svm_layer_norm_backward(
+        ct.byref(g), ct.byref(a), mp, rp, _ref(w), _ref(r),
+        _ref(_arr(dX, "dX", c, True)), _ref(_arr(dw, "dweight", c, True)),
+        _ref(_arr(db, "dbias", c, True)), _ptr(ws), size.value, c.index,
+        c.handle))
+    c.done()
+    return dX, dw, db
+
+
+def svm_hinge_loss(S, labels, scale: Optional[float] = None,
+                   need_grad: bool = True, stream=None):
+    """Squared hinge loss of the scores S (rows x classes), one class against
+    the rest -> (loss, dS): a float32 scalar on the device and the gradient
+    (None without `need_grad`).  labels: int32, one to a row; a row whose
+    label is no class is left out.  `scale` multiplies both (1 / rows when
+    None)."""
+    import torch
+    lib = load()
+    c = _Call(S, stream)
+    a = _arr(S, "S", c)
+    if not _is_torch(labels) or not labels.is_cuda or \
+            labels.dtype != torch.int32:
+        raise SvmError(SVM_E_UNSUPPORTED, "labels must be an int32 tensor in "
+                       "device memory")
+    if labels.numel() != a.rows:
+        raise SvmError(SVM_E_INVALID, "labels must have one for each row")
+    labels = labels.contiguous()
+    c.keep.append(labels)
+    loss = c.empty((), torch.float32)
+    dS = c.empty(S.shape, S.dtype) if need_grad else None
+    size = ct.c_int64()
+    _check(lib.svm_hinge_loss_workspace(a.rows, a.cols, ct.byref(size)))
+    ws = c.work(size.value)
+    c.ready()
+    _check(lib.svm_hinge_loss(
+        ct.byref(a), labels.data_ptr(),
+        1.0 / max(a.rows, 1) if scale is None else scale,
+        _ref(_arr(dS, "dS", c, True)), loss.data_ptr(), _ptr(ws), size.value,
+        c.index, c.handle))
+    c.done()
+    return loss, dS
+
+
+def svm_adamw_parts(params):
+    """Where each tensor's states begin in the flat states of
+    svm_adamw_step, and their total length: the tensors follow one another,
+    each from a multiple of SVM_ADAMW_BLOCK."""
+    sizes = np.array([p.numel() for p in params], dtype=np.int64)
+    room = -(-sizes // SVM_ADAMW_BLOCK) * SVM_ADAMW_BLOCK
+    ends = np.cumsum(room)
+    return ends - room, int(ends[-1]) if len(ends) else 0
+
+
+def svm_adamw_states(params, bits: int = 32, master: bool = False):
+    """States to start from -> (m, v, m_scale, v_scale, master) for
+    svm_adamw_step: zeros, and with `master` the parameters in 32 bits."""
+    import torch
+    at, total = svm_adamw_parts(params)
+    dev = params[0].device
+    z = lambda n, t: torch.zeros(n, dtype=t, device=dev)  # noqa: E731
+    ms = vs = flat = None
+    if bits == 8:
+        m, v = z(total, torch.int8), z(total, torch.uint8)
+        ms, vs = (z(total // SVM_ADAMW_BLOCK, torch.float32)
+                  for _ in range(2))
+    else:
+        m, v = z(total, torch.float32), z(total, torch.float32)
+    if master:
+        flat = z(total, torch.float32)
+        for a, p in zip(at, params):
+            flat[a:a + p.numel()].copy_(p.detach().reshape(-1))
+    return m, v, ms, vs, flat
+
+
+_ADAMW_ROW = np.dtype([("param", "u8"), ("grad", "u8"), ("master", "u8"),
+                       ("m", "u8"), ("v", "u8"), ("m_scale", "u8"),
+                       ("v_scale", "u8"), ("n", "i8"), ("dtype", "i4"),
+                       ("grad_dtype", "i4")])
+
+
+def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
+                   master=None, lr: float = 1e-3, beta1: float = 0.9,
+                   beta2: float = 0.999, eps: float = 1e-8,
+                   weight_decay: float = 0.01, step: int = 1,
+                   grad_scale: float = 1.0, stream=None):
+    """One AdamW step over the tensors `params` (contiguous, updated in
+    place) with the gradients `grads`.  The states are flat tensors as
+    svm_adamw_states makes them: m and v in float32, or int8 and uint8 with
+    float32 scales, and optionally the master weights."""
+    import torch
+    if len(params) != len(grads):
+        raise SvmError(SVM_E_INVALID, "params and grads differ in number")
+    if not len(params):
+        return
+    lib = load()
+    c = _Call(params[0], stream)
+    at, total = svm_adamw_parts(params)
+    bits = 8 if m.dtype == torch.int8 else 32
+    want = [("m", m, torch.int8 if bits == 8 else torch.float32, total),
+            ("v", v, torch.uint8 if bits == 8 else torch.float32, total)]
+    if bits == 8:
+        nb = total // SVM_ADAMW_BLOCK
+        want += [("m_scale", m_scale, torch.float32, nb),
+                 ("v_scale", v_scale, torch.float32, nb)]
+    if master is not None:
+        want.append(("master", master, torch.float32, total))
+    for what, t, dtype, n in want:
+        if not _is_torch(t) or t.dtype != dtype or t.device != c.device or \
+                t.numel() != n or not t.is_contiguous():
+            raise SvmError(SVM_E_INVALID, "%s must be a contiguous %s tensor "
+                           "of %d values on the parameters' device"
+                           % (what, dtype, n))
+        c.keep.append(t)
+    tab = np.zeros(len(params), dtype=_ADAMW_ROW)
+    pd, gd, gp = [], [], []
+    for p, g in zip(params, grads):
+        pd.append(_dtype(p, "a parameter"))
+        gd.append(_dtype(g, "a gradient"))
+        if g.shape != p.shape or not p.is_contiguous():
+            raise SvmError(SVM_E_INVALID, "parameters must be contiguous, "
+                           "gradients of their shapes")
+        if not g.is_contiguous():
+            g = g.contiguous()
+        if p.device != c.device or g.device != c.device:
+            raise SvmError(SVM_E_INVALID, "the tensors are on several "
+                           "devices")
+        c.keep += (p, g)
+        gp.append(g.data_ptr())
+    tab["param"] = [p.data_ptr() for p in params]
+    tab["grad"] = gp
+    tab["n"] = [p.numel() for p in params]
+    tab["dtype"], tab["grad_dtype"] = pd, gd
+    esize = 1 if bits == 8 else 4
+    tab["m"], tab["v"] = m.data_ptr() + at * esize, v.data_ptr() + at * esize
+    if bits == 8:
+        sc = at // SVM_ADAMW_BLOCK * 4
+        tab["m_scale"], tab["v_scale"] = (m_scale.data_ptr() + sc,
+                                          v_scale.data_ptr() + sc)
+    if master is not None:
+        tab["master"] = np.where(tab["dtype"] == SVM_F32, 0,
+                                 master.data_ptr() + at * 4)
+    h = svm_adamw_params(lr, beta1, beta2, eps, weight_decay, grad_scale,
+                         step, bits)
+    c.ready()
+    _check(lib.svm_adamw_step(_np_ptr(tab), len(params), ct.byref(h), c.index,
+                              c.handle))
+    c.done()
+
+
+def svm_adamw_state(m, v, m_scale, v_scale, stream=None):
+    """The values that states in 8 bits stand for -> (m, v) in float32."""
+    import torch
+    lib = load()
+    c = _Call(m, stream)
+    n = m.numel()
+    nb = -(-n // SVM_ADAMW_BLOCK)
+    for what, t, dtype, k in (("m", m, torch.int8, n), ("v", v, torch.uint8, n),
+                              ("m_scale", m_scale, torch.float32, nb),
+                              ("v_scale", v_scale, torch.float32, nb)):
+        if not _is_torch(t) or t.dtype != dtype or t.numel() != k or \
+                t.device != c.device or not t.is_contiguous():
+            raise SvmError(SVM_E_INVALID, "%s must be a contiguous %s tensor "
+                           "of %d values" % (what, dtype, k))
+        c.keep.append(t)
+    mo, vo = c.empty((n,), torch.float32), c.empty((n,), torch.float32)
+    c.ready()
+    _check(lib.svm_adamw_state(m.data_ptr(), v.data_ptr(), m_scale.data_ptr(),
+                               v_scale.data_ptr(), n, mo.data_ptr(),
+                               vo.data_ptr(), c.index, c.handle))
+    c.done()
+    return mo, vo
 
 
 class Solver:
