@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libmi355svm.so")
 ARCH = "gfx950"
 DEVICE_SOURCES = ["kernels.hip", "rows.hip", "lockstep.hip", "select.hip",
                   "predict.hip", "noalloc.hip", "iterate.hip", "factor.hip",
-                  "resident.hip", "linear.hip", "norm.hip", "hinge.hip",
+                  "resident.hip", "linear.hip", "matmul.hip", "norm.hip", "hinge.hip",
                   "adamw.hip"]
 HOST_SOURCES = ["solver.cpp", "api.cpp", "layers.cpp"]
 

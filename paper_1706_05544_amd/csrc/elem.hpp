@@ -52,6 +52,43 @@ __device__ __forceinline__ float wave_max(float v)
     return v;
 }
 
+// cos(z) and sin(z): z less the nearest multiple of pi (in 64 bits: the
+// angle of a 32-bit z is then good to 1e-8 up to |z| = 1e8), by the series
+// to r^14 and r^13 (below 1e-9 at r = pi/2), with the sign of the multiple.
+__device__ __forceinline__ float turn(float z, bool& odd)
+{
+    const double k = rint((double)z * 0.31830988618379067154);
+    odd = k != 2.0 * rint(0.5 * k);
+    return (float)fma(-k, 3.14159265358979323846, (double)z);
+}
+
+__device__ __forceinline__ float cos_of(float z)
+{
+    bool odd;
+    const float r = turn(z, odd), q = r * r;
+    float c = fmaf(q, -1.1470746e-11f, 2.0876757e-9f);
+    c = fmaf(q, c, -2.7557319e-7f);
+    c = fmaf(q, c, 2.4801587e-5f);
+    c = fmaf(q, c, -1.3888889e-3f);
+    c = fmaf(q, c, 4.1666667e-2f);
+    c = fmaf(q, c, -0.5f);
+    c = fmaf(q, c, 1.0f);
+    return odd ? -c : c;
+}
+
+__device__ __forceinline__ float sin_of(float z)
+{
+    bool odd;
+    const float r = turn(z, odd), q = r * r;
+    float c = fmaf(q, 1.6059044e-10f, -2.5052108e-8f);
+    c = fmaf(q, c, 2.7557319e-6f);
+    c = fmaf(q, c, -1.9841270e-4f);
+    c = fmaf(q, c, 8.3333333e-3f);
+    c = fmaf(q, c, -1.6666667e-1f);
+    c = fmaf(r * q, c, r);
+    return odd ? -c : c;
+}
+
 // act(z)
 __device__ __forceinline__ float act_value(int act, float z)
 {
@@ -60,9 +97,28 @@ __device__ __forceinline__ float act_value(int act, float z)
     case SVM_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
     case SVM_ACT_SILU: return z / (1.0f + __expf(-z));
     case SVM_ACT_TANH: return tanhf(z);
-    case SVM_ACT_COS: return cosf(z);
+    case SVM_ACT_COS: return cos_of(z);
     default: return z;
     }
+}
+
+// act of eight values, the choice made once
+__device__ __forceinline__ void act_values(int act, float (&v)[8])
+{
+#define MSVM_EACH(A)                                            \
+    case A:                                                     \
+        _Pragma("unroll") for (int e = 0; e < 8; ++e) v[e] =    \
+            act_value(A, v[e]);                                 \
+        break
+    switch (act) {
+        MSVM_EACH(SVM_ACT_RELU);
+        MSVM_EACH(SVM_ACT_GELU);
+        MSVM_EACH(SVM_ACT_SILU);
+        MSVM_EACH(SVM_ACT_TANH);
+        MSVM_EACH(SVM_ACT_COS);
+    default: break;
+    }
+#undef MSVM_EACH
 }
 
 // act'(z)
@@ -81,7 +137,7 @@ __device__ __forceinline__ float act_slope(int act, float z)
         const float y = tanhf(z);
         return fmaf(-y, y, 1.0f);
     }
-    case SVM_ACT_COS: return -sinf(z);
+    case SVM_ACT_COS: return -sin_of(z);
     default: return 1.0f;
     }
 }

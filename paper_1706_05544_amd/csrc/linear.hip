@@ -1,99 +1,10 @@
 // The fused linear layer Y = act(X W^T + b) + R and its gradients.
 #include "elem.hpp"
-#include "layers.hpp"
+#include "matmul.hpp"
 
 namespace msvm {
 
 namespace {
-
-constexpr int kTile = 64;  // rows and columns of an output tile
-constexpr int kStep = 16;  // of the summed index at a time
-
-// C(i, j) = sum_r A(i, r) B(j, r); element (i, r) of A at A[i ai + r ar].
-struct Product {
-    const void *A, *B;
-    int64_t ai, ar, bj, br;
-    int64_t m, n, k;
-};
-
-// What happens to the sums: bias, pre-activations out, activation, residual.
-struct Epilogue {
-    const void *bias, *residual;
-    void *Y, *Z;
-    int64_t ldr, ldy, ldz;
-    int act;
-};
-
-template <int DT>
-__global__ __launch_bounds__(256) void k_product(Product p, Epilogue e)
-{
-    using T = Elem<DT>;
-    __shared__ float As[kStep][kTile + 1], Bs[kStep][kTile + 1];
-    const T* A = (const T*)p.A;
-    const T* B = (const T*)p.B;
-    const int t = threadIdx.x, tx = t & 15, ty = t >> 4;
-    const int64_t i0 = (int64_t)blockIdx.y * kTile;
-    const int64_t j0 = (int64_t)blockIdx.x * kTile;
-    float acc[4][4] = {};
-    for (int64_t r0 = 0; r0 < p.k; r0 += kStep) {
-        for (int x = t; x < kTile * kStep; x += 256) {
-            const int i = x / kStep, r = x % kStep;
-            As[r][i] = i0 + i < p.m && r0 + r < p.k
-                           ? (float)A[(i0 + i) * p.ai + (r0 + r) * p.ar]
-                           : 0.0f;
-            Bs[r][i] = j0 + i < p.n && r0 + r < p.k
-                           ? (float)B[(j0 + i) * p.bj + (r0 + r) * p.br]
-                           : 0.0f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < kStep; ++r)
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                    acc[u][v] = fmaf(As[r][ty * 4 + u], Bs[r][tx + 16 * v],
-                                     acc[u][v]);
-        __syncthreads();
-    }
-    for (int u = 0; u < 4; ++u) {
-        const int64_t i = i0 + ty * 4 + u;
-        if (i >= p.m) break;
-        for (int v = 0; v < 4; ++v) {
-            const int64_t j = j0 + tx + 16 * v;
-            if (j >= p.n) break;
-            float z = acc[u][v];
-            if (e.bias) z += (float)((const T*)e.bias)[j];
-            if (e.Z) ((T*)e.Z)[i * e.ldz + j] = (T)z;
-            float y = act_value(e.act, z);
-            if (e.residual) y += (float)((const T*)e.residual)[i * e.ldr + j];
-            ((T*)e.Y)[i * e.ldy + j] = (T)y;
-        }
-    }
-}
-
-void launch_product(int32_t dtype, const Product& p, const Epilogue& e,
-                    hipStream_t s)
-{
-    if (p.m == 0 || p.n == 0) return;
-    // rows in slices of at most 65535 tiles (the grid's y)
-    const int64_t slice = (int64_t)65535 * kTile;
-    for (int64_t i0 = 0; i0 < p.m; i0 += slice) {
-        Product q = p;
-        Epilogue f = e;
-        const size_t eb = dtype_bytes(dtype);
-        q.m = p.m - i0 < slice ? p.m - i0 : slice;
-        q.A = (const char*)p.A + i0 * p.ai * eb;
-        f.Y = (char*)e.Y + i0 * e.ldy * eb;
-        if (e.Z) f.Z = (char*)e.Z + i0 * e.ldz * eb;
-        if (e.residual) f.residual = (const char*)e.residual + i0 * e.ldr * eb;
-        const dim3 grid((unsigned)((p.n + kTile - 1) / kTile),
-                        (unsigned)((q.m + kTile - 1) / kTile));
-        for_dtype(dtype, [&]<int DT>() {
-            hipLaunchKernelGGL((k_product<DT>), grid, dim3(256), 0, s, q, f);
-        });
-    }
-}
 
 // dZ = dY act'(Z), and the sums of its columns over this block's rows
 constexpr int kGradRows = 64;
@@ -105,8 +16,13 @@ __global__ __launch_bounds__(256) void k_act_grad(
 {
     using T = Elem<DT>;
     const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (j >= n) return;
     const int64_t i0 = (int64_t)blockIdx.y * kGradRows;
+    if (j >= n) {  // the zeros that end the rows of dZ
+        if (dZ_ && j < ldd)
+            for (int64_t i = i0; i < m && i < i0 + kGradRows; ++i)
+                ((T*)dZ_)[i * ldd + j] = (T)0.0f;
+        return;
+    }
     const int64_t i1 = i0 + kGradRows < m ? i0 + kGradRows : m;
     float sum = 0.0f;
     for (int64_t i = i0; i < i1; ++i) {
@@ -116,6 +32,27 @@ __global__ __launch_bounds__(256) void k_act_grad(
         if (dZ_) ((T*)dZ_)[i * ldd + j] = (T)g;
     }
     if (part) part[(int64_t)blockIdx.y * n + j] = sum;
+}
+
+// Zeros to rows x cols of an array.
+template <int DT>
+__global__ __launch_bounds__(256) void k_zero(Elem<DT>* out, int64_t ld,
+                                              int64_t rows, int64_t cols)
+{
+    const int64_t all = rows * cols;
+    for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all;
+         t += (int64_t)gridDim.x * 256)
+        out[t / cols * ld + t % cols] = (Elem<DT>)0.0f;
+}
+
+void launch_zero(const svm_array& a, hipStream_t s)
+{
+    const int64_t nb = (a.rows * a.cols + 255) / 256;
+    for_dtype(a.dtype, [&]<int DT>() {
+        hipLaunchKernelGGL((k_zero<DT>),
+                           dim3((unsigned)(nb < 4096 ? nb : 4096)), dim3(256),
+                           0, s, (Elem<DT>*)a.data, a.ld, a.rows, a.cols);
+    });
 }
 
 template <int DT>
@@ -146,14 +83,42 @@ void launch_column_sums(const float* part0, const float* part1, int64_t np,
     });
 }
 
+namespace {
+
+// A factor of a product from an array: as it is where the product can read
+// it so, else a copy in the workspace (32 bits: in three planes).
+Factor factor_of(const svm_array& a, bool along, Pieces& ws, hipStream_t s)
+{
+    Factor f{a.data, a.ld, 0, along, (const float*)a.data, a.ld};
+    if (factor_fits(a, along)) return f;
+    f.ld = (a.cols + 7) / 8 * 8;
+    f.plane = a.rows * f.ld;
+    void* copy = ws.take<uint16_t>((a.dtype == SVM_F32 ? 3 : 1) * f.plane);
+    f.data = copy;
+    if (ws.run) launch_planes(a, copy, f.ld, f.plane, s);
+    return f;
+}
+
+Epilogue plain(const svm_array& out)
+{
+    return {nullptr, nullptr, out.data, nullptr, 0, out.ld, 0, SVM_ACT_NONE};
+}
+
+}  // namespace
+
 void linear_forward(const LinearArgs& a, Pieces& ws, hipStream_t s)
 {
-    if (!ws.run) return;
-    Product p{a.X.data, a.W.data, a.X.ld, 1, a.W.ld, 1,
-              a.X.rows, a.W.rows, a.X.cols};
-    Epilogue e{a.bias.data, a.residual.data, a.Y.data, a.Z.data,
-               a.residual.ld, a.Y.ld, a.Z.ld, a.act};
-    launch_product(a.X.dtype, p, e, s);
+    Product p;
+    p.m = a.X.rows;
+    p.n = a.W.rows;
+    p.k = a.X.cols;
+    p.dtype = a.X.dtype;
+    if (p.m == 0) return;
+    p.A = factor_of(a.X, true, ws, s);
+    p.B = factor_of(a.W, true, ws, s);
+    p.e = {a.bias.data, a.residual.data, a.Y.data, a.Z.data,
+           a.residual.ld, a.Y.ld, a.Z.ld, a.act};
+    product(p, ws, s);
 }
 
 void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
@@ -165,12 +130,11 @@ void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
     const int64_t np = (m + kGradRows - 1) / kGradRows;
     svm_array dZ = a.dY;
     if (slope && (dx || dw)) {
-        dZ.ld = n;
-        dZ.data = ws.take<char>(m * n * dtype_bytes(t));
+        dZ.ld = (n + 7) / 8 * 8;
+        dZ.data = ws.take<char>(m * dZ.ld * dtype_bytes(t));
     }
     float* part = db ? ws.take<float>(np * n) : nullptr;
-    if (!ws.run) return;
-    if (np > 0 && (slope || db)) {
+    if (ws.run && np > 0 && (slope || db)) {
         for_dtype(t, [&]<int DT>() {
             // rows in slices of at most 65535 blocks (the grid's y)
             for (int64_t b0 = 0; b0 < np; b0 += 65535) {
@@ -179,7 +143,7 @@ void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
                 using T = Elem<DT>;
                 hipLaunchKernelGGL(
                     (k_act_grad<DT>),
-                    dim3((unsigned)((n + 255) / 256), (unsigned)nb),
+                    dim3((unsigned)((dZ.ld + 255) / 256), (unsigned)nb),
                     dim3(256), 0, s, (const T*)a.dY.data + i0 * a.dY.ld,
                     a.dY.ld,
                     slope ? (const T*)a.Z.data + i0 * a.Z.ld : nullptr,
@@ -189,19 +153,44 @@ void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
             }
         });
     }
-    if (db)
+    if (ws.run && db)
         launch_column_sums(part, nullptr, np, n, t, a.dbias.data, nullptr, s);
+    if (!dx && !dw) return;
+    if (m == 0) {
+        if (dw && ws.run) launch_zero(a.dW, s);
+        return;
+    }
+    // both products read one copy of dZ, where it has to be copied at all
+    svm_array part_dz = dZ;
+    Factor dz;
+    if (dx && slope && t != SVM_F32) {
+        // the workspace's own rows end in zeros up to a multiple of 8
+        part_dz.cols = dZ.ld;
+    }
+    dz = factor_of(part_dz, dx, ws, s);
     if (dx) {
-        Product p{dZ.data, a.W.data, dZ.ld, 1, 1, a.W.ld, m, a.W.cols, n};
-        Epilogue e{nullptr, nullptr, a.dX.data, nullptr,
-                   0,       a.dX.ld, 0,         SVM_ACT_NONE};
-        launch_product(t, p, e, s);
+        Product p;
+        p.A = dz;
+        p.A.along = true;
+        p.B = factor_of(a.W, false, ws, s);
+        p.m = m;
+        p.n = a.W.cols;
+        p.k = n;
+        p.dtype = t;
+        p.e = plain(a.dX);
+        product(p, ws, s);
     }
     if (dw) {
-        Product p{dZ.data, a.X.data, 1, dZ.ld, 1, a.X.ld, n, a.X.cols, m};
-        Epilogue e{nullptr, nullptr, a.dW.data, nullptr,
-                   0,       a.dW.ld, 0,         SVM_ACT_NONE};
-        launch_product(t, p, e, s);
+        Product p;
+        p.A = dz;
+        p.A.along = false;
+        p.B = factor_of(a.X, false, ws, s);
+        p.m = n;
+        p.n = a.X.cols;
+        p.k = m;
+        p.dtype = t;
+        p.e = plain(a.dW);
+        product(p, ws, s);
     }
 }
 
