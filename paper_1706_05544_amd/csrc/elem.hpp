@@ -89,14 +89,50 @@ __device__ __forceinline__ float sin_of(float z)
     return odd ? -c : c;
 }
 
+// The normal distribution's upper tail at |z| and exp(-z^2 / 2): the rational
+// approximation 7.1.26 of Abramowitz and Stegun's handbook (to 7.5e-8).
+__device__ __forceinline__ float upper_tail(float z, float& e)
+{
+    const float a = fabsf(z);
+    e = __expf(-0.5f * z * z);
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.23164189f, a, 1.0f));
+    float q = fmaf(t, 0.530702714f, -0.726576014f);
+    q = fmaf(t, q, 0.710706870f);
+    q = fmaf(t, q, -0.142248368f);
+    q = fmaf(t, q, 0.127414796f);
+    return t * q * e;
+}
+
+// tanh by exp, and by its series near 0 (to 1e-8 below 0.2)
+__device__ __forceinline__ float tanh_of(float z)
+{
+    const float e = __expf(-2.0f * fabsf(z));
+    const float y = copysignf(
+        (1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e), z);
+    const float q = z * z;
+    float c = fmaf(q, 2.1869489e-2f, -5.3968254e-2f);
+    c = fmaf(q, c, 1.3333333e-1f);
+    c = fmaf(q, c, -3.3333333e-1f);
+    return fabsf(z) < 0.2f ? fmaf(z * q, c, z) : y;
+}
+
+__device__ __forceinline__ float sigmoid_of(float z)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+}
+
 // act(z)
 __device__ __forceinline__ float act_value(int act, float z)
 {
     switch (act) {
     case SVM_ACT_RELU: return z > 0.0f ? z : (z != z ? z : 0.0f);
-    case SVM_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
-    case SVM_ACT_SILU: return z / (1.0f + __expf(-z));
-    case SVM_ACT_TANH: return tanhf(z);
+    case SVM_ACT_GELU: {
+        float e;
+        const float q = upper_tail(z, e);
+        return z * (z > 0.0f ? 1.0f - q : q);
+    }
+    case SVM_ACT_SILU: return z * sigmoid_of(z);
+    case SVM_ACT_TANH: return tanh_of(z);
     case SVM_ACT_COS: return cos_of(z);
     default: return z;
     }
@@ -126,15 +162,17 @@ __device__ __forceinline__ float act_slope(int act, float z)
 {
     switch (act) {
     case SVM_ACT_RELU: return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
-    case SVM_ACT_GELU:
-        return fmaf(z * 0.39894228f, __expf(-0.5f * z * z),
-                    0.5f * (1.0f + erff(z * 0.70710678f)));
+    case SVM_ACT_GELU: {
+        float e;
+        const float q = upper_tail(z, e);
+        return fmaf(z * 0.39894228f, e, z > 0.0f ? 1.0f - q : q);
+    }
     case SVM_ACT_SILU: {
-        const float s = 1.0f / (1.0f + __expf(-z));
+        const float s = sigmoid_of(z);
         return s * fmaf(z, 1.0f - s, 1.0f);
     }
     case SVM_ACT_TANH: {
-        const float y = tanhf(z);
+        const float y = tanh_of(z);
         return fmaf(-y, y, 1.0f);
     }
     case SVM_ACT_COS: return -sin_of(z);

@@ -59,14 +59,17 @@ __device__ __forceinline__ floatx4 mfma(short8v a, short8v b, floatx4 c)
 // Products of the planes of 32-bit factors (0: leading 8 bits), the smallest
 // first.  The three that are left out (1 2, 2 1, 2 2) are below 2^-24 of the
 // whole.
-__device__ constexpr int kSegA[6] = {0, 2, 1, 0, 1, 0};
-__device__ constexpr int kSegB[6] = {2, 0, 1, 1, 0, 0};
+constexpr uint32_t kSegA = 0x010120;  // plane of product s at 4 s bits
+constexpr uint32_t kSegB = 0x001102;
+__device__ __forceinline__ int64_t plane_of(uint32_t planes, int seg)
+{
+    return (planes >> (4 * seg)) & 15;
+}
 
 struct Args {
     Factor A, B;
     int64_t m, n, k;
-    int nseg;           // 1, or 6 products of planes
-    int nk;             // steps of one of them
+    int nk;             // steps of a product (32 bits: of one of planes)
     int splits, per;    // parts of all steps, steps of a part
     unsigned tm, tn;    // tiles
     float* part;        // splits > 1: sums, splits x m x n
@@ -81,9 +84,9 @@ struct Stage {
     static constexpr int kRowLanes = ALONG ? 8 : R / 8;  // 16-byte pieces
     static constexpr int kRows = 64 / kRowLanes;         // rows of a load
     uint32_t off[2];  // byte offset in the tile, for each kind of load
-    int piece[2];     // first summed value of the piece (ALONG)
+    int piece;        // first summed value of the piece (ALONG, kind 0)
 
-    __device__ __forceinline__ void init(int64_t ld, int wave, int lane)
+    __device__ __forceinline__ void init(int64_t ld, int lane)
     {
         const int row = lane / kRowLanes, pos = lane % kRowLanes;
 #pragma unroll
@@ -96,43 +99,46 @@ struct Stage {
                 const int r = kRows == 2 ? v * 2 + row : row;
                 c = pos ^ (2 * (r & 3));
             }
-            piece[v] = c * 8;
+            if (v == 0) piece = c * 8;
             off[v] = (uint32_t)((int64_t)row * ld * 2 + c * 16);
         }
-    }
-
-    // Which of the two kinds load q of the tile is.
-    static __device__ __forceinline__ int kind(int q)
-    {
-        if (ALONG) return (q >> 1) & 1;
-        return kRows == 2 ? q & 1 : 0;
     }
 
     // Loads the tile whose first element is `base` (bytes left: `left`).
     // summed: summed values left from here (ALONG).
     __device__ __forceinline__ void load(const char* base, int64_t left,
-                                         int64_t ld, int64_t summed,
-                                         short* lds, int wave) const
+                                         int ld2, int summed, short* lds,
+                                         int wave) const
     {
         // (the range ends at a whole dword: a dword that lies half past it
         // would be returned as zero)
-        const uint32_t range = left <= 0       ? 0u
+        const uint32_t range = left <= 0          ? 0u
                                : left < kPast - 4 ? ((uint32_t)left + 3) & ~3u
-                                               : kPast;
+                                                  : kPast;
         __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
             const_cast<char*>(base), 0, (int)range, 0x00020000);
-        const bool cut = ALONG && summed < kBK;
+        uint32_t o[2] = {off[0], off[1]};
+        if (ALONG) {
+            if (piece >= summed) o[0] = kPast;
+            if ((piece ^ 32) >= summed) o[1] = kPast;
+        }
 #pragma unroll
         for (int it = 0; it < kInstr; ++it) {
             const int q = wave * kInstr + it;
-            const int v = kind(q);
-            uint32_t o = v ? off[1] : off[0];
-            if (cut && (v ? piece[1] : piece[0]) >= summed) o = kPast;
+            // which kind load q is
+            const int v = ALONG ? (q >> 1) & 1 : kRows == 2 ? q & 1 : 0;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 rs, (__attribute__((address_space(3))) void*)(lds + q * 512),
-                16, o, (uint32_t)((int64_t)q * kRows * ld * 2), 0, 0);
+                16, v ? o[1] : o[0], (uint32_t)(q * kRows) * (uint32_t)ld2, 0,
+                0);
         }
     }
+};
+
+// Where the loads of a factor are: the tile of the next step.
+struct Cursor {
+    const char* at;
+    int64_t left;  // bytes from there to the factor's end
 };
 
 // Reads a fragment: 16 rows (of the factor's other index) x 32 summed values.
@@ -304,6 +310,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
 {
     constexpr int NW = WGM * WGN;
     constexpr int FM = BM / WGM / 16, FN = BN / WGN / 16;
+    constexpr int kSegs = OT == SVM_F32 ? 6 : 1;
     constexpr int kLds = (BM + BN) * kBK;  // values of a buffer
     __shared__ __align__(1024) short lds0[kLds];
     __shared__ __align__(1024) short lds1[kLds];
@@ -319,42 +326,57 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
     Stage<BN, NW, BALONG> sb;
     Frag<BM, AALONG> fa;
     Frag<BN, BALONG> fb;
-    sa.init(p.A.ld, wave, lane);
-    sb.init(p.B.ld, wave, lane);
+    sa.init(p.A.ld, lane);
+    sb.init(p.B.ld, lane);
     fa.init(wi, lane);
     fb.init(wj, lane);
 
+    // Steps t0 .. t1 - 1 of the products of planes one after another.
     const int t0 = blockIdx.y * p.per;
-    const int all = p.nseg * p.nk;
+    const int all = kSegs * p.nk;
     const int t1 = t0 + p.per < all ? t0 + p.per : all;
-
-    // loads of step t (of all products of planes) into a buffer
-    auto load = [&](int t, short* lds) {
-        int seg = 0;
-        if (p.nseg > 1) {
-            seg = t / p.nk;
-            t -= seg * p.nk;
+    const int lda2 = (int)p.A.ld * 2, ldb2 = (int)p.B.ld * 2;
+    const int64_t stepa = AALONG ? 2 * kBK : (int64_t)kBK * lda2;
+    const int64_t stepb = BALONG ? 2 * kBK : (int64_t)kBK * ldb2;
+    int seg = kSegs > 1 ? t0 / p.nk : 0;
+    int tl = t0 - seg * p.nk;  // step of the next loads in its product
+    int todo = t1 - t0;        // steps not loaded yet
+    Cursor ca, cb;
+    auto seek = [&]() {
+        const int64_t k0 = (int64_t)tl * kBK;
+        ca.at = (const char*)p.A.data +
+                (AALONG ? i0 * lda2 + k0 * 2 : k0 * lda2 + i0 * 2);
+        ca.left = (AALONG ? (p.m - 1 - i0) * lda2 + (p.k - k0) * 2
+                          : (p.k - 1 - k0) * lda2 + (p.m - i0) * 2);
+        cb.at = (const char*)p.B.data +
+                (BALONG ? j0 * ldb2 + k0 * 2 : k0 * ldb2 + j0 * 2);
+        cb.left = (BALONG ? (p.n - 1 - j0) * ldb2 + (p.k - k0) * 2
+                          : (p.k - 1 - k0) * ldb2 + (p.n - j0) * 2);
+        if (kSegs > 1) {
+            ca.at += 2 * plane_of(kSegA, seg) * p.A.plane;
+            cb.at += 2 * plane_of(kSegB, seg) * p.B.plane;
         }
-        const int64_t k0 = (int64_t)t * kBK;
-        int64_t pa = 0, pb = 0;
-        if (p.nseg > 1) {
-            pa = kSegA[seg] * p.A.plane;
-            pb = kSegB[seg] * p.B.plane;
+    };
+    seek();
+    // Loads of the next step; past the last one they return zeros.
+    auto load = [&](short* lds) {
+        const int summed = p.k - (int64_t)tl * kBK < kBK
+                               ? (int)(p.k - (int64_t)tl * kBK)
+                               : kBK;
+        sa.load(ca.at, todo > 0 ? ca.left : 0, lda2, summed, lds, wave);
+        sb.load(cb.at, todo > 0 ? cb.left : 0, ldb2, summed, lds + BM * kBK,
+                wave);
+        --todo;
+        ++tl;
+        ca.at += stepa;
+        ca.left -= stepa;
+        cb.at += stepb;
+        cb.left -= stepb;
+        if (kSegs > 1 && tl == p.nk) {
+            tl = 0;
+            ++seg;
+            seek();
         }
-        const char* a = (const char*)p.A.data +
-                        2 * (pa + (AALONG ? i0 * p.A.ld + k0
-                                          : k0 * p.A.ld + i0));
-        const int64_t la =
-            2 * (AALONG ? (p.m - 1 - i0) * p.A.ld + p.k - k0
-                        : (p.k - 1 - k0) * p.A.ld + p.m - i0);
-        sa.load(a, la, p.A.ld, p.k - k0, lds, wave);
-        const char* b = (const char*)p.B.data +
-                        2 * (pb + (BALONG ? j0 * p.B.ld + k0
-                                          : k0 * p.B.ld + j0));
-        const int64_t lb =
-            2 * (BALONG ? (p.n - 1 - j0) * p.B.ld + p.k - k0
-                        : (p.k - 1 - k0) * p.B.ld + p.n - j0);
-        sb.load(b, lb, p.B.ld, p.k - k0, lds + BM * kBK, wave);
     };
 
     floatx4 acc[FM][FN];
@@ -366,10 +388,10 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
     short8v a0[FM], b0[FN], a1[FM], b1[FN];
     auto frags = [&](const short* lds, int h, short8v* a, short8v* b) {
 #pragma unroll
-        for (int f = 0; f < FM; ++f) a[f] = fa.read(lds, wi, f, h, lane);
-#pragma unroll
         for (int g = 0; g < FN; ++g)
             b[g] = fb.read(lds + BM * kBK, wj, g, h, lane);
+#pragma unroll
+        for (int f = 0; f < FM; ++f) a[f] = fa.read(lds, wi, f, h, lane);
     };
     auto multiply = [&](const short8v* a, const short8v* b) {
 #pragma unroll
@@ -378,29 +400,45 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
             for (int g = 0; g < FN; ++g)
                 acc[f][g] = mfma<IT>(b[g], a[f], acc[f][g]);
     };
+    // The reads of a half spread over the products of the other half.
+    constexpr int kReads = (AALONG ? FM : 2 * FM) + (BALONG ? FN : 2 * FN);
+    constexpr int kMul = FM * FN;
+    auto spread = [&]() {
+#pragma unroll
+        for (int r = 0; r < kReads; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(
+                0x008, kMul / kReads > 2 ? 2 : kMul / kReads ? kMul / kReads : 1,
+                0);
+        }
+    };
     // one step from `cur`, with the next in `oth`
-    auto step = [&](int t, short* cur, short* oth) {
+    auto step = [&](short* cur, short* oth) {
+        __builtin_amdgcn_sched_barrier(0);
         frags(cur, 1, a1, b1);
         multiply(a0, b0);
+        spread();
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(kVmcnt0);
         __syncthreads();
-        if (t + 2 < t1) load(t + 2, cur);
+        load(cur);
+        __builtin_amdgcn_sched_barrier(0);
         frags(oth, 0, a0, b0);
         multiply(a1, b1);
+        spread();
+        __builtin_amdgcn_sched_barrier(0);
     };
 
-    load(t0, lds0);
-    if (t0 + 1 < t1) load(t0 + 1, lds1);
+    load(lds0);
+    load(lds1);
     __builtin_amdgcn_s_waitcnt(kVmcnt0);
     __syncthreads();
     frags(lds0, 0, a0, b0);
-    int t = t0;
-    for (; t + 2 <= t1; t += 2) {
-        step(t, lds0, lds1);
-        step(t + 1, lds1, lds0);
+    for (int t = t0; t < t1; t += 2) {
+        step(lds0, lds1);
+        if (t + 1 < t1) step(lds1, lds0);
     }
-    if (t < t1) step(t, lds0, lds1);
+    __builtin_amdgcn_s_waitcnt(kVmcnt0);
     __syncthreads();
 
     // the wave's own part of the buffers, kRows rows of its columns at a time
@@ -570,7 +608,7 @@ void launch_tiles(const Args& a, hipStream_t s)
 template <int IT, int OT>
 void launch_any(const Args& a, int tile, hipStream_t s)
 {
-    if (tile == 256) launch_tiles<IT, OT, 256, 256, 2, 2>(a, s);
+    if (tile == 256) launch_tiles<IT, OT, 256, 256, 2, 4>(a, s);
     else if (tile == 128) launch_tiles<IT, OT, 128, 128, 2, 2>(a, s);
     else launch_tiles<IT, OT, 64, 64, 2, 2>(a, s);
 }
@@ -614,7 +652,7 @@ void product(const Product& p, Pieces& ws, hipStream_t s)
     a.n = p.n;
     a.k = p.k;
     a.e = p.e;
-    a.nseg = p.dtype == SVM_F32 ? 6 : 1;
+    const int segs = p.dtype == SVM_F32 ? 6 : 1;
     a.nk = (int)((p.k + kBK - 1) / kBK);
     // Tiles: the largest of which there are enough for every CU; then, where
     // there are still too few, the steps are split over blocks.
@@ -622,7 +660,7 @@ void product(const Product& p, Pieces& ws, hipStream_t s)
     if (tiles(p.m, p.n, 256) < kCus) tile = 128;
     if (tile == 128 && tiles(p.m, p.n, 128) < kCus) tile = 64;
     const int64_t nt = tiles(p.m, p.n, tile);
-    const int64_t steps = (int64_t)a.nseg * a.nk;
+    const int64_t steps = (int64_t)segs * a.nk;
     int64_t splits = 1;
     if (nt < kCus) splits = (2 * kCus) / nt;
     if (splits > steps / 4) splits = steps / 4;
