@@ -89,6 +89,111 @@ __device__ __forceinline__ float sin_of(float z)
     return odd ? -c : c;
 }
 
+// Eight consecutive values of a row: 16 or 32 bytes at once where `wide` says
+// that they are aligned and there, else the first `count` one by one.
+template <int DT>
+struct Eight {
+    float v[8];
+
+    __device__ __forceinline__ void load(const void* p, int64_t at, bool wide,
+                                         int count)
+    {
+        using T = Elem<DT>;
+        const T* q = (const T*)p + at;
+        if (wide) {
+            if constexpr (DT == SVM_F32) {
+                const float4 a = *(const float4*)q, b = *(const float4*)(q + 4);
+                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+                v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+            } else {
+                typedef T T8 __attribute__((ext_vector_type(8)));
+                const T8 a = *(const T8*)q;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = (float)a[e];
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e] = e < count ? (float)q[e] : 0.0f;
+        }
+    }
+
+    __device__ __forceinline__ void store(void* p, int64_t at, bool wide,
+                                          int count) const
+    {
+        using T = Elem<DT>;
+        T* q = (T*)p + at;
+        if (wide) {
+            if constexpr (DT == SVM_F32) {
+                *(float4*)q = make_float4(v[0], v[1], v[2], v[3]);
+                *(float4*)(q + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+                typedef T T8 __attribute__((ext_vector_type(8)));
+                T8 a;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a[e] = (T)v[e];
+                *(T8*)q = a;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e < count) q[e] = (T)v[e];
+        }
+    }
+};
+
+// The three bf16 parts of a 32-bit value: x = h + m + l, each part what is
+// left rounded to nearest (to zero where rounding would overflow).
+__device__ __forceinline__ void three_parts(float x, __bf16& h, __bf16& m,
+                                            __bf16& l)
+{
+    h = (__bf16)x;
+    if (!(fabsf(x) <= 3.402823466e38f)) {  // infinity, NaN: h alone
+        m = l = (__bf16)0.0f;
+        return;
+    }
+    if (!(fabsf((float)h) <= 3.402823466e38f))
+        h = __builtin_bit_cast(
+            __bf16, (unsigned short)(__builtin_bit_cast(uint32_t, x) >> 16));
+    const float r = x - (float)h;
+    m = (__bf16)r;
+    l = (__bf16)(r - (float)m);
+}
+
+// Eight values as a factor of a product keeps them: DT itself, or for 32 bits
+// three bf16 planes, `plane` values apart.
+template <int DT>
+__device__ __forceinline__ void store_factor(const float (&v)[8], void* dst,
+                                             int64_t at, int64_t plane)
+{
+    if constexpr (DT == SVM_F32) {
+        typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+        B8 part[3];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            __bf16 h, m, l;
+            three_parts(v[e], h, m, l);
+            part[0][e] = h, part[1][e] = m, part[2][e] = l;
+        }
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+            *(B8*)((__bf16*)dst + q * plane + at) = part[q];
+    } else {
+        typedef Elem<DT> T8 __attribute__((ext_vector_type(8)));
+        T8 x;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (Elem<DT>)v[e];
+        *(T8*)((Elem<DT>*)dst + at) = x;
+    }
+}
+
+// Whether the rows of an array are aligned to 16 bytes (NULL: yes).
+inline bool wide_rows(const void* p, int64_t ld, int32_t dtype)
+{
+    const int64_t row = ld * (dtype == SVM_F32 ? 4 : 2);
+    return !p || (((uintptr_t)p & 15) == 0 && row % 16 == 0);
+}
+
 // The normal distribution's upper tail at |z| and exp(-z^2 / 2): the rational
 // approximation 7.1.26 of Abramowitz and Stegun's handbook (to 7.5e-8).
 __device__ __forceinline__ float upper_tail(float z, float& e)
@@ -138,25 +243,6 @@ __device__ __forceinline__ float act_value(int act, float z)
     }
 }
 
-// act of eight values, the choice made once
-__device__ __forceinline__ void act_values(int act, float (&v)[8])
-{
-#define MSVM_EACH(A)                                            \
-    case A:                                                     \
-        _Pragma("unroll") for (int e = 0; e < 8; ++e) v[e] =    \
-            act_value(A, v[e]);                                 \
-        break
-    switch (act) {
-        MSVM_EACH(SVM_ACT_RELU);
-        MSVM_EACH(SVM_ACT_GELU);
-        MSVM_EACH(SVM_ACT_SILU);
-        MSVM_EACH(SVM_ACT_TANH);
-        MSVM_EACH(SVM_ACT_COS);
-    default: break;
-    }
-#undef MSVM_EACH
-}
-
 // act'(z)
 __device__ __forceinline__ float act_slope(int act, float z)
 {
@@ -179,5 +265,27 @@ __device__ __forceinline__ float act_slope(int act, float z)
     default: return 1.0f;
     }
 }
+
+// act and act' of eight values, the choice made once
+#define MSVM_EACH(F, A)                                                      \
+    case A:                                                                  \
+        _Pragma("unroll") for (int e = 0; e < 8; ++e) v[e] = F(A, v[e]);     \
+        break
+#define MSVM_EIGHT(NAME, F)                                                  \
+    __device__ __forceinline__ void NAME(int act, float (&v)[8])             \
+    {                                                                        \
+        switch (act) {                                                       \
+            MSVM_EACH(F, SVM_ACT_RELU);                                      \
+            MSVM_EACH(F, SVM_ACT_GELU);                                      \
+            MSVM_EACH(F, SVM_ACT_SILU);                                      \
+            MSVM_EACH(F, SVM_ACT_TANH);                                      \
+            MSVM_EACH(F, SVM_ACT_COS);                                       \
+        default: break;                                                      \
+        }                                                                    \
+    }
+MSVM_EIGHT(act_values, act_value)
+MSVM_EIGHT(act_slopes, act_slope)
+#undef MSVM_EIGHT
+#undef MSVM_EACH
 
 }  // namespace msvm

@@ -6,32 +6,69 @@ namespace msvm {
 
 namespace {
 
-// dZ = dY act'(Z), and the sums of its columns over this block's rows
-constexpr int kGradRows = 64;
+// dZ = dY act'(Z) as a factor of the products (in 32 bits: three planes; its
+// rows end in zeros up to a multiple of 8), and the sums of its columns over
+// this block's rows.  One pass over dY and Z: 8 columns to a thread, 32
+// threads side by side, 8 rows at once.
+constexpr int kGradCols = 256, kGradLanes = 8;
+
+struct GradArgs {
+    const void *dY, *Z;
+    int64_t ldg, ldz, m, n, rows;  // rows of a block
+    void* dZ;
+    int64_t ldd, plane;
+    float* part;
+    int act;
+    bool wide;
+};
 
 template <int DT>
-__global__ __launch_bounds__(256) void k_act_grad(
-    const void* dY_, int64_t ldg, const void* Z_, int64_t ldz, int act,
-    int64_t m, int64_t n, void* dZ_, int64_t ldd, float* part)
+__global__ __launch_bounds__(256) void k_act_grad(GradArgs p)
 {
-    using T = Elem<DT>;
-    const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t i0 = (int64_t)blockIdx.y * kGradRows;
-    if (j >= n) {  // the zeros that end the rows of dZ
-        if (dZ_ && j < ldd)
-            for (int64_t i = i0; i < m && i < i0 + kGradRows; ++i)
-                ((T*)dZ_)[i * ldd + j] = (T)0.0f;
-        return;
+    __shared__ float red[kGradLanes][kGradCols];
+    const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+    const int64_t j = (int64_t)blockIdx.x * kGradCols + tx * 8;
+    const int64_t i0 = (int64_t)blockIdx.y * p.rows;
+    const int64_t i1 = i0 + p.rows < p.m ? i0 + p.rows : p.m;
+    const int count = p.n - j >= 8 ? 8 : p.n - j > 0 ? (int)(p.n - j) : 0;
+    const bool wide = p.wide && count == 8;
+    float sum[8] = {};
+    if (count > 0) {
+#pragma unroll 2
+        for (int64_t i = i0 + ty; i < i1; i += kGradLanes) {
+            Eight<DT> g, z;
+            g.load(p.dY, i * p.ldg + j, wide, count);
+            if (p.Z) {
+                z.load(p.Z, i * p.ldz + j, wide, count);
+                act_slopes(p.act, z.v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    g.v[e] = e < count ? g.v[e] * z.v[e] : 0.0f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += g.v[e];
+            if (p.dZ) store_factor<DT>(g.v, p.dZ, i * p.ldd + j, p.plane);
+        }
     }
-    const int64_t i1 = i0 + kGradRows < m ? i0 + kGradRows : m;
-    float sum = 0.0f;
-    for (int64_t i = i0; i < i1; ++i) {
-        float g = (float)((const T*)dY_)[i * ldg + j];
-        if (Z_) g *= act_slope(act, (float)((const T*)Z_)[i * ldz + j]);
-        sum += g;
-        if (dZ_) ((T*)dZ_)[i * ldd + j] = (T)g;
-    }
-    if (part) part[(int64_t)blockIdx.y * n + j] = sum;
+    if (!p.part) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) red[ty][tx * 8 + e] = sum[e];
+    __syncthreads();
+    const int64_t c = (int64_t)blockIdx.x * kGradCols + threadIdx.x;
+    if (c >= p.n) return;
+    float s = 0.0f;
+#pragma unroll
+    for (int r = 0; r < kGradLanes; ++r) s += red[r][threadIdx.x];
+    p.part[blockIdx.y * p.n + c] = s;
+}
+
+// Rows of a block: some 2048 blocks in all, at least 16 rows to one.
+int64_t grad_rows(int64_t m, int64_t n)
+{
+    const int64_t across = (n + kGradCols - 1) / kGradCols;
+    int64_t rows = (m * across + 2047) / 2048;
+    rows = (rows + kGradLanes - 1) / kGradLanes * kGradLanes;
+    return rows < 16 ? 16 : rows;
 }
 
 // Zeros to rows x cols of an array.
@@ -55,18 +92,31 @@ void launch_zero(const svm_array& a, hipStream_t s)
     });
 }
 
+// 16 columns to a block, 16 threads to a column.
 template <int DT>
 __global__ __launch_bounds__(256) void k_column_sums(
     const float* part0, const float* part1, int64_t np, int64_t cols,
     void* out0, void* out1)
 {
+    __shared__ float red[16][17];
     const float* part = blockIdx.y ? part1 : part0;
     void* out = blockIdx.y ? out1 : out0;
-    const int64_t j = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (j >= cols || !out) return;
-    double sum = 0.0;
-    for (int64_t i = 0; i < np; ++i) sum += part[i * cols + j];
-    ((Elem<DT>*)out)[j] = (Elem<DT>)(float)sum;
+    if (!out) return;
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
+    const int64_t j = (int64_t)blockIdx.x * 16 + tx;
+    float sum = 0.0f;
+    if (j < cols) {
+#pragma unroll 8
+        for (int64_t i = ty; i < np; i += 16) sum += part[i * cols + j];
+    }
+    red[ty][tx] = sum;
+    __syncthreads();
+    if (ty == 0 && j < cols) {
+        sum = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum += red[r][tx];
+        ((Elem<DT>*)out)[j] = (Elem<DT>)sum;
+    }
 }
 
 }  // namespace
@@ -78,8 +128,8 @@ void launch_column_sums(const float* part0, const float* part1, int64_t np,
     if (!out0 && !out1) return;
     for_dtype(dtype, [&]<int DT>() {
         hipLaunchKernelGGL((k_column_sums<DT>),
-                           dim3((unsigned)((cols + 255) / 256), 2), dim3(256),
-                           0, s, part0, part1, np, cols, out0, out1);
+                           dim3((unsigned)((cols + 15) / 16), out1 ? 2 : 1),
+                           dim3(256), 0, s, part0, part1, np, cols, out0, out1);
     });
 }
 
@@ -89,7 +139,7 @@ namespace {
 // it so, else a copy in the workspace (32 bits: in three planes).
 Factor factor_of(const svm_array& a, bool along, Pieces& ws, hipStream_t s)
 {
-    Factor f{a.data, a.ld, 0, along, (const float*)a.data, a.ld};
+    Factor f{a.data, a.ld, 0, along};
     if (factor_fits(a, along)) return f;
     f.ld = (a.cols + 7) / 8 * 8;
     f.plane = a.rows * f.ld;
@@ -127,30 +177,31 @@ void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
     const int32_t t = a.dY.dtype;
     const bool dx = a.dX.data, dw = a.dW.data, db = a.dbias.data;
     const bool slope = a.act != SVM_ACT_NONE;
-    const int64_t np = (m + kGradRows - 1) / kGradRows;
-    svm_array dZ = a.dY;
-    if (slope && (dx || dw)) {
-        dZ.ld = (n + 7) / 8 * 8;
-        dZ.data = ws.take<char>(m * dZ.ld * dtype_bytes(t));
+    // dY itself serves as dZ where there is no slope and its rows can be
+    // read as they are; else one pass makes dZ, and the sums with it
+    const bool copy =
+        (dx || dw) && (slope || !factor_fits(a.dY, dx));
+    Factor dz{a.dY.data, a.dY.ld, 0, true};
+    if (copy) {
+        dz.ld = (n + 7) / 8 * 8;
+        dz.plane = m * dz.ld;
+        dz.data = ws.take<uint16_t>((t == SVM_F32 ? 3 : 1) * dz.plane);
     }
+    const int64_t rows = grad_rows(m, n), np = (m + rows - 1) / rows;
     float* part = db ? ws.take<float>(np * n) : nullptr;
-    if (ws.run && np > 0 && (slope || db)) {
+    if (ws.run && m > 0 && (copy || db)) {
+        GradArgs g{a.dY.data, slope ? a.Z.data : nullptr,
+                   a.dY.ld,   a.Z.ld,
+                   m,         n,
+                   rows,      copy ? const_cast<void*>(dz.data) : nullptr,
+                   dz.ld,     dz.plane,
+                   part,      a.act,
+                   wide_rows(a.dY.data, a.dY.ld, t) &&
+                       (!slope || wide_rows(a.Z.data, a.Z.ld, t))};
+        const dim3 grid((unsigned)((n + kGradCols - 1) / kGradCols),
+                        (unsigned)np);
         for_dtype(t, [&]<int DT>() {
-            // rows in slices of at most 65535 blocks (the grid's y)
-            for (int64_t b0 = 0; b0 < np; b0 += 65535) {
-                const int64_t nb = np - b0 < 65535 ? np - b0 : 65535;
-                const int64_t i0 = b0 * kGradRows;
-                using T = Elem<DT>;
-                hipLaunchKernelGGL(
-                    (k_act_grad<DT>),
-                    dim3((unsigned)((dZ.ld + 255) / 256), (unsigned)nb),
-                    dim3(256), 0, s, (const T*)a.dY.data + i0 * a.dY.ld,
-                    a.dY.ld,
-                    slope ? (const T*)a.Z.data + i0 * a.Z.ld : nullptr,
-                    a.Z.ld, a.act, m - i0, n,
-                    slope && (dx || dw) ? (T*)dZ.data + i0 * dZ.ld : nullptr,
-                    dZ.ld, db ? part + b0 * n : nullptr);
-            }
+            hipLaunchKernelGGL((k_act_grad<DT>), grid, dim3(256), 0, s, g);
         });
     }
     if (ws.run && db)
@@ -160,14 +211,6 @@ void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
         if (dw && ws.run) launch_zero(a.dW, s);
         return;
     }
-    // both products read one copy of dZ, where it has to be copied at all
-    svm_array part_dz = dZ;
-    Factor dz;
-    if (dx && slope && t != SVM_F32) {
-        // the workspace's own rows end in zeros up to a multiple of 8
-        part_dz.cols = dZ.ld;
-    }
-    dz = factor_of(part_dz, dx, ws, s);
     if (dx) {
         Product p;
         p.A = dz;

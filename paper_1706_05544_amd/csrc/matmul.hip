@@ -35,12 +35,12 @@ constexpr int kBK = 64;         // summed values of a step
 // An address past every descriptor: the rows of a tile end below it, and
 // added to a tile's own offsets it does not wrap.
 constexpr uint32_t kPast = 0x80000000u;
-constexpr int kVmcnt0 = 0x0f70;  // s_waitcnt: loads only
 
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef short short8v __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef int intx4 __attribute__((ext_vector_type(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
 template <int DT>
@@ -76,6 +76,24 @@ struct Args {
     Epilogue e;
     int wide;           // outputs and residual in aligned rows of 16 bytes
 };
+
+// 16 bytes for each lane from the buffer `rs` at off + soff into LDS, lane
+// after lane.  In assembly, so that the compiler does not wait for loads
+// under way before LDS reads that it takes to depend on them; meet() waits
+// for those that a step needs.  It has no output register; nothing else in
+// this file uses m0 (LDS reads and writes of gfx950 do not).
+__device__ __forceinline__ void lds_load(intx4 rs, short* lds, uint32_t off,
+                                         uint32_t soff)
+{
+    const uint32_t to =
+        (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short*)lds;
+    asm volatile(
+        "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+        "buffer_load_dwordx4 %1, %2, %3 offen lds"
+        :
+        : "s"(to), "v"(off), "s"(rs), "s"(soff)
+        : "memory");
+}
 
 // The lane's share of a factor's tile loads: R rows (ALONG) or columns.
 template <int R, int NW, bool ALONG>
@@ -115,8 +133,9 @@ struct Stage {
         const uint32_t range = left <= 0          ? 0u
                                : left < kPast - 4 ? ((uint32_t)left + 3) & ~3u
                                                   : kPast;
-        __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
-            const_cast<char*>(base), 0, (int)range, 0x00020000);
+        const uint64_t at = (uint64_t)base;
+        const intx4 rs = {(int)(uint32_t)at, (int)(uint32_t)(at >> 32),
+                          (int)range, 0x00020000};
         uint32_t o[2] = {off[0], off[1]};
         if (ALONG) {
             if (piece >= summed) o[0] = kPast;
@@ -127,13 +146,26 @@ struct Stage {
             const int q = wave * kInstr + it;
             // which kind load q is
             const int v = ALONG ? (q >> 1) & 1 : kRows == 2 ? q & 1 : 0;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(
-                rs, (__attribute__((address_space(3))) void*)(lds + q * 512),
-                16, v ? o[1] : o[0], (uint32_t)(q * kRows) * (uint32_t)ld2, 0,
-                0);
+            lds_load(rs, lds + q * 512, v ? o[1] : o[0],
+                     (uint32_t)(q * kRows) * (uint32_t)ld2);
         }
     }
 };
+
+// Waits until at most LEFT of the wave's loads are under way (they end in
+// order) and its LDS reads are done, then for the block's other waves.
+template <int LEFT>
+__device__ __forceinline__ void meet()
+{
+    static_assert(LEFT < 64, "vmcnt");
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    // vmcnt LEFT, expcnt not waited, lgkmcnt 0
+    __builtin_amdgcn_s_waitcnt((LEFT & 15) | (LEFT >> 4) << 14 | 7 << 4);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 // Where the loads of a factor are: the tile of the next step.
 struct Cursor {
@@ -185,70 +217,25 @@ struct Frag {
     }
 };
 
-// Eight consecutive values of an output row.
-template <int DT>
-struct Eight {
-    float v[8];
-
-    __device__ __forceinline__ void load(const void* p, int64_t at, bool wide,
-                                         int count)
-    {
-        using T = Elem<DT>;
-        const T* q = (const T*)p + at;
-        if (wide) {
-            if constexpr (DT == SVM_F32) {
-                const float4 a = *(const float4*)q, b = *(const float4*)(q + 4);
-                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-                v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-            } else {
-                typedef T T8 __attribute__((ext_vector_type(8)));
-                const T8 a = *(const T8*)q;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = (float)a[e];
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] = e < count ? (float)q[e] : 0.0f;
-        }
-    }
-
-    __device__ __forceinline__ void store(void* p, int64_t at, bool wide,
-                                          int count) const
-    {
-        using T = Elem<DT>;
-        T* q = (T*)p + at;
-        if (wide) {
-            if constexpr (DT == SVM_F32) {
-                *(float4*)q = make_float4(v[0], v[1], v[2], v[3]);
-                *(float4*)(q + 4) = make_float4(v[4], v[5], v[6], v[7]);
-            } else {
-                typedef T T8 __attribute__((ext_vector_type(8)));
-                T8 a;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) a[e] = (T)v[e];
-                *(T8*)q = a;
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < count) q[e] = (T)v[e];
-        }
-    }
-};
-
 // A sum of 32-bit factors that is not finite, again from the factors
-// themselves: an infinity has zeros or other signs in its lower planes.
+// themselves, which their planes add up to: an infinity has zeros in its
+// lower planes, and its products with another factor's differ in sign.
 __device__ __forceinline__ float exact_sum(const Factor& A, const Factor& B,
                                            int64_t i, int64_t j, int64_t k)
 {
-    const float* a = A.exact + (A.along ? i * A.exact_ld : i);
-    const float* b = B.exact + (B.along ? j * B.exact_ld : j);
-    const int64_t sa = A.along ? 1 : A.exact_ld;
-    const int64_t sb = B.along ? 1 : B.exact_ld;
+    const __bf16* a = (const __bf16*)A.data + (A.along ? i * A.ld : i);
+    const __bf16* b = (const __bf16*)B.data + (B.along ? j * B.ld : j);
+    const int64_t sa = A.along ? 1 : A.ld, sb = B.along ? 1 : B.ld;
     float sum = 0.0f;
 #pragma unroll 1
-    for (int64_t r = 0; r < k; ++r) sum = fmaf(a[r * sa], b[r * sb], sum);
+    for (int64_t r = 0; r < k; ++r) {
+        const __bf16 *x = a + r * sa, *y = b + r * sb;
+        const float u = (float)x[0] + ((float)x[A.plane] +
+                                       (float)x[2 * A.plane]);
+        const float v = (float)y[0] + ((float)y[B.plane] +
+                                       (float)y[2 * B.plane]);
+        sum = fmaf(u, v, sum);
+    }
     return sum;
 }
 
@@ -304,16 +291,23 @@ __device__ __forceinline__ void tile_of(unsigned b, unsigned tm, unsigned tn,
 }
 
 // IT: type of the 16-bit factors; OT: type of the outputs.
-template <int IT, int OT, int BM, int BN, int WGM, int WGN, bool AALONG,
-          bool BALONG>
+// ST: buffers, and so steps whose loads are under way.
+template <int IT, int OT, int BM, int BN, int WGM, int WGN, int ST,
+          bool AALONG, bool BALONG>
 __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
 {
     constexpr int NW = WGM * WGN;
     constexpr int FM = BM / WGM / 16, FN = BN / WGN / 16;
     constexpr int kSegs = OT == SVM_F32 ? 6 : 1;
     constexpr int kLds = (BM + BN) * kBK;  // values of a buffer
+    // (arrays of their own, so that the compiler knows a buffer that is being
+    // loaded from one that is being read)
     __shared__ __align__(1024) short lds0[kLds];
     __shared__ __align__(1024) short lds1[kLds];
+    __shared__ __align__(1024) short lds2[ST > 2 ? kLds : 8];
+    __shared__ __align__(1024) short lds3[ST > 2 ? kLds : 8];
+    static_assert(ST == 2 || ST == 4, "buffers");
+    constexpr int kLoads = (BM + BN) / 8 / NW;  // of a wave in a step
 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -418,9 +412,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
         frags(cur, 1, a1, b1);
         multiply(a0, b0);
         spread();
-        __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(kVmcnt0);
-        __syncthreads();
+        meet<(ST - 2) * kLoads>();
         load(cur);
         __builtin_amdgcn_sched_barrier(0);
         frags(oth, 0, a0, b0);
@@ -431,15 +423,21 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
 
     load(lds0);
     load(lds1);
-    __builtin_amdgcn_s_waitcnt(kVmcnt0);
-    __syncthreads();
-    frags(lds0, 0, a0, b0);
-    for (int t = t0; t < t1; t += 2) {
-        step(lds0, lds1);
-        if (t + 1 < t1) step(lds1, lds0);
+    if (ST > 2) {
+        load(lds2);
+        load(lds3);
     }
-    __builtin_amdgcn_s_waitcnt(kVmcnt0);
-    __syncthreads();
+    meet<(ST - 1) * kLoads>();
+    frags(lds0, 0, a0, b0);
+    for (int t = t0; t < t1; t += ST) {
+        step(lds0, lds1);
+        if (t + 1 < t1) step(lds1, ST > 2 ? lds2 : lds0);
+        if (ST > 2) {
+            if (t + 2 < t1) step(lds2, lds3);
+            if (t + 3 < t1) step(lds3, lds0);
+        }
+    }
+    meet<0>();
 
     // the wave's own part of the buffers, kRows rows of its columns at a time
     constexpr int kCols = FN * 16, kRows = BM / WGM < 64 ? BM / WGM : 64;
@@ -532,85 +530,44 @@ __global__ __launch_bounds__(256) void k_join(Args p)
 
 // ---- factors that cannot be read as they are
 
-// The three bf16 parts of a 32-bit value: x = h + m + l, each part what is
-// left rounded to nearest (to zero where rounding would overflow).
-__device__ __forceinline__ void three_parts(float x, __bf16& h, __bf16& m,
-                                            __bf16& l)
-{
-    h = (__bf16)x;
-    if (!(fabsf(x) <= 3.402823466e38f)) {  // infinity, NaN: h alone
-        m = l = (__bf16)0.0f;
-        return;
-    }
-    if (!(fabsf((float)h) <= 3.402823466e38f))
-        h = __builtin_bit_cast(
-            __bf16, (unsigned short)(__builtin_bit_cast(uint32_t, x) >> 16));
-    const float r = x - (float)h;
-    m = (__bf16)r;
-    l = (__bf16)(r - (float)m);
-}
-
 template <int DT>
 __global__ __launch_bounds__(256) void k_planes(const Elem<DT>* X, int64_t ld,
                                                 int64_t rows, int64_t cols,
                                                 void* dst, int64_t ldp,
-                                                int64_t plane)
+                                                int64_t plane, bool wide)
 {
     const int64_t groups = ldp / 8, all = rows * groups;
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all;
          t += (int64_t)gridDim.x * 256) {
         const int64_t i = t / groups, j = t % groups * 8;
-        const Elem<DT>* x = X + i * ld + j;
-        if constexpr (DT == SVM_F32) {
-            typedef __bf16 B8 __attribute__((ext_vector_type(8)));
-            B8 part[3];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                __bf16 h, m, l;
-                three_parts(j + e < cols ? x[e] : 0.0f, h, m, l);
-                part[0][e] = h, part[1][e] = m, part[2][e] = l;
-            }
-#pragma unroll
-            for (int q = 0; q < 3; ++q)
-                *(B8*)((__bf16*)dst + q * plane + i * ldp + j) = part[q];
-        } else {
-            typedef Elem<DT> T8 __attribute__((ext_vector_type(8)));
-            T8 v;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[e] = j + e < cols ? x[e] : (Elem<DT>)0.0f;
-            *(T8*)((Elem<DT>*)dst + i * ldp + j) = v;
-        }
+        const int count = cols - j >= 8 ? 8 : cols - j > 0 ? (int)(cols - j) : 0;
+        Eight<DT> x;
+        x.load(X, i * ld + j, wide && count == 8, count);
+        store_factor<DT>(x.v, dst, i * ldp + j, plane);
     }
 }
 
-bool wide_rows(const void* p, int64_t ld, int32_t dtype)
-{
-    return !p || (((uintptr_t)p & 15) == 0 &&
-                  (ld * (int64_t)dtype_bytes(dtype)) % 16 == 0);
-}
-
-template <int IT, int OT, int BM, int BN, int WGM, int WGN>
+template <int IT, int OT, int BM, int BN, int WGM, int WGN, int ST>
 void launch_tiles(const Args& a, hipStream_t s)
 {
     const dim3 grid(a.tm * a.tn, (unsigned)a.splits), block(64 * WGM * WGN);
     if (a.A.along && a.B.along)
-        hipLaunchKernelGGL((k_product<IT, OT, BM, BN, WGM, WGN, true, true>),
+        hipLaunchKernelGGL((k_product<IT, OT, BM, BN, WGM, WGN, ST, true, true>),
                            grid, block, 0, s, a);
     else if (a.A.along)
-        hipLaunchKernelGGL((k_product<IT, OT, BM, BN, WGM, WGN, true, false>),
+        hipLaunchKernelGGL((k_product<IT, OT, BM, BN, WGM, WGN, ST, true, false>),
                            grid, block, 0, s, a);
     else
-        hipLaunchKernelGGL((k_product<IT, OT, BM, BN, WGM, WGN, false, false>),
+        hipLaunchKernelGGL((k_product<IT, OT, BM, BN, WGM, WGN, ST, false, false>),
                            grid, block, 0, s, a);
 }
 
 template <int IT, int OT>
 void launch_any(const Args& a, int tile, hipStream_t s)
 {
-    if (tile == 256) launch_tiles<IT, OT, 256, 256, 2, 4>(a, s);
-    else if (tile == 128) launch_tiles<IT, OT, 128, 128, 2, 2>(a, s);
-    else launch_tiles<IT, OT, 64, 64, 2, 2>(a, s);
+    if (tile == 256) launch_tiles<IT, OT, 256, 256, 2, 4, 2>(a, s);
+    else if (tile == 128) launch_tiles<IT, OT, 128, 128, 2, 2, 4>(a, s);
+    else launch_tiles<IT, OT, 64, 64, 2, 2, 4>(a, s);
 }
 
 int64_t tiles(int64_t m, int64_t n, int t)
@@ -638,7 +595,8 @@ void launch_planes(const svm_array& a, void* dst, int64_t ldp, int64_t plane,
         hipLaunchKernelGGL((k_planes<DT>),
                            dim3((unsigned)(nb < 16384 ? nb : 16384)),
                            dim3(256), 0, s, (const Elem<DT>*)a.data, a.ld,
-                           a.rows, a.cols, dst, ldp, plane);
+                           a.rows, a.cols, dst, ldp, plane,
+                           wide_rows(a.data, a.ld, a.dtype));
     });
 }
 

@@ -15,9 +15,6 @@ struct Factor {
     int64_t ld;
     int64_t plane;  // elements from one plane to the next
     bool along;
-    // the 32-bit values themselves: for sums that are not finite
-    const float* exact;
-    int64_t exact_ld;
 };
 
 // What happens to the sums.

@@ -537,18 +537,6 @@ def _act(act) -> int:
     return act
 
 
-def _dtype(t, what: str) -> int:
-    if not _DTYPES:
-        import torch
-        _DTYPES.update({torch.float32: SVM_F32, torch.bfloat16: SVM_BF16,
-                        torch.float16: SVM_F16})
-    d = _DTYPES.get(getattr(t, "dtype", None)) if _is_torch(t) else None
-    if d is None or not t.is_cuda:
-        raise SvmError(SVM_E_UNSUPPORTED, "%s must be a float32, bfloat16 or "
-                       "float16 tensor in device memory" % what)
-    return d
-
-
 def _rows_of(t):
     """(rows, cols, ld) of a tensor whose rows are at one stride, else
     None."""
@@ -556,8 +544,11 @@ def _rows_of(t):
     if nd == 0:
         return None
     cols = t.shape[-1]
-    if t.numel() == 0:
+    n = t.numel()
+    if n == 0:
         return (0 if cols else 1), cols, cols
+    if t.is_contiguous():
+        return n // cols, cols, cols
     st = t.stride()
     if cols > 1 and st[-1] != 1:
         return None
@@ -573,34 +564,9 @@ def _rows_of(t):
         rows *= size
     if rows == 1:
         ld = cols
-    if rows and ld < cols:
+    if ld < cols:
         return None
-    return rows, cols, max(ld, cols)
-
-
-def _arr(t, what: str, call, out: bool = False):
-    """svm_array of a tensor; a copy with rows side by side where it is an
-    input that has none (kept alive by the call)."""
-    if t is None:
-        return None
-    d = _dtype(t, what)
-    if t.device != call.device:
-        raise SvmError(SVM_E_INVALID, "%s is on another device" % what)
-    r = _rows_of(t)
-    if r is None:
-        if out:
-            raise SvmError(SVM_E_INVALID, "%s: its rows must be at one "
-                           "stride, the values of a row side by side" % what)
-        t = t.contiguous()
-        r = _rows_of(t)
-        if r is None:
-            raise SvmError(SVM_E_INVALID, "%s must have a dimension" % what)
-    call.keep.append(t)
-    return svm_array(t.data_ptr(), r[0], r[1], r[2], d, 1)
-
-
-def _ref(a):
-    return None if a is None else ct.byref(a)
+    return rows, cols, ld
 
 
 class _Call:
@@ -608,17 +574,59 @@ class _Call:
     uses."""
 
     def __init__(self, t, stream):
-        import torch
         if not _is_torch(t) or not t.is_cuda:
             raise SvmError(SVM_E_UNSUPPORTED,
                            "this call takes tensors in device memory")
+        import torch
+        if not _DTYPES:
+            _DTYPES.update({torch.float32: SVM_F32, torch.bfloat16: SVM_BF16,
+                            torch.float16: SVM_F16})
         self.device = t.device
-        self.index = t.device.index or 0
-        cur = torch.cuda.current_stream(t.device)
-        self.stream = cur if stream is None else stream
-        self.handle = self.stream.cuda_stream
-        self.other = self.handle != cur.cuda_stream
+        self.index = t.get_device()
+        cur = torch._C._cuda_getCurrentRawStream(self.index)
+        self.stream = stream
+        self.handle = cur if stream is None else stream.cuda_stream
+        self.other = self.handle != cur
         self.keep = []
+
+    def arr(self, t, what: str, out: bool = False):
+        """svm_array of a tensor (None: None); a copy with rows side by side
+        where it is an input that has none."""
+        if t is None:
+            return None
+        d = _DTYPES.get(getattr(t, "dtype", None)) if _is_torch(t) else None
+        if d is None or t.get_device() < 0:
+            raise SvmError(SVM_E_UNSUPPORTED, "%s must be a float32, bfloat16 "
+                           "or float16 tensor in device memory" % what)
+        if t.get_device() != self.index:
+            raise SvmError(SVM_E_INVALID, "%s is on another device" % what)
+        r = _rows_of(t)
+        if r is None:
+            if out:
+                raise SvmError(SVM_E_INVALID, "%s: its rows must be at one "
+                               "stride, the values of a row side by side"
+                               % what)
+            t = t.contiguous()
+            r = _rows_of(t)
+            if r is None:
+                raise SvmError(SVM_E_INVALID, "%s must have a dimension"
+                               % what)
+        self.keep.append(t)
+        return svm_array(t.data_ptr(), r[0], r[1], r[2], d, 1)
+
+    def floats(self, t, rows: int, what: str) -> int:
+        """Address of a float32 value for each row."""
+        import torch
+        if not _is_torch(t) or t.dtype != torch.float32 or \
+                t.get_device() < 0:
+            raise SvmError(SVM_E_UNSUPPORTED, "%s must be a float32 tensor in "
+                           "device memory" % what)
+        if t.numel() != rows or t.get_device() != self.index:
+            raise SvmError(SVM_E_INVALID, "%s must have a value for each row, "
+                           "on the same device" % what)
+        t = t.contiguous()
+        self.keep.append(t)
+        return t.data_ptr()
 
     def empty(self, shape, dtype):
         import torch
@@ -627,15 +635,18 @@ class _Call:
         return t
 
     def work(self, nbytes: int):
+        """Address of a workspace (None for no bytes)."""
+        if not nbytes:
+            return None
         import torch
-        return self.empty((nbytes,), torch.uint8) if nbytes else None
+        return self.empty((nbytes,), torch.uint8).data_ptr()
 
     def ready(self):
         """Before the launch: on another stream than torch's current one the
         work waits for what that one has queued (copies of inputs, earlier
         users of the memory given out here)."""
-        import torch
         if self.other:
+            import torch
             self.stream.wait_stream(torch.cuda.current_stream(self.device))
 
     def done(self):
@@ -644,6 +655,10 @@ class _Call:
         if self.other:
             for t in self.keep:
                 t.record_stream(self.stream)
+
+
+def _ref(a):
+    return None if a is None else ct.byref(a)
 
 
 def _ptr(t):
@@ -656,7 +671,7 @@ def svm_linear(X, W, bias=None, residual=None, act="none", save: bool = False,
     Z when `save`.  `out` receives Y when given (it may be `residual`)."""
     lib = load()
     c = _Call(X, stream)
-    a, w = _arr(X, "X", c), _arr(W, "W", c)
+    a, w = c.arr(X, "X"), c.arr(W, "W")
     shape = X.shape[:-1] + (w.rows,)
     Y = out if out is not None else c.empty(shape, X.dtype)
     Z = c.empty(shape, X.dtype) if save else None
@@ -666,10 +681,10 @@ def svm_linear(X, W, bias=None, residual=None, act="none", save: bool = False,
     ws = c.work(need.value)
     c.ready()
     _check(lib.svm_linear(ct.byref(a), ct.byref(w),
-                          _ref(_arr(bias, "bias", c)),
-                          _ref(_arr(residual, "residual", c)), _act(act),
-                          ct.byref(_arr(Y, "out", c, True)),
-                          _ref(_arr(Z, "Z", c, True)), _ptr(ws), need.value,
+                          _ref(c.arr(bias, "bias")),
+                          _ref(c.arr(residual, "residual")), _act(act),
+                          ct.byref(c.arr(Y, "out", True)),
+                          _ref(c.arr(Z, "Z", True)), ws, need.value,
                           c.index, c.handle))
     c.done()
     return (Y, Z) if save else Y
@@ -681,23 +696,23 @@ def svm_linear_backward(dY, X, W, Z=None, act="none", need=(True, True, True),
     The residual's gradient is dY itself."""
     lib = load()
     c = _Call(dY, stream)
-    g, a, w = _arr(dY, "dY", c), _arr(X, "X", c), _arr(W, "W", c)
+    g, a, w = c.arr(dY, "dY"), c.arr(X, "X"), c.arr(W, "W")
     dX = c.empty(X.shape, dY.dtype) if need[0] else None
     dW = c.empty(W.shape, dY.dtype) if need[1] else None
     db = c.empty((g.cols,), dY.dtype) if need[2] else None
-    rx, rw, rb = (_arr(dX, "dX", c, True), _arr(dW, "dW", c, True),
-                  _arr(db, "dbias", c, True))
+    rx, rw, rb = (c.arr(dX, "dX", True), c.arr(dW, "dW", True),
+                  c.arr(db, "dbias", True))
     size = ct.c_int64()
     act = _act(act)
     _check(lib.svm_linear_backward_workspace(
         ct.byref(g), _ref(a), _ref(w), act, _ref(rx), _ref(rw), _ref(rb),
         ct.byref(size)))
     ws = c.work(size.value)
-    z = _arr(Z, "Z", c)
+    z = c.arr(Z, "Z")
     c.ready()
     _check(lib.svm_linear_backward(
         ct.byref(g), _ref(a), _ref(w), _ref(z), act, _ref(rx), _ref(rw),
-        _ref(rb), _ptr(ws), size.value, c.index, c.handle))
+        _ref(rb), ws, size.value, c.index, c.handle))
     c.done()
     return dX, dW, db
 
@@ -709,30 +724,17 @@ def svm_layer_norm(X, weight=None, bias=None, eps: float = 1e-5,
     import torch
     lib = load()
     c = _Call(X, stream)
-    a = _arr(X, "X", c)
+    a = c.arr(X, "X")
     Y = out if out is not None else c.empty(X.shape, X.dtype)
     mean = c.empty(X.shape[:-1], torch.float32) if save else None
     rstd = c.empty(X.shape[:-1], torch.float32) if save else None
-    w, b = _arr(weight, "weight", c), _arr(bias, "bias", c)
+    w, b = c.arr(weight, "weight"), c.arr(bias, "bias")
     c.ready()
     _check(lib.svm_layer_norm(ct.byref(a), _ref(w), _ref(b), eps,
-                              ct.byref(_arr(Y, "out", c, True)), _ptr(mean),
+                              ct.byref(c.arr(Y, "out", True)), _ptr(mean),
                               _ptr(rstd), c.index, c.handle))
     c.done()
     return (Y, mean, rstd) if save else Y
-
-
-def _float_rows(t, rows: int, what: str, call):
-    import torch
-    if not _is_torch(t) or not t.is_cuda or t.dtype != torch.float32:
-        raise SvmError(SVM_E_UNSUPPORTED, "%s must be a float32 tensor in "
-                       "device memory" % what)
-    if t.numel() != rows:
-        raise SvmError(SVM_E_INVALID, "%s must have a value for each row"
-                       % what)
-    t = t.contiguous()
-    call.keep.append(t)
-    return t.data_ptr()
 
 
 def svm_layer_norm_backward(dY, X, mean, rstd, weight=None, residual=None,
@@ -742,9 +744,9 @@ def svm_layer_norm_backward(dY, X, mean, rstd, weight=None, residual=None,
     norm."""
     lib = load()
     c = _Call(dY, stream)
-    g, a = _arr(dY, "dY", c), _arr(X, "X", c)
-    mp = _float_rows(mean, g.rows, "mean", c)
-    rp = _float_rows(rstd, g.rows, "rstd", c)
+    g, a = c.arr(dY, "dY"), c.arr(X, "X")
+    mp = c.floats(mean, g.rows, "mean")
+    rp = c.floats(rstd, g.rows, "rstd")
     dX = c.empty(X.shape, dY.dtype) if need[0] else None
     dw = c.empty((g.cols,), dY.dtype) if need[1] else None
     db = c.empty((g.cols,), dY.dtype) if need[2] else None
@@ -753,12 +755,12 @@ def svm_layer_norm_backward(dY, X, mean, rstd, weight=None, residual=None,
         _check(lib.svm_layer_norm_backward_workspace(g.rows, g.cols,
                                                      ct.byref(size)))
     ws = c.work(size.value)
-    w, r = _arr(weight, "weight", c), _arr(residual, "residual", c)
+    w, r = c.arr(weight, "weight"), c.arr(residual, "residual")
     c.ready()
     _check(lib.svm_layer_norm_backward(
         ct.byref(g), ct.byref(a), mp, rp, _ref(w), _ref(r),
-        _ref(_arr(dX, "dX", c, True)), _ref(_arr(dw, "dweight", c, True)),
-        _ref(_arr(db, "dbias", c, True)), _ptr(ws), size.value, c.index,
+        _ref(c.arr(dX, "dX", True)), _ref(c.arr(dw, "dweight", True)),
+        _ref(c.arr(db, "dbias", True)), ws, size.value, c.index,
         c.handle))
     c.done()
     return dX, dw, db
@@ -774,8 +776,8 @@ def svm_hinge_loss(S, labels, scale: Optional[float] = None,
     import torch
     lib = load()
     c = _Call(S, stream)
-    a = _arr(S, "S", c)
-    if not _is_torch(labels) or not labels.is_cuda or \
+    a = c.arr(S, "S")
+    if not _is_torch(labels) or labels.get_device() != c.index or \
             labels.dtype != torch.int32:
         raise SvmError(SVM_E_UNSUPPORTED, "labels must be an int32 tensor in "
                        "device memory")
@@ -792,7 +794,7 @@ def svm_hinge_loss(S, labels, scale: Optional[float] = None,
     _check(lib.svm_hinge_loss(
         ct.byref(a), labels.data_ptr(),
         1.0 / max(a.rows, 1) if scale is None else scale,
-        _ref(_arr(dS, "dS", c, True)), loss.data_ptr(), _ptr(ws), size.value,
+        _ref(c.arr(dS, "dS", True)), loss.data_ptr(), ws, size.value,
         c.index, c.handle))
     c.done()
     return loss, dS
@@ -870,22 +872,27 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
         c.keep.append(t)
     tab = np.zeros(len(params), dtype=_ADAMW_ROW)
     pd, gd, gp = [], [], []
+    pp, sizes = [], []
     for p, g in zip(params, grads):
-        pd.append(_dtype(p, "a parameter"))
-        gd.append(_dtype(g, "a gradient"))
+        pt, gt = _DTYPES.get(p.dtype), _DTYPES.get(g.dtype)
+        if pt is None or gt is None:
+            raise SvmError(SVM_E_UNSUPPORTED, "parameters and gradients must "
+                           "be float32, bfloat16 or float16")
         if g.shape != p.shape or not p.is_contiguous():
             raise SvmError(SVM_E_INVALID, "parameters must be contiguous, "
                            "gradients of their shapes")
-        if not g.is_contiguous():
-            g = g.contiguous()
-        if p.device != c.device or g.device != c.device:
+        if p.get_device() != c.index or g.get_device() != c.index:
             raise SvmError(SVM_E_INVALID, "the tensors are on several "
                            "devices")
+        if not g.is_contiguous():
+            g = g.contiguous()
         c.keep += (p, g)
+        pd.append(pt)
+        gd.append(gt)
+        pp.append(p.data_ptr())
         gp.append(g.data_ptr())
-    tab["param"] = [p.data_ptr() for p in params]
-    tab["grad"] = gp
-    tab["n"] = [p.numel() for p in params]
+        sizes.append(p.numel())
+    tab["param"], tab["grad"], tab["n"] = pp, gp, sizes
     tab["dtype"], tab["grad_dtype"] = pd, gd
     esize = 1 if bits == 8 else 4
     tab["m"], tab["v"] = m.data_ptr() + at * esize, v.data_ptr() + at * esize
