@@ -89,25 +89,26 @@ __device__ __forceinline__ float sin_of(float z)
     return odd ? -c : c;
 }
 
-// Eight consecutive values of a row: 16 or 32 bytes at once where `wide` says
-// that they are aligned and there, else the first `count` one by one.
+// Eight consecutive values of a row: 16 or 32 bytes at once where all are
+// there, else the first `count` one by one.  Rows may begin at any multiple
+// of their type's size (loads and stores of 16 bytes need no alignment here).
 template <int DT>
 struct Eight {
+    using T = Elem<DT>;
+    typedef T Wide __attribute__((ext_vector_type(DT == SVM_F32 ? 4 : 8)));
+    typedef Wide Loose __attribute__((aligned(sizeof(T))));
     float v[8];
 
-    __device__ __forceinline__ void load(const void* p, int64_t at, bool wide,
-                                         int count)
+    __device__ __forceinline__ void load(const void* p, int64_t at, int count)
     {
-        using T = Elem<DT>;
         const T* q = (const T*)p + at;
-        if (wide) {
+        if (count == 8) {
             if constexpr (DT == SVM_F32) {
-                const float4 a = *(const float4*)q, b = *(const float4*)(q + 4);
-                v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-                v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+                const Wide a = *(const Loose*)q, b = *(const Loose*)(q + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
             } else {
-                typedef T T8 __attribute__((ext_vector_type(8)));
-                const T8 a = *(const T8*)q;
+                const Wide a = *(const Loose*)q;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = (float)a[e];
             }
@@ -118,21 +119,21 @@ struct Eight {
         }
     }
 
-    __device__ __forceinline__ void store(void* p, int64_t at, bool wide,
-                                          int count) const
+    __device__ __forceinline__ void store(void* p, int64_t at, int count) const
     {
-        using T = Elem<DT>;
         T* q = (T*)p + at;
-        if (wide) {
+        if (count == 8) {
             if constexpr (DT == SVM_F32) {
-                *(float4*)q = make_float4(v[0], v[1], v[2], v[3]);
-                *(float4*)(q + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                Wide a, b;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[e] = v[e], b[e] = v[4 + e];
+                *(Loose*)q = a;
+                *(Loose*)(q + 4) = b;
             } else {
-                typedef T T8 __attribute__((ext_vector_type(8)));
-                T8 a;
+                Wide a;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) a[e] = (T)v[e];
-                *(T8*)q = a;
+                *(Loose*)q = a;
             }
         } else {
 #pragma unroll
@@ -141,6 +142,12 @@ struct Eight {
         }
     }
 };
+
+// Of n values, how many of the eight from j on there are.
+__device__ __forceinline__ int eight_of(int64_t n, int64_t j)
+{
+    return n - j >= 8 ? 8 : n - j > 0 ? (int)(n - j) : 0;
+}
 
 // The three bf16 parts of a 32-bit value: x = h + m + l, each part what is
 // left rounded to nearest (to zero where rounding would overflow).
@@ -185,13 +192,6 @@ __device__ __forceinline__ void store_factor(const float (&v)[8], void* dst,
         for (int e = 0; e < 8; ++e) x[e] = (Elem<DT>)v[e];
         *(T8*)((Elem<DT>*)dst + at) = x;
     }
-}
-
-// Whether the rows of an array are aligned to 16 bytes (NULL: yes).
-inline bool wide_rows(const void* p, int64_t ld, int32_t dtype)
-{
-    const int64_t row = ld * (dtype == SVM_F32 ? 4 : 2);
-    return !p || (((uintptr_t)p & 15) == 0 && row % 16 == 0);
 }
 
 // The normal distribution's upper tail at |z| and exp(-z^2 / 2): the rational

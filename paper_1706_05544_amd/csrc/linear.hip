@@ -19,7 +19,6 @@ struct GradArgs {
     int64_t ldd, plane;
     float* part;
     int act;
-    bool wide;
 };
 
 template <int DT>
@@ -30,16 +29,15 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs p)
     const int64_t j = (int64_t)blockIdx.x * kGradCols + tx * 8;
     const int64_t i0 = (int64_t)blockIdx.y * p.rows;
     const int64_t i1 = i0 + p.rows < p.m ? i0 + p.rows : p.m;
-    const int count = p.n - j >= 8 ? 8 : p.n - j > 0 ? (int)(p.n - j) : 0;
-    const bool wide = p.wide && count == 8;
+    const int count = eight_of(p.n, j);
     float sum[8] = {};
     if (count > 0) {
 #pragma unroll 2
         for (int64_t i = i0 + ty; i < i1; i += kGradLanes) {
             Eight<DT> g, z;
-            g.load(p.dY, i * p.ldg + j, wide, count);
+            g.load(p.dY, i * p.ldg + j, count);
             if (p.Z) {
-                z.load(p.Z, i * p.ldz + j, wide, count);
+                z.load(p.Z, i * p.ldz + j, count);
                 act_slopes(p.act, z.v);
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
@@ -195,9 +193,7 @@ void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
                    m,         n,
                    rows,      copy ? const_cast<void*>(dz.data) : nullptr,
                    dz.ld,     dz.plane,
-                   part,      a.act,
-                   wide_rows(a.dY.data, a.dY.ld, t) &&
-                       (!slope || wide_rows(a.Z.data, a.Z.ld, t))};
+                   part,      a.act};
         const dim3 grid((unsigned)((n + kGradCols - 1) / kGradCols),
                         (unsigned)np);
         for_dtype(t, [&]<int DT>() {

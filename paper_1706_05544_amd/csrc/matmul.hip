@@ -74,7 +74,6 @@ struct Args {
     unsigned tm, tn;    // tiles
     float* part;        // splits > 1: sums, splits x m x n
     Epilogue e;
-    int wide;           // outputs and residual in aligned rows of 16 bytes
 };
 
 // 16 bytes for each lane from the buffer `rs` at off + soff into LDS, lane
@@ -244,7 +243,7 @@ template <int OT>
 __device__ __forceinline__ void finish(const Args& p, Eight<OT>& x,
                                        const Eight<OT>& bias,
                                        const Eight<OT>& res, int64_t i,
-                                       int64_t j, bool wide, int count)
+                                       int64_t j, int count)
 {
     const Epilogue& e = p.e;
     if constexpr (OT == SVM_F32) {
@@ -265,13 +264,13 @@ __device__ __forceinline__ void finish(const Args& p, Eight<OT>& x,
     }
 #pragma unroll
     for (int c = 0; c < 8; ++c) x.v[c] += bias.v[c];
-    if (e.Z) x.store(e.Z, i * e.ldz + j, wide, count);
+    if (e.Z) x.store(e.Z, i * e.ldz + j, count);
     act_values(e.act, x.v);
     if (e.residual) {
 #pragma unroll
         for (int c = 0; c < 8; ++c) x.v[c] += res.v[c];
     }
-    x.store(e.Y, i * e.ldy + j, wide, count);
+    x.store(e.Y, i * e.ldy + j, count);
 }
 
 // Tile of block b: each XCD takes a run of consecutive tiles (blocks go to
@@ -450,13 +449,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
     constexpr int kAtOnce = 64 / kLanes;
     const int lr = lane / kLanes, lc = lane % kLanes * 8;
     const int64_t j = j0 + wj + lc;
-    const int64_t left = p.n - j;
-    const int count = left >= 8 ? 8 : left > 0 ? (int)left : 0;
-    const bool wide = p.wide && count == 8;
+    const int count = eight_of(p.n, j);
     Eight<OT> bias;
 #pragma unroll
     for (int c = 0; c < 8; ++c) bias.v[c] = 0.0f;
-    if (p.e.bias && p.splits == 1) bias.load(p.e.bias, j, wide, count);
+    if (p.e.bias && p.splits == 1) bias.load(p.e.bias, j, count);
 #pragma unroll
     for (int s = 0; s < BM / WGM / kRows; ++s) {
 #pragma unroll
@@ -490,11 +487,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
                     for (int c = 0; c < 8; ++c) y.v[c] = x.v[c];
                     const int64_t at =
                         ((int64_t)blockIdx.y * p.m + i) * p.n + j;
-                    y.store(p.part, at, count == 8 && (p.n & 3) == 0, count);
+                    y.store(p.part, at, count);
                 } else {
                     if (p.e.residual)
-                        res.load(p.e.residual, i * p.e.ldr + j, wide, count);
-                    finish<OT>(p, x, bias, res, i, j, wide, count);
+                        res.load(p.e.residual, i * p.e.ldr + j, count);
+                    finish<OT>(p, x, bias, res, i, j, count);
                 }
             }
         }
@@ -510,21 +507,20 @@ __global__ __launch_bounds__(256) void k_join(Args p)
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all;
          t += (int64_t)gridDim.x * 256) {
         const int64_t i = t / groups, j = t % groups * 8;
-        const int count = p.n - j < 8 ? (int)(p.n - j) : 8;
-        const bool wide = p.wide && count == 8;
+        const int count = eight_of(p.n, j);
         Eight<OT> x, bias, res;
 #pragma unroll
         for (int c = 0; c < 8; ++c) x.v[c] = bias.v[c] = 0.0f;
+#pragma unroll 4
         for (int s = 0; s < p.splits; ++s) {
             Eight<SVM_F32> y;
-            y.load(p.part, ((int64_t)s * p.m + i) * p.n + j,
-                   count == 8 && (p.n & 3) == 0, count);
+            y.load(p.part, ((int64_t)s * p.m + i) * p.n + j, count);
 #pragma unroll
             for (int c = 0; c < 8; ++c) x.v[c] += y.v[c];
         }
-        if (p.e.bias) bias.load(p.e.bias, j, wide, count);
-        if (p.e.residual) res.load(p.e.residual, i * p.e.ldr + j, wide, count);
-        finish<OT>(p, x, bias, res, i, j, wide, count);
+        if (p.e.bias) bias.load(p.e.bias, j, count);
+        if (p.e.residual) res.load(p.e.residual, i * p.e.ldr + j, count);
+        finish<OT>(p, x, bias, res, i, j, count);
     }
 }
 
@@ -534,15 +530,14 @@ template <int DT>
 __global__ __launch_bounds__(256) void k_planes(const Elem<DT>* X, int64_t ld,
                                                 int64_t rows, int64_t cols,
                                                 void* dst, int64_t ldp,
-                                                int64_t plane, bool wide)
+                                                int64_t plane)
 {
     const int64_t groups = ldp / 8, all = rows * groups;
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all;
          t += (int64_t)gridDim.x * 256) {
         const int64_t i = t / groups, j = t % groups * 8;
-        const int count = cols - j >= 8 ? 8 : cols - j > 0 ? (int)(cols - j) : 0;
         Eight<DT> x;
-        x.load(X, i * ld + j, wide && count == 8, count);
+        x.load(X, i * ld + j, eight_of(cols, j));
         store_factor<DT>(x.v, dst, i * ldp + j, plane);
     }
 }
@@ -595,8 +590,7 @@ void launch_planes(const svm_array& a, void* dst, int64_t ldp, int64_t plane,
         hipLaunchKernelGGL((k_planes<DT>),
                            dim3((unsigned)(nb < 16384 ? nb : 16384)),
                            dim3(256), 0, s, (const Elem<DT>*)a.data, a.ld,
-                           a.rows, a.cols, dst, ldp, plane,
-                           wide_rows(a.data, a.ld, a.dtype));
+                           a.rows, a.cols, dst, ldp, plane);
     });
 }
 
@@ -629,10 +623,6 @@ void product(const Product& p, Pieces& ws, hipStream_t s)
     a.tn = (unsigned)((p.n + tile - 1) / tile);
     if (a.splits > 1) a.part = ws.take<float>(a.splits * p.m * p.n);
     if (!ws.run) return;
-    a.wide = wide_rows(a.e.Y, a.e.ldy, p.dtype) &&
-             wide_rows(a.e.Z, a.e.ldz, p.dtype) &&
-             wide_rows(a.e.residual, a.e.ldr, p.dtype) &&
-             ((uintptr_t)a.e.bias & 15) == 0;
     if (p.dtype == SVM_F32) launch_any<SVM_BF16, SVM_F32>(a, tile, s);
     else if (p.dtype == SVM_BF16) launch_any<SVM_BF16, SVM_BF16>(a, tile, s);
     else launch_any<SVM_F16, SVM_F16>(a, tile, s);
