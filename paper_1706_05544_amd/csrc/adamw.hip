@@ -8,6 +8,8 @@ namespace msvm {
 
 namespace {
 
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
 // The tensors of one launch travel in its arguments (no table is copied to
 // the device, nothing outlives the call).
 constexpr int kPerLaunch = 48;
@@ -54,7 +56,12 @@ __device__ __forceinline__ void adam_value(const AdamConst& k, float g,
     m = m * k.b1 + g * k.c1;
     v = v * k.b2 + (g * g) * k.c2;
     r = sqrtf(v);
-    p = p * k.keep - k.rate * (m / (r * k.root + k.eps));
+    // (the states above are the definition's bit for bit; the weight's step
+    // is good to a few units of the quotient's last place)
+    const float d = r * k.root + k.eps;
+    float q = m * __builtin_amdgcn_rcpf(d);
+    q = fmaf(fmaf(-d, q, m), __builtin_amdgcn_rcpf(d), q);
+    p = p * k.keep - k.rate * (fabsf(q) <= 3.402823466e38f ? q : m / d);
 }
 
 // The code of x (magnitude a) in a block with `by` = steps^2 / largest.
@@ -71,12 +78,43 @@ __device__ __forceinline__ int encode8(float x, float by, bool live, int steps,
     return x < 0.0f ? -c : c;
 }
 
-// A block of kAdamBlock values to a wave, four of them to a lane.
+// Four consecutive values: 4 times their size at once where all are there.
+template <class T>
+struct Four {
+    typedef T Wide __attribute__((ext_vector_type(4)));
+    typedef Wide Loose __attribute__((aligned(sizeof(T))));
+
+    static __device__ __forceinline__ Wide load(const T* p, int64_t at, int left)
+    {
+        if (left >= 4) return *(const Loose*)(p + at);
+        Wide x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = e < left ? p[at + e] : (T)0;
+        return x;
+    }
+
+    static __device__ __forceinline__ void store(T* p, int64_t at, int left,
+                                                 Wide x)
+    {
+        if (left >= 4) {
+            *(Loose*)(p + at) = x;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (e < left) p[at + e] = x[e];
+    }
+};
+
+// A block of kAdamBlock values to a wave, four of them to a lane.  One read
+// and one write of all that a step touches; bound by memory (and, with
+// states in 8 bits, nearly as much by the square roots).
 template <int PT, int GT, int BITS, bool MASTER>
 __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
 {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int blk = blockIdx.x * 4 + wave;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int blk = (int)blockIdx.x * 4 + wave;
     if (blk >= t.first[t.count]) return;
     int lo = 0, hi = t.count - 1;  // the tensor of this block
     while (lo < hi) {
@@ -88,37 +126,45 @@ __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
     const int64_t b = blk - t.first[lo];
     const int64_t at = b * kAdamBlock + lane * 4;
     const int64_t n = t.n[lo];
+    // past the tensor's end: its states' last block, with gradient 0
+    const int left = n - at >= 4 ? 4 : n - at > 0 ? (int)(n - at) : 0;
     P* param = (P*)t.param[lo];
-    const G* grad = (const G*)t.grad[lo];
-    float* master = t.master[lo];
-    float m[4], v[4], r[4];
-    float ms = 0.0f, vs = 0.0f;
+    float* master = MASTER ? t.master[lo] : nullptr;
+    const auto g = Four<G>::load((const G*)t.grad[lo], at, left);
+    floatx4 p;
+    if (MASTER) {
+        p = *(const floatx4*)(master + at);
+    } else {
+        const auto q = Four<P>::load(param, at, left);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = (float)q[e];
+    }
+    floatx4 m, v, r;
     if (BITS == 8) {
-        ms = t.ms[lo][b];
-        vs = t.vs[lo][b];
+        const auto cm = Four<int8_t>::load((const int8_t*)t.m[lo], at, 4);
+        const auto cv = Four<uint8_t>::load((const uint8_t*)t.v[lo], at, 4);
+        const float ms = t.ms[lo][b], vs = t.vs[lo][b];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            m[e] = decode8(cm[e], ms, 127);
+            r[e] = decode8(cv[e], vs, 254);
+            v[e] = r[e] * r[e];
+        }
+    } else {
+        m = *(const floatx4*)((const float*)t.m[lo] + at);
+        v = *(const floatx4*)((const float*)t.v[lo] + at);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        // past the tensor's end: its states' last block, with gradient 0
-        const int64_t i = at + e;
-        const bool in = i < n;
-        if (BITS == 8) {
-            m[e] = decode8(((const int8_t*)t.m[lo])[i], ms, 127);
-            r[e] = decode8(((const uint8_t*)t.v[lo])[i], vs, 254);
-            v[e] = r[e] * r[e];
-        } else {
-            m[e] = ((const float*)t.m[lo])[i];
-            v[e] = ((const float*)t.v[lo])[i];
-        }
-        float p = MASTER ? master[i] : in ? (float)param[i] : 0.0f;
-        adam_value(k, in ? (float)grad[i] : 0.0f, p, m[e], v[e], r[e]);
-        if (MASTER) master[i] = p;
-        if (in) param[i] = (P)p;
-        if (BITS == 32) {
-            ((float*)t.m[lo])[i] = m[e];
-            ((float*)t.v[lo])[i] = v[e];
-        }
+        float pe = p[e], me = m[e], ve = v[e], re;
+        adam_value(k, (float)g[e], pe, me, ve, re);
+        p[e] = pe, m[e] = me, v[e] = ve, r[e] = re;
     }
+    if (MASTER) *(floatx4*)(master + at) = p;
+    typename Four<P>::Wide out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = (P)p[e];
+    Four<P>::store(param, at, left, out);
     if (BITS == 8) {
         float tm = 0.0f, tr = 0.0f;
 #pragma unroll
@@ -132,31 +178,50 @@ __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
         const bool lm = tm > kTiny, lr = tr > kTiny;
         const float bm = lm ? 16129.0f / tm : 0.0f;
         const float br = lr ? 64516.0f / tr : 0.0f;
+        Four<int8_t>::Wide cm;
+        Four<uint8_t>::Wide cv;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int64_t i = at + e;
-            ((int8_t*)t.m[lo])[i] =
-                (int8_t)encode8(m[e], bm, lm, 127, -128, false);
-            ((uint8_t*)t.v[lo])[i] =
-                (uint8_t)encode8(r[e], br, lr, 254, 255, true);
+            cm[e] = (int8_t)encode8(m[e], bm, lm, 127, -128, false);
+            cv[e] = (uint8_t)encode8(r[e], br, lr, 254, 255, true);
         }
+        *(Four<int8_t>::Wide*)((int8_t*)t.m[lo] + at) = cm;
+        *(Four<uint8_t>::Wide*)((uint8_t*)t.v[lo] + at) = cv;
         if (lane == 0) {
             t.ms[lo][b] = lm ? tm : 0.0f;
             t.vs[lo][b] = lr ? tr : 0.0f;
         }
+    } else {
+        *(floatx4*)((float*)t.m[lo] + at) = m;
+        *(floatx4*)((float*)t.v[lo] + at) = v;
     }
 }
 
+// Four values to a thread.
 __global__ __launch_bounds__(256) void k_adamw_state(
     const int8_t* m, const uint8_t* v, const float* ms, const float* vs,
     int64_t n, float* mo, float* vo)
 {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    if (mo) mo[i] = decode8(m[i], ms[i / kAdamBlock], 127);
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= n) return;
+    const int left = n - at >= 4 ? 4 : (int)(n - at);
+    Four<float>::Wide x;
+    if (mo) {
+        const auto c = Four<int8_t>::load(m, at, left);
+        const float s = ms[at / kAdamBlock];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = decode8(c[e], s, 127);
+        Four<float>::store(mo, at, left, x);
+    }
     if (vo) {
-        const float r = decode8(v[i], vs[i / kAdamBlock], 254);
-        vo[i] = r * r;
+        const auto c = Four<uint8_t>::load(v, at, left);
+        const float s = vs[at / kAdamBlock];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float r = decode8(c[e], s, 254);
+            x[e] = r * r;
+        }
+        Four<float>::store(vo, at, left, x);
     }
 }
 
@@ -273,7 +338,7 @@ void adamw_state(const int8_t* m, const uint8_t* v, const float* ms,
     for (int64_t at = 0; at < n; at += most) {
         const int64_t len = n - at < most ? n - at : most;
         hipLaunchKernelGGL(k_adamw_state,
-                           dim3((unsigned)((len + 255) / 256)), dim3(256), 0,
+                           dim3((unsigned)((len + 1023) / 1024)), dim3(256), 0,
                            s, m ? m + at : nullptr, v ? v + at : nullptr,
                            ms ? ms + at / kAdamBlock : nullptr,
                            vs ? vs + at / kAdamBlock : nullptr, len,

@@ -143,6 +143,43 @@ struct Eight {
     }
 };
 
+// The same as they lie in memory: loaded ahead of their use in a fraction of
+// the registers.
+template <int DT>
+struct RawEight {
+    using T = Elem<DT>;
+    using E = Eight<DT>;
+    static constexpr int kN = DT == SVM_F32 ? 2 : 1;
+    typename E::Wide v[kN];
+
+    __device__ __forceinline__ void load(const void* p, int64_t at, int count)
+    {
+        constexpr int kEach = 8 / kN;
+        const T* q = (const T*)p + at;
+        if (count == 8) {
+#pragma unroll
+            for (int k = 0; k < kN; ++k)
+                v[k] = *(const typename E::Loose*)(q + k * kEach);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[e / kEach][e % kEach] = e < count ? q[e] : (T)0.0f;
+        }
+    }
+
+    __device__ __forceinline__ void ones()
+    {
+#pragma unroll
+        for (int k = 0; k < kN; ++k) v[k] = (T)1.0f;
+    }
+
+    __device__ __forceinline__ float at(int e) const
+    {
+        constexpr int kEach = 8 / kN;
+        return (float)v[e / kEach][e % kEach];
+    }
+};
+
 // Of n values, how many of the eight from j on there are.
 __device__ __forceinline__ int eight_of(int64_t n, int64_t j)
 {

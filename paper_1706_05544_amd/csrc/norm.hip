@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kThreads<G>) void k_norm_grad(NormGradView p)
     __shared__ float red[G > 64 ? 2 * (G / 64) : 1];
     __shared__ float join[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kCols : 1];
     const int lane = threadIdx.x % G, group = threadIdx.x / G;
-    Eight<DT> w[IT];
+    RawEight<DT> w[IT];
     float sw[IT][8], sb[IT][8];
     int count[IT];
 #pragma unroll
@@ -189,39 +189,55 @@ __global__ __launch_bounds__(kThreads<G>) void k_norm_grad(NormGradView p)
         const int64_t j = ((int64_t)t * G + lane) * 8;
         count[t] = eight_of(p.n, j);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            w[t].v[e] = 1.0f;
-            sw[t][e] = sb[t][e] = 0.0f;
-        }
+        for (int e = 0; e < 8; ++e) sw[t][e] = sb[t][e] = 0.0f;
+        w[t].ones();
         if (p.w) w[t].load(p.w, j, count[t]);
     }
     const float over = 1.0f / (float)p.n;
-    for (int64_t i = (int64_t)blockIdx.x * kGroups + group; i < p.m;
-         i += (int64_t)gridDim.x * kGroups) {
-        Eight<DT> x[IT], g[IT], r[IT];
+    const int64_t turn = (int64_t)gridDim.x * kGroups;
+    // The next row is under way while this one is summed (16 bits, where a
+    // row takes few registers; 32-bit rows reach the memory's rate without,
+    // and 1024 threads with two pieces each have no registers for it).
+    constexpr bool kAhead = DT != SVM_F32 && !(G > 256 && IT > 1);
+    RawEight<DT> nx[IT], ng[IT], nr[IT];
+    auto fetch = [&](int64_t i) {
 #pragma unroll
         for (int t = 0; t < IT; ++t) {
             const int64_t j = ((int64_t)t * G + lane) * 8;
-            x[t].load(p.X, i * p.ldx + j, count[t]);
-            g[t].load(p.dY, i * p.ldg + j, count[t]);
-            if (p.res) r[t].load(p.res, i * p.ldr + j, count[t]);
+            nx[t].load(p.X, i * p.ldx + j, count[t]);
+            ng[t].load(p.dY, i * p.ldg + j, count[t]);
+            if (p.res) nr[t].load(p.res, i * p.ldr + j, count[t]);
         }
+    };
+    int64_t i = (int64_t)blockIdx.x * kGroups + group;
+    if (kAhead && i < p.m) fetch(i);
+    for (; i < p.m; i += turn) {
+        if (!kAhead) fetch(i);
+        RawEight<DT> r[IT];
+        float xh[IT][8], g[IT][8];
         const float mu = p.mean[i], rs = p.rstd[i];
         float s1 = 0.0f, s2 = 0.0f;
+        // Past the row's end X and dY are 0: what is added is 0, or NaN in a
+        // row whose mean or rstd is not finite, and such rows are NaN anyway.
+#pragma unroll
+        for (int t = 0; t < IT; ++t) {
+            r[t] = nr[t];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                xh[t][e] = (nx[t].at(e) - mu) * rs;
+                g[t][e] = ng[t].at(e);
+            }
+        }
+        if (kAhead && i + turn < p.m) fetch(i + turn);
 #pragma unroll
         for (int t = 0; t < IT; ++t)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                // (past the row's end dY is 0, and x is left out of sums)
-                const float xh = (x[t].v[e] - mu) * rs;
-                const float gv = g[t].v[e];
-                if (e < count[t]) sw[t][e] = fmaf(gv, xh, sw[t][e]);
-                sb[t][e] += gv;
-                const float a = e < count[t] ? gv * w[t].v[e] : 0.0f;
-                x[t].v[e] = xh;
-                g[t].v[e] = a;
-                s1 += a;
-                if (e < count[t]) s2 = fmaf(a, xh, s2);
+                sw[t][e] = fmaf(g[t][e], xh[t][e], sw[t][e]);
+                sb[t][e] += g[t][e];
+                g[t][e] *= w[t].at(e);
+                s1 += g[t][e];
+                s2 = fmaf(g[t][e], xh[t][e], s2);
             }
         if (!p.dX) continue;
         group_sums<G>(s1, s2, red);
@@ -229,14 +245,13 @@ __global__ __launch_bounds__(kThreads<G>) void k_norm_grad(NormGradView p)
         s2 *= over;
 #pragma unroll
         for (int t = 0; t < IT; ++t) {
+            Eight<DT> d;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float d = rs * (g[t].v[e] - fmaf(x[t].v[e], s2, s1));
-                if (p.res) d += r[t].v[e];
-                x[t].v[e] = d;
+                d.v[e] = rs * (g[t][e] - fmaf(xh[t][e], s2, s1));
+                if (p.res) d.v[e] += r[t].at(e);
             }
-            x[t].store(p.dX, i * p.ldd + ((int64_t)t * G + lane) * 8,
-                       count[t]);
+            d.store(p.dX, i * p.ldd + ((int64_t)t * G + lane) * 8, count[t]);
         }
     }
     if (!p.pw) return;
@@ -353,13 +368,15 @@ void for_width(int64_t n, F&& f)
     else f.template operator()<1024, 2>();
 }
 
-// Blocks of the gradient: enough rows under way to keep the memory busy, few
-// enough that their partial sums are small beside the rows (n columns, m
-// rows, `groups` rows at a time to a block).
-int64_t grad_blocks(int64_t m, int64_t groups, int threads)
+// Blocks of the gradient: those that the registers of the kernel let run at
+// once (a block more would run alone at the end), but no more than there are
+// turns of `groups` rows.
+template <int G, int IT>
+int64_t grad_blocks(int64_t m)
 {
+    const int64_t groups = kThreads<G> / G;
     const int64_t turns = (m + groups - 1) / groups;
-    const int64_t most = 256 * (1024 / threads);
+    const int64_t most = 256 * (G > 256 ? 1 : IT > 1 ? 3 : 4);
     return turns < most ? turns : most;
 }
 
@@ -369,7 +386,7 @@ int64_t norm_partials(int64_t m, int64_t n)
     if (n > kMostCols) return (m + 255) / 256 < 1024 ? (m + 255) / 256 : 1024;
     int64_t np = 0;
     for_width(n, [&]<int G, int IT>() {
-        np = grad_blocks(m, kThreads<G> / G, kThreads<G>);
+        np = grad_blocks<G, IT>(m);
     });
     return np;
 }
