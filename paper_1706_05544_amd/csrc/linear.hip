@@ -162,10 +162,14 @@ void linear_forward(const LinearArgs& a, Pieces& ws, hipStream_t s)
     p.k = a.X.cols;
     p.dtype = a.X.dtype;
     if (p.m == 0) return;
-    p.A = factor_of(a.X, true, ws, s);
-    p.B = factor_of(a.W, true, ws, s);
     p.e = {a.bias.data, a.residual.data, a.Y.data, a.Z.data,
            a.residual.ld, a.Y.ld, a.Z.ld, a.act};
+    if (few_rows(p.m, p.n, p.k)) {
+        if (ws.run) few_rows_product(a.X, a.W, p.e, s);
+        return;
+    }
+    p.A = factor_of(a.X, true, ws, s);
+    p.B = factor_of(a.W, true, ws, s);
     product(p, ws, s);
 }
 

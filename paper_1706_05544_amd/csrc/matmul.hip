@@ -238,30 +238,30 @@ __device__ __forceinline__ float exact_sum(const Factor& A, const Factor& B,
     return sum;
 }
 
+// Replaces those of eight sums that are not finite by exact(c).
+template <class F>
+__device__ __forceinline__ void mend(float (&v)[8], int count, F&& exact)
+{
+    bool fine = true;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) fine &= fabsf(v[c]) <= 3.402823466e38f;
+    if (fine) return;
+#pragma unroll 1
+    for (int c = 0; c < count; ++c) {
+        const float s = exact(c);
+#pragma unroll
+        for (int d = 0; d < 8; ++d)
+            if (d == c && !(fabsf(v[d]) <= 3.402823466e38f)) v[d] = s;
+    }
+}
+
 // Finishes eight sums of row i from column j on and writes them.
 template <int OT>
-__device__ __forceinline__ void finish(const Args& p, Eight<OT>& x,
+__device__ __forceinline__ void finish(const Epilogue& e, Eight<OT>& x,
                                        const Eight<OT>& bias,
                                        const Eight<OT>& res, int64_t i,
                                        int64_t j, int count)
 {
-    const Epilogue& e = p.e;
-    if constexpr (OT == SVM_F32) {
-        bool fine = true;
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-            fine &= fabsf(x.v[c]) <= 3.402823466e38f;
-        if (!fine) {
-#pragma unroll 1
-            for (int c = 0; c < count; ++c) {
-                const float s = exact_sum(p.A, p.B, i, j + c, p.k);
-#pragma unroll
-                for (int d = 0; d < 8; ++d)
-                    if (d == c && !(fabsf(x.v[d]) <= 3.402823466e38f))
-                        x.v[d] = s;
-            }
-        }
-    }
 #pragma unroll
     for (int c = 0; c < 8; ++c) x.v[c] += bias.v[c];
     if (e.Z) x.store(e.Z, i * e.ldz + j, count);
@@ -491,7 +491,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
                 } else {
                     if (p.e.residual)
                         res.load(p.e.residual, i * p.e.ldr + j, count);
-                    finish<OT>(p, x, bias, res, i, j, count);
+                    if constexpr (OT == SVM_F32)
+                        mend(x.v, count, [&](int c) {
+                            return exact_sum(p.A, p.B, i, j + c, p.k);
+                        });
+                    finish<OT>(p.e, x, bias, res, i, j, count);
                 }
             }
         }
@@ -520,8 +524,136 @@ __global__ __launch_bounds__(256) void k_join(Args p)
         }
         if (p.e.bias) bias.load(p.e.bias, j, count);
         if (p.e.residual) res.load(p.e.residual, i * p.e.ldr + j, count);
-        finish<OT>(p, x, bias, res, i, j, count);
+        if constexpr (OT == SVM_F32)
+            mend(x.v, count, [&](int c) {
+                return exact_sum(p.A, p.B, i, j + c, p.k);
+            });
+        finish<OT>(p.e, x, bias, res, i, j, count);
     }
+}
+
+// ---- few rows
+
+// Y for at most 16 MT rows of X: 16 columns (rows of W) to a block, the
+// summed index split over its waves and the waves' sums joined in LDS.  Rows
+// of W go from memory to registers, in 32 bytes a lane (128 of a row at
+// once), with no LDS between: each is used once, and W is all that counts.
+// Rows may begin anywhere, and 32-bit values are split in registers.
+constexpr int kFewWaves = 8;
+
+struct FewArgs {
+    const void *X, *W;
+    int64_t ldx, ldw, m, n, k;
+    Epilogue e;
+};
+
+// 16 values of a row as they lie in memory, and as two fragments (for 32 bits
+// two of each part).
+template <int DT>
+struct Sixteen {
+    RawEight<DT> raw[2];
+    short8v h[2], m[2], l[2];
+
+    __device__ __forceinline__ void load(const void* p, int64_t at, int64_t left)
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            raw[u].load(p, at + u * 8, eight_of(left, u * 8));
+    }
+
+    __device__ __forceinline__ void split()
+    {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if constexpr (DT == SVM_F32) {
+                bf16x8 a, b, c;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    __bf16 ph, pm, pl;
+                    three_parts(raw[u].at(e), ph, pm, pl);
+                    a[e] = ph, b[e] = pm, c[e] = pl;
+                }
+                h[u] = __builtin_bit_cast(short8v, a);
+                m[u] = __builtin_bit_cast(short8v, b);
+                l[u] = __builtin_bit_cast(short8v, c);
+            } else {
+                h[u] = __builtin_bit_cast(short8v, raw[u].v[0]);
+            }
+        }
+    }
+};
+
+template <int DT, int MT>
+__global__ __launch_bounds__(64 * kFewWaves) void k_few(FewArgs p)
+{
+    __shared__ float red[kFewWaves][MT * 16][20];  // (rows 16 apart in banks)
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int i = lane & 15, g = lane >> 4;
+    const int64_t j0 = (int64_t)blockIdx.x * 16;
+    constexpr int IT = DT == SVM_F32 ? SVM_BF16 : DT;
+    floatx4 acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) acc[t] = floatx4{0, 0, 0, 0};
+    // past W's or X's rows, and past the summed index, nothing is loaded
+    const int64_t wrow = j0 + i < p.n ? (j0 + i) * p.ldw : -1;
+    Sixteen<DT> w, x[MT];
+    auto fetch = [&](int64_t k0) {
+        const int64_t at = k0 + g * 16;
+        w.load(p.W, wrow + at, wrow < 0 ? 0 : p.k - at);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const int64_t r = t * 16 + i;
+            x[t].load(p.X, r * p.ldx + at, r < p.m ? p.k - at : 0);
+        }
+    };
+    fetch(wave * 64);
+    for (int64_t k0 = wave * 64; k0 < p.k; k0 += 64 * kFewWaves) {
+        w.split();
+#pragma unroll
+        for (int t = 0; t < MT; ++t) x[t].split();
+        fetch(k0 + 64 * kFewWaves);
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                if constexpr (DT == SVM_F32) {  // the smallest first
+                    acc[t] = mfma<IT>(w.h[u], x[t].l[u], acc[t]);
+                    acc[t] = mfma<IT>(w.l[u], x[t].h[u], acc[t]);
+                    acc[t] = mfma<IT>(w.m[u], x[t].m[u], acc[t]);
+                    acc[t] = mfma<IT>(w.h[u], x[t].m[u], acc[t]);
+                    acc[t] = mfma<IT>(w.m[u], x[t].h[u], acc[t]);
+                }
+                acc[t] = mfma<IT>(w.h[u], x[t].h[u], acc[t]);
+            }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+        *(floatx4*)&red[wave][t * 16 + i][g * 4] = acc[t];
+    __syncthreads();
+    if (threadIdx.x >= MT * 32) return;
+    const int row = threadIdx.x >> 1, c0 = (threadIdx.x & 1) * 8;
+    const int64_t j = j0 + c0;
+    const int count = eight_of(p.n, j);
+    if (row >= p.m || count == 0) return;
+    Eight<DT> v, bias, res;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v.v[c] = bias.v[c] = res.v[c] = 0.0f;
+    if (p.e.bias) bias.load(p.e.bias, j, count);
+    if (p.e.residual) res.load(p.e.residual, row * p.e.ldr + j, count);
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w)
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v.v[c] += red[w][row][c0 + c];
+    if constexpr (DT == SVM_F32)
+        mend(v.v, count, [&](int c) {
+            const float* x = (const float*)p.X + row * p.ldx;
+            const float* w = (const float*)p.W + (j + c) * p.ldw;
+            float s = 0.0f;
+#pragma unroll 1
+            for (int64_t r = 0; r < p.k; ++r) s = fmaf(x[r], w[r], s);
+            return s;
+        });
+    finish<DT>(p.e, v, bias, res, row, j, count);
 }
 
 // ---- factors that cannot be read as they are
@@ -591,6 +723,24 @@ void launch_planes(const svm_array& a, void* dst, int64_t ldp, int64_t plane,
                            dim3((unsigned)(nb < 16384 ? nb : 16384)),
                            dim3(256), 0, s, (const Elem<DT>*)a.data, a.ld,
                            a.rows, a.cols, dst, ldp, plane);
+    });
+}
+
+bool few_rows(int64_t m, int64_t n, int64_t k)
+{
+    return m <= 32 && (k <= 32768 || n >= 4096);
+}
+
+void few_rows_product(const svm_array& X, const svm_array& W,
+                      const Epilogue& e, hipStream_t s)
+{
+    const FewArgs a{X.data, W.data, X.ld, W.ld, X.rows, W.rows, X.cols, e};
+    const dim3 grid((unsigned)((a.n + 15) / 16)), block(64 * kFewWaves);
+    for_dtype(X.dtype, [&]<int DT>() {
+        if (a.m <= 16)
+            hipLaunchKernelGGL((k_few<DT, 1>), grid, block, 0, s, a);
+        else
+            hipLaunchKernelGGL((k_few<DT, 2>), grid, block, 0, s, a);
     });
 }
 

@@ -39,6 +39,12 @@ bool factor_fits(const svm_array& a, bool along);
 // Queues the product; with ws.run false only counts its workspace.
 void product(const Product& p, Pieces& ws, hipStream_t s);
 
+// The product of few rows X with W (both along), in one launch and without a
+// workspace; and whether a product is one of these.
+bool few_rows(int64_t m, int64_t n, int64_t k);
+void few_rows_product(const svm_array& X, const svm_array& W,
+                      const Epilogue& e, hipStream_t s);
+
 // Copies rows of a into dst (ldp values to a row, a multiple of 8, zeros
 // past the columns); float32 rows into three bf16 planes, `plane` apart.
 void launch_planes(const svm_array& a, void* dst, int64_t ldp, int64_t plane,

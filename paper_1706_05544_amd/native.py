@@ -804,10 +804,11 @@ def svm_adamw_parts(params):
     """Where each tensor's states begin in the flat states of
     svm_adamw_step, and their total length: the tensors follow one another,
     each from a multiple of SVM_ADAMW_BLOCK."""
-    sizes = np.array([p.numel() for p in params], dtype=np.int64)
-    room = -(-sizes // SVM_ADAMW_BLOCK) * SVM_ADAMW_BLOCK
-    ends = np.cumsum(room)
-    return ends - room, int(ends[-1]) if len(ends) else 0
+    at, total = [], 0
+    for p in params:
+        at.append(total)
+        total += -(-p.numel() // SVM_ADAMW_BLOCK) * SVM_ADAMW_BLOCK
+    return np.array(at, dtype=np.int64), total
 
 
 def svm_adamw_states(params, bits: int = 32, master: bool = False):
@@ -870,29 +871,25 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
                            "of %d values on the parameters' device"
                            % (what, dtype, n))
         c.keep.append(t)
+    if not all(p.is_contiguous() for p in params) or \
+            [p.shape for p in params] != [g.shape for g in grads]:
+        raise SvmError(SVM_E_INVALID, "parameters must be contiguous, "
+                       "gradients of their shapes")
+    grads = [g if g.is_contiguous() else g.contiguous() for g in grads]
+    if {t.get_device() for t in params} | {t.get_device() for t in grads} \
+            != {c.index}:
+        raise SvmError(SVM_E_INVALID, "the tensors are on several devices")
+    pd = [_DTYPES.get(p.dtype) for p in params]
+    gd = [_DTYPES.get(g.dtype) for g in grads]
+    if None in pd or None in gd:
+        raise SvmError(SVM_E_UNSUPPORTED, "parameters and gradients must be "
+                       "float32, bfloat16 or float16")
+    c.keep += params
+    c.keep += grads
     tab = np.zeros(len(params), dtype=_ADAMW_ROW)
-    pd, gd, gp = [], [], []
-    pp, sizes = [], []
-    for p, g in zip(params, grads):
-        pt, gt = _DTYPES.get(p.dtype), _DTYPES.get(g.dtype)
-        if pt is None or gt is None:
-            raise SvmError(SVM_E_UNSUPPORTED, "parameters and gradients must "
-                           "be float32, bfloat16 or float16")
-        if g.shape != p.shape or not p.is_contiguous():
-            raise SvmError(SVM_E_INVALID, "parameters must be contiguous, "
-                           "gradients of their shapes")
-        if p.get_device() != c.index or g.get_device() != c.index:
-            raise SvmError(SVM_E_INVALID, "the tensors are on several "
-                           "devices")
-        if not g.is_contiguous():
-            g = g.contiguous()
-        c.keep += (p, g)
-        pd.append(pt)
-        gd.append(gt)
-        pp.append(p.data_ptr())
-        gp.append(g.data_ptr())
-        sizes.append(p.numel())
-    tab["param"], tab["grad"], tab["n"] = pp, gp, sizes
+    tab["param"] = [p.data_ptr() for p in params]
+    tab["grad"] = [g.data_ptr() for g in grads]
+    tab["n"] = [p.numel() for p in params]
     tab["dtype"], tab["grad_dtype"] = pd, gd
     esize = 1 if bits == 8 else 4
     tab["m"], tab["v"] = m.data_ptr() + at * esize, v.data_ptr() + at * esize

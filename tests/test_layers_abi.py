@@ -168,8 +168,9 @@ def hinge(S=None, labels=16, scale=1.0, dS=None, loss=16, work=16,
 @pytest.mark.parametrize("kw", [
     dict(S=arr(6, 0)), dict(labels=None), dict(loss=None),
     dict(scale=float("inf")), dict(dS=arr(6, 3, at=2 << 20)),
-    dict(dS=arr(6, 4, at=(1 << 20) + 4)), dict(work=None),
-    dict(nbytes=4)])
+    dict(dS=arr(6, 4, at=(1 << 20) + 4)),
+    # (losses of few scores need no workspace)
+    dict(S=arr(60000, 4), work=None), dict(S=arr(60000, 4), nbytes=4)])
 def test_hinge_refusals(kw):
     assert hinge(**kw) == INV
 
