@@ -31,7 +31,8 @@ namespace msvm {
 
 namespace {
 
-constexpr int kBK = 64;         // summed values of a step
+constexpr int kStep16 = 64;  // summed values of a step: 16-bit factors,
+constexpr int kStep32 = 32;  // 32-bit ones (three planes)
 // An address past every descriptor: the rows of a tile end below it, and
 // added to a tile's own offsets it does not wrap.
 constexpr uint32_t kPast = 0x80000000u;
@@ -56,20 +57,10 @@ __device__ __forceinline__ floatx4 mfma(short8v a, short8v b, floatx4 c)
             0, 0);
 }
 
-// Products of the planes of 32-bit factors (0: leading 8 bits), the smallest
-// first.  The three that are left out (1 2, 2 1, 2 2) are below 2^-24 of the
-// whole.
-constexpr uint32_t kSegA = 0x010120;  // plane of product s at 4 s bits
-constexpr uint32_t kSegB = 0x001102;
-__device__ __forceinline__ int64_t plane_of(uint32_t planes, int seg)
-{
-    return (planes >> (4 * seg)) & 15;
-}
-
 struct Args {
     Factor A, B;
     int64_t m, n, k;
-    int nk;             // steps of a product (32 bits: of one of planes)
+    int nk;             // steps
     int splits, per;    // parts of all steps, steps of a part
     unsigned tm, tn;    // tiles
     float* part;        // splits > 1: sums, splits x m x n
@@ -94,11 +85,12 @@ __device__ __forceinline__ void lds_load(intx4 rs, short* lds, uint32_t off,
         : "memory");
 }
 
-// The lane's share of a factor's tile loads: R rows (ALONG) or columns.
-template <int R, int NW, bool ALONG>
+// The lane's share of a factor's tile loads: R rows (ALONG) or columns, BK
+// summed values.
+template <int R, int BK, int NW, bool ALONG>
 struct Stage {
-    static constexpr int kInstr = R / 8 / NW;  // loads of a wave, 1 KiB each
-    static constexpr int kRowLanes = ALONG ? 8 : R / 8;  // 16-byte pieces
+    static constexpr int kInstr = R * BK / 512 / NW;  // of a wave, 1 KiB each
+    static constexpr int kRowLanes = (ALONG ? BK : R) / 8;  // 16-byte pieces
     static constexpr int kRows = 64 / kRowLanes;         // rows of a load
     uint32_t off[2];  // byte offset in the tile, for each kind of load
     int piece;        // first summed value of the piece (ALONG, kind 0)
@@ -109,9 +101,11 @@ struct Stage {
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
             int c;
-            if (ALONG) {
+            if (ALONG && BK == 64) {
                 // rows 8 q + row: key = (r & 3) | ((r >> 2 ^ r >> 4) & 1) << 2
                 c = pos ^ ((row & 3) | (((row >> 2) ^ v) & 1) << 2);
+            } else if (ALONG) {
+                c = pos ^ ((row >> 1) & 3);  // two rows to 128 bytes
             } else {
                 const int r = kRows == 2 ? v * 2 + row : row;
                 c = pos ^ (2 * (r & 3));
@@ -138,13 +132,15 @@ struct Stage {
         uint32_t o[2] = {off[0], off[1]};
         if (ALONG) {
             if (piece >= summed) o[0] = kPast;
-            if ((piece ^ 32) >= summed) o[1] = kPast;
+            if (BK == 64 && (piece ^ 32) >= summed) o[1] = kPast;
         }
 #pragma unroll
         for (int it = 0; it < kInstr; ++it) {
             const int q = wave * kInstr + it;
             // which kind load q is
-            const int v = ALONG ? (q >> 1) & 1 : kRows == 2 ? q & 1 : 0;
+            const int v = ALONG ? (BK == 64 ? (q >> 1) & 1 : 0)
+                          : kRows == 2 ? q & 1
+                                       : 0;
             lds_load(rs, lds + q * 512, v ? o[1] : o[0],
                      (uint32_t)(q * kRows) * (uint32_t)ld2);
         }
@@ -166,14 +162,45 @@ __device__ __forceinline__ void meet()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// Where the loads of a factor are: the tile of the next step.
-struct Cursor {
-    const char* at;
-    int64_t left;  // bytes from there to the factor's end
+// A factor's tile loads step by step: P planes, R rows or columns.
+template <int R, int BK, int NW, bool ALONG, int P>
+struct Walk {
+    Stage<R, BK, NW, ALONG> stage;
+    const char* at;  // the tile of the next step (first plane)
+    int64_t left;    // bytes from there to the plane's end
+    int64_t step, plane;
+    int ld2;
+
+    // x0: first row or column of the tile, of n; t0: first step, of k values
+    __device__ __forceinline__ void init(const Factor& f, int64_t x0, int64_t n,
+                                         int64_t t0, int64_t k, int lane)
+    {
+        stage.init(f.ld, lane);
+        ld2 = (int)f.ld * 2;
+        step = ALONG ? 2 * BK : (int64_t)BK * ld2;
+        plane = 2 * f.plane;
+        const int64_t k0 = t0 * BK;
+        at = (const char*)f.data + (ALONG ? x0 * ld2 + k0 * 2
+                                          : k0 * ld2 + x0 * 2);
+        left = ALONG ? (n - 1 - x0) * ld2 + (k - k0) * 2
+                     : (k - 1 - k0) * ld2 + (n - x0) * 2;
+    }
+
+    // Loads the next step (`summed` values of it there; none: zeros).
+    __device__ __forceinline__ void load(int summed, bool there, short* lds,
+                                         int wave)
+    {
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+            stage.load(at + q * plane, there ? left : 0, ld2, summed,
+                       lds + q * R * BK, wave);
+        at += step;
+        left -= step;
+    }
 };
 
 // Reads a fragment: 16 rows (of the factor's other index) x 32 summed values.
-template <int R, bool ALONG>
+template <int R, int BK, bool ALONG>
 struct Frag {
     int base[2];
 
@@ -184,8 +211,10 @@ struct Frag {
         if (ALONG) {
 #pragma unroll
             for (int v = 0; v < 2; ++v) {
-                const int key = (i & 3) | (((i >> 2) ^ v) & 1) << 2;
-                base[v] = (first + i) * 64 + (g ^ key) * 8;
+                const int key = BK == 64
+                                    ? (i & 3) | (((i >> 2) ^ v) & 1) << 2
+                                    : (i >> 1) & 3;
+                base[v] = (first + i) * BK + (g ^ key) * 8;
             }
         } else {
             const int r = 8 * g + (i >> 2);  // summed value; + 4: same key
@@ -195,13 +224,14 @@ struct Frag {
     }
 
     // fragment f (rows first + 16 f ..), summed values 32 h .. of the step
+    // (h = 1 only where BK is 64)
     __device__ __forceinline__ short8v read(const short* lds, int first, int f,
                                             int h, int lane) const
     {
         if (ALONG) {
             // bit 4 of the row (the wave's first is a multiple of 32)
             const int b = f & 1 ? base[1] : base[0];
-            return *(const short8v*)(lds + (b ^ (h * 32)) + f * 16 * 64);
+            return *(const short8v*)(lds + (b ^ (h * 32)) + f * 16 * BK);
         } else {
             const int key = 2 * ((lane >> 2) & 3);
             const int col = first + f * 16 + base[1];
@@ -289,15 +319,91 @@ __device__ __forceinline__ void tile_of(unsigned b, unsigned tm, unsigned tn,
     tj = in / rows;
 }
 
-// IT: type of the 16-bit factors; OT: type of the outputs.
-// ST: buffers, and so steps whose loads are under way.
-template <int IT, int OT, int BM, int BN, int WGM, int WGN, int ST,
-          bool AALONG, bool BALONG>
+// The rows of a wave's tile that go through LDS at a time.
+constexpr int slab_rows(int fm) { return fm * 16 < 64 ? fm * 16 : 64; }
+
+// The wave's own part of the first two buffers: SLAB floats.
+template <int SLAB, int NW, int LDS>
+__device__ __forceinline__ float* wave_slab(short* lds0, short* lds1, int wave)
+{
+    static_assert(NW / 2 * SLAB * 4 <= LDS * 2, "slab");
+    return (float*)(wave < NW / 2 ? lds0 : lds1) + (wave % (NW / 2)) * SLAB;
+}
+
+// Finishes and writes the sums of a wave's tile (FM x FN fragments, from row
+// iw and column jw on); `slab` is LDS of its own.
+template <int OT, int FM, int FN>
+__device__ __forceinline__ void write_tile(const Args& p,
+                                           const floatx4 (&acc)[FM][FN],
+                                           float* slab, int64_t iw, int64_t jw,
+                                           int lane)
+{
+    constexpr int kCols = FN * 16, kRows = slab_rows(FM);
+    constexpr int kLanes = kCols / 8;   // lanes of a row
+    constexpr int kAtOnce = 64 / kLanes;
+    const int lr = lane / kLanes, lc = lane % kLanes * 8;
+    const int64_t j = jw + lc;
+    const int count = eight_of(p.n, j);
+    Eight<OT> bias;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) bias.v[c] = 0.0f;
+    if (p.e.bias && p.splits == 1) bias.load(p.e.bias, j, count);
+#pragma unroll
+    for (int s = 0; s < FM * 16 / kRows; ++s) {
+#pragma unroll
+        for (int f = 0; f < kRows / 16; ++f)
+#pragma unroll
+            for (int g = 0; g < FN; ++g) {
+                const int r = f * 16 + (lane & 15);
+                const int c = g * 4 + (lane >> 4);  // 4 columns each
+                *(floatx4*)(slab + r * kCols + ((c ^ (r & 7)) * 4)) =
+                    acc[s * (kRows / 16) + f][g];
+            }
+#pragma unroll 2
+        for (int r0 = 0; r0 < kRows; r0 += kAtOnce) {
+            const int r = r0 + lr;
+            const int64_t i = iw + s * kRows + r;
+            if (i < p.m && count > 0) {
+                Eight<OT> x, res;
+                const float* q = slab + r * kCols;
+                const floatx4 u =
+                    *(const floatx4*)(q + (((lc / 4) ^ (r & 7)) * 4));
+                const floatx4 v =
+                    *(const floatx4*)(q + (((lc / 4 + 1) ^ (r & 7)) * 4));
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    x.v[c] = u[c];
+                    x.v[4 + c] = v[c];
+                }
+                if (p.splits > 1) {
+                    Eight<SVM_F32> y;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) y.v[c] = x.v[c];
+                    const int64_t at =
+                        ((int64_t)blockIdx.y * p.m + i) * p.n + j;
+                    y.store(p.part, at, count);
+                } else {
+                    if (p.e.residual)
+                        res.load(p.e.residual, i * p.e.ldr + j, count);
+                    if constexpr (OT == SVM_F32)
+                        mend(x.v, count, [&](int c) {
+                            return exact_sum(p.A, p.B, i, j + c, p.k);
+                        });
+                    finish<OT>(p.e, x, bias, res, i, j, count);
+                }
+            }
+        }
+    }
+}
+
+// 16-bit factors.  ST: buffers, and so steps whose loads are under way.
+template <int OT, int BM, int BN, int WGM, int WGN, int ST, bool AALONG,
+          bool BALONG>
 __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
 {
     constexpr int NW = WGM * WGN;
     constexpr int FM = BM / WGM / 16, FN = BN / WGN / 16;
-    constexpr int kSegs = OT == SVM_F32 ? 6 : 1;
+    constexpr int kBK = kStep16, kSlab = slab_rows(FM) * FN * 16;
     constexpr int kLds = (BM + BN) * kBK;  // values of a buffer
     // (arrays of their own, so that the compiler knows a buffer that is being
     // loaded from one that is being read)
@@ -315,61 +421,23 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
     const int64_t i0 = (int64_t)ti * BM, j0 = (int64_t)tj * BN;
     const int wi = wave / WGN * (BM / WGM), wj = wave % WGN * (BN / WGN);
 
-    Stage<BM, NW, AALONG> sa;
-    Stage<BN, NW, BALONG> sb;
-    Frag<BM, AALONG> fa;
-    Frag<BN, BALONG> fb;
-    sa.init(p.A.ld, lane);
-    sb.init(p.B.ld, lane);
+    Frag<BM, kBK, AALONG> fa;
+    Frag<BN, kBK, BALONG> fb;
     fa.init(wi, lane);
     fb.init(wj, lane);
-
-    // Steps t0 .. t1 - 1 of the products of planes one after another.
     const int t0 = blockIdx.y * p.per;
-    const int all = kSegs * p.nk;
-    const int t1 = t0 + p.per < all ? t0 + p.per : all;
-    const int lda2 = (int)p.A.ld * 2, ldb2 = (int)p.B.ld * 2;
-    const int64_t stepa = AALONG ? 2 * kBK : (int64_t)kBK * lda2;
-    const int64_t stepb = BALONG ? 2 * kBK : (int64_t)kBK * ldb2;
-    int seg = kSegs > 1 ? t0 / p.nk : 0;
-    int tl = t0 - seg * p.nk;  // step of the next loads in its product
-    int todo = t1 - t0;        // steps not loaded yet
-    Cursor ca, cb;
-    auto seek = [&]() {
-        const int64_t k0 = (int64_t)tl * kBK;
-        ca.at = (const char*)p.A.data +
-                (AALONG ? i0 * lda2 + k0 * 2 : k0 * lda2 + i0 * 2);
-        ca.left = (AALONG ? (p.m - 1 - i0) * lda2 + (p.k - k0) * 2
-                          : (p.k - 1 - k0) * lda2 + (p.m - i0) * 2);
-        cb.at = (const char*)p.B.data +
-                (BALONG ? j0 * ldb2 + k0 * 2 : k0 * ldb2 + j0 * 2);
-        cb.left = (BALONG ? (p.n - 1 - j0) * ldb2 + (p.k - k0) * 2
-                          : (p.k - 1 - k0) * ldb2 + (p.n - j0) * 2);
-        if (kSegs > 1) {
-            ca.at += 2 * plane_of(kSegA, seg) * p.A.plane;
-            cb.at += 2 * plane_of(kSegB, seg) * p.B.plane;
-        }
-    };
-    seek();
-    // Loads of the next step; past the last one they return zeros.
+    const int t1 = t0 + p.per < p.nk ? t0 + p.per : p.nk;
+    Walk<BM, kBK, NW, AALONG, 1> wa;
+    Walk<BN, kBK, NW, BALONG, 1> wb;
+    wa.init(p.A, i0, p.m, t0, p.k, lane);
+    wb.init(p.B, j0, p.n, t0, p.k, lane);
+    int tl = t0;  // step of the next loads
     auto load = [&](short* lds) {
-        const int summed = p.k - (int64_t)tl * kBK < kBK
-                               ? (int)(p.k - (int64_t)tl * kBK)
-                               : kBK;
-        sa.load(ca.at, todo > 0 ? ca.left : 0, lda2, summed, lds, wave);
-        sb.load(cb.at, todo > 0 ? cb.left : 0, ldb2, summed, lds + BM * kBK,
-                wave);
-        --todo;
+        const int64_t summed = p.k - (int64_t)tl * kBK;
+        const int have = summed < kBK ? (int)summed : kBK;
+        wa.load(have, tl < t1, lds, wave);
+        wb.load(have, tl < t1, lds + BM * kBK, wave);
         ++tl;
-        ca.at += stepa;
-        ca.left -= stepa;
-        cb.at += stepb;
-        cb.left -= stepb;
-        if (kSegs > 1 && tl == p.nk) {
-            tl = 0;
-            ++seg;
-            seek();
-        }
     };
 
     floatx4 acc[FM][FN];
@@ -391,7 +459,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
         for (int f = 0; f < FM; ++f)
 #pragma unroll
             for (int g = 0; g < FN; ++g)
-                acc[f][g] = mfma<IT>(b[g], a[f], acc[f][g]);
+                acc[f][g] = mfma<OT>(b[g], a[f], acc[f][g]);
     };
     // The reads of a half spread over the products of the other half.
     constexpr int kReads = (AALONG ? FM : 2 * FM) + (BALONG ? FN : 2 * FN);
@@ -438,68 +506,128 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
     }
     meet<0>();
 
-    // the wave's own part of the buffers, kRows rows of its columns at a time
-    constexpr int kCols = FN * 16, kRows = BM / WGM < 64 ? BM / WGM : 64;
-    constexpr int kWaveFloats = 2 * kLds / 2 / NW;
-    static_assert(kRows * kCols <= kWaveFloats, "slab");
-    static_assert(BM / WGM % 32 == 0 && BN / WGN % 32 == 0, "Frag");
-    float* slab = (float*)(wave < NW / 2 ? lds0 : lds1) +
-                  (wave % (NW / 2)) * kWaveFloats;
-    constexpr int kLanes = kCols / 8;   // lanes of a row
-    constexpr int kAtOnce = 64 / kLanes;
-    const int lr = lane / kLanes, lc = lane % kLanes * 8;
-    const int64_t j = j0 + wj + lc;
-    const int count = eight_of(p.n, j);
-    Eight<OT> bias;
+    write_tile<OT, FM, FN>(p, acc,
+                           wave_slab<kSlab, NW, kLds>(lds0, lds1, wave),
+                           i0 + wi, j0 + wj, lane);
+}
+
+// 32-bit factors in three bf16 planes h, m, l: of the nine products of planes
+// the six that reach 2^-24 of the whole.  All six come from one reading of
+// the planes' fragments, so that here LDS is read half as much for each
+// matrix instruction as with 16-bit factors.  A step (32 summed values):
+//   h and h' are in registers; read m and m', multiply h h';  read l and l',
+//   multiply h m', m h', m m';  meet the other waves, start the loads of the
+//   step after next, read the next h and h', multiply h l', l h'.
+template <int BM, int BN, int WGM, int WGN, int ST, bool AALONG, bool BALONG>
+__global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
+{
+    constexpr int NW = WGM * WGN;
+    constexpr int FM = BM / WGM / 16, FN = BN / WGN / 16;
+    constexpr int kBK = kStep32, kSlab = slab_rows(FM) * FN * 16;
+    constexpr int kB = 3 * BM * kBK;            // where B's planes begin
+    constexpr int kLds = 3 * (BM + BN) * kBK;   // values of a buffer
+    __shared__ __align__(1024) short lds0[kLds];
+    __shared__ __align__(1024) short lds1[kLds];
+    __shared__ __align__(1024) short lds2[ST > 2 ? kLds : 8];
+    static_assert(ST == 2 || ST == 3, "buffers");
+    constexpr int kLoads = kLds / 512 / NW;  // of a wave in a step
+
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    unsigned ti, tj;
+    tile_of(blockIdx.x, p.tm, p.tn, ti, tj);
+    const int64_t i0 = (int64_t)ti * BM, j0 = (int64_t)tj * BN;
+    const int wi = wave / WGN * (BM / WGM), wj = wave % WGN * (BN / WGN);
+
+    Frag<BM, kBK, AALONG> fa;
+    Frag<BN, kBK, BALONG> fb;
+    fa.init(wi, lane);
+    fb.init(wj, lane);
+    const int t0 = blockIdx.y * p.per;
+    const int t1 = t0 + p.per < p.nk ? t0 + p.per : p.nk;
+    Walk<BM, kBK, NW, AALONG, 3> wa;
+    Walk<BN, kBK, NW, BALONG, 3> wb;
+    wa.init(p.A, i0, p.m, t0, p.k, lane);
+    wb.init(p.B, j0, p.n, t0, p.k, lane);
+    int tl = t0;  // step of the next loads
+    auto load = [&](short* lds) {
+        const int64_t summed = p.k - (int64_t)tl * kBK;
+        const int have = summed < kBK ? (int)summed : kBK;
+        wa.load(have, tl < t1, lds, wave);
+        wb.load(have, tl < t1, lds + kB, wave);
+        ++tl;
+    };
+
+    floatx4 acc[FM][FN];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) bias.v[c] = 0.0f;
-    if (p.e.bias && p.splits == 1) bias.load(p.e.bias, j, count);
+    for (int f = 0; f < FM; ++f)
 #pragma unroll
-    for (int s = 0; s < BM / WGM / kRows; ++s) {
+        for (int g = 0; g < FN; ++g) acc[f][g] = floatx4{0, 0, 0, 0};
+
+    short8v ah[FM], bh[FN], am[FM], bm[FN], al[FM], bl[FN], an[FM], bn[FN];
+    auto frags = [&](const short* lds, int plane, short8v* a, short8v* b) {
 #pragma unroll
-        for (int f = 0; f < kRows / 16; ++f)
+        for (int g = 0; g < FN; ++g)
+            b[g] = fb.read(lds + kB + plane * BN * kBK, wj, g, 0, lane);
 #pragma unroll
-            for (int g = 0; g < FN; ++g) {
-                const int r = f * 16 + (lane & 15);
-                const int c = g * 4 + (lane >> 4);  // 4 columns each
-                *(floatx4*)(slab + r * kCols + ((c ^ (r & 7)) * 4)) =
-                    acc[s * (kRows / 16) + f][g];
-            }
-#pragma unroll 2
-        for (int r0 = 0; r0 < kRows; r0 += kAtOnce) {
-            const int r = r0 + lr;
-            const int64_t i = i0 + wi + s * kRows + r;
-            if (i < p.m && count > 0) {
-                Eight<OT> x, res;
-                const float* q = slab + r * kCols;
-                const floatx4 u =
-                    *(const floatx4*)(q + (((lc / 4) ^ (r & 7)) * 4));
-                const floatx4 v =
-                    *(const floatx4*)(q + (((lc / 4 + 1) ^ (r & 7)) * 4));
+        for (int f = 0; f < FM; ++f)
+            a[f] = fa.read(lds + plane * BM * kBK, wi, f, 0, lane);
+    };
+    auto multiply = [&](const short8v* a, const short8v* b) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    x.v[c] = u[c];
-                    x.v[4 + c] = v[c];
-                }
-                if (p.splits > 1) {
-                    Eight<SVM_F32> y;
+        for (int f = 0; f < FM; ++f)
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) y.v[c] = x.v[c];
-                    const int64_t at =
-                        ((int64_t)blockIdx.y * p.m + i) * p.n + j;
-                    y.store(p.part, at, count);
-                } else {
-                    if (p.e.residual)
-                        res.load(p.e.residual, i * p.e.ldr + j, count);
-                    if constexpr (OT == SVM_F32)
-                        mend(x.v, count, [&](int c) {
-                            return exact_sum(p.A, p.B, i, j + c, p.k);
-                        });
-                    finish<OT>(p.e, x, bias, res, i, j, count);
-                }
-            }
+            for (int g = 0; g < FN; ++g)
+                acc[f][g] = mfma<SVM_BF16>(b[g], a[f], acc[f][g]);
+    };
+    constexpr int kReads = (AALONG ? FM : 2 * FM) + (BALONG ? FN : 2 * FN);
+    // the reads spread over the products of a part of the step
+    auto spread = [&]() {
+#pragma unroll
+        for (int r = 0; r < kReads; ++r) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         }
+    };
+    auto step = [&](short* cur, short* oth) {
+        __builtin_amdgcn_sched_barrier(0);
+        frags(cur, 1, am, bm);
+        multiply(ah, bh);
+        spread();
+        __builtin_amdgcn_sched_barrier(0);
+        frags(cur, 2, al, bl);
+        multiply(ah, bm);
+        multiply(am, bh);
+        multiply(am, bm);
+        spread();
+        meet<(ST - 2) * kLoads>();
+        load(cur);
+        __builtin_amdgcn_sched_barrier(0);
+        frags(oth, 0, an, bn);
+        multiply(ah, bl);
+        multiply(al, bh);
+        spread();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < FM; ++f) ah[f] = an[f];
+#pragma unroll
+        for (int g = 0; g < FN; ++g) bh[g] = bn[g];
+    };
+
+    load(lds0);
+    load(lds1);
+    if (ST > 2) load(lds2);
+    meet<(ST - 1) * kLoads>();
+    frags(lds0, 0, ah, bh);
+    for (int t = t0; t < t1; t += ST) {
+        step(lds0, lds1);
+        if (t + 1 < t1) step(lds1, ST > 2 ? lds2 : lds0);
+        if (ST > 2 && t + 2 < t1) step(lds2, lds0);
     }
+    meet<0>();
+    write_tile<SVM_F32, FM, FN>(p, acc,
+                                wave_slab<kSlab, NW, kLds>(lds0, lds1, wave),
+                                i0 + wi, j0 + wj, lane);
 }
 
 // Sums the parts of a split product and finishes it, eight columns a thread.
@@ -566,16 +694,14 @@ struct Sixteen {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             if constexpr (DT == SVM_F32) {
-                bf16x8 a, b, c;
+                float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    __bf16 ph, pm, pl;
-                    three_parts(raw[u].at(e), ph, pm, pl);
-                    a[e] = ph, b[e] = pm, c[e] = pl;
-                }
-                h[u] = __builtin_bit_cast(short8v, a);
-                m[u] = __builtin_bit_cast(short8v, b);
-                l[u] = __builtin_bit_cast(short8v, c);
+                for (int e = 0; e < 8; ++e) v[e] = raw[u].at(e);
+                Bf16x8 part[3];
+                three_parts8(v, part);
+                h[u] = __builtin_bit_cast(short8v, part[0]);
+                m[u] = __builtin_bit_cast(short8v, part[1]);
+                l[u] = __builtin_bit_cast(short8v, part[2]);
             } else {
                 h[u] = __builtin_bit_cast(short8v, raw[u].v[0]);
             }
@@ -674,32 +800,42 @@ __global__ __launch_bounds__(256) void k_planes(const Elem<DT>* X, int64_t ld,
     }
 }
 
-template <int IT, int OT, int BM, int BN, int WGM, int WGN, int ST>
+template <int OT, int BM, int BN, int WGM, int WGN, int ST>
 void launch_tiles(const Args& a, hipStream_t s)
 {
     const dim3 grid(a.tm * a.tn, (unsigned)a.splits), block(64 * WGM * WGN);
-    if (a.A.along && a.B.along)
-        hipLaunchKernelGGL((k_product<IT, OT, BM, BN, WGM, WGN, ST, true, true>),
-                           grid, block, 0, s, a);
-    else if (a.A.along)
-        hipLaunchKernelGGL((k_product<IT, OT, BM, BN, WGM, WGN, ST, true, false>),
-                           grid, block, 0, s, a);
-    else
-        hipLaunchKernelGGL((k_product<IT, OT, BM, BN, WGM, WGN, ST, false, false>),
-                           grid, block, 0, s, a);
+    auto go = [&]<bool AALONG, bool BALONG>() {
+        if constexpr (OT == SVM_F32)
+            hipLaunchKernelGGL(
+                (k_product32<BM, BN, WGM, WGN, ST, AALONG, BALONG>), grid,
+                block, 0, s, a);
+        else
+            hipLaunchKernelGGL(
+                (k_product<OT, BM, BN, WGM, WGN, ST, AALONG, BALONG>), grid,
+                block, 0, s, a);
+    };
+    if (a.A.along && a.B.along) go.template operator()<true, true>();
+    else if (a.A.along) go.template operator()<true, false>();
+    else go.template operator()<false, false>();
 }
 
-template <int IT, int OT>
-void launch_any(const Args& a, int tile, hipStream_t s)
+template <int OT>
+void launch_product(const Args& a, int tile, hipStream_t s)
 {
-    if (tile == 256) launch_tiles<IT, OT, 256, 256, 2, 4, 2>(a, s);
-    else if (tile == 128) launch_tiles<IT, OT, 128, 128, 2, 2, 4>(a, s);
-    else launch_tiles<IT, OT, 64, 64, 2, 2, 4>(a, s);
+    if constexpr (OT == SVM_F32) {
+        if (tile == 256) launch_tiles<OT, 128, 256, 2, 4, 2>(a, s);
+        else if (tile == 128) launch_tiles<OT, 128, 128, 2, 2, 3>(a, s);
+        else launch_tiles<OT, 64, 64, 2, 2, 3>(a, s);
+    } else {
+        if (tile == 256) launch_tiles<OT, 256, 256, 2, 4, 2>(a, s);
+        else if (tile == 128) launch_tiles<OT, 128, 128, 2, 2, 4>(a, s);
+        else launch_tiles<OT, 64, 64, 2, 2, 4>(a, s);
+    }
 }
 
-int64_t tiles(int64_t m, int64_t n, int t)
+int64_t tiles(int64_t m, int64_t n, int bm, int bn)
 {
-    return ((m + t - 1) / t) * ((n + t - 1) / t);
+    return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
 }
 
 constexpr int kCus = 256;
@@ -754,28 +890,28 @@ void product(const Product& p, Pieces& ws, hipStream_t s)
     a.n = p.n;
     a.k = p.k;
     a.e = p.e;
-    const int segs = p.dtype == SVM_F32 ? 6 : 1;
-    a.nk = (int)((p.k + kBK - 1) / kBK);
+    const bool f32 = p.dtype == SVM_F32;
+    const int bk = f32 ? kStep32 : kStep16;
+    a.nk = (int)((p.k + bk - 1) / bk);
     // Tiles: the largest of which there are enough for every CU; then, where
     // there are still too few, the steps are split over blocks.
-    int tile = 256;
-    if (tiles(p.m, p.n, 256) < kCus) tile = 128;
-    if (tile == 128 && tiles(p.m, p.n, 128) < kCus) tile = 64;
-    const int64_t nt = tiles(p.m, p.n, tile);
-    const int64_t steps = (int64_t)segs * a.nk;
+    int tile = 256, bm = f32 ? 128 : 256;
+    if (tiles(p.m, p.n, bm, tile) < kCus) bm = tile = 128;
+    if (tile == 128 && tiles(p.m, p.n, 128, 128) < kCus) bm = tile = 64;
+    const int64_t nt = tiles(p.m, p.n, bm, tile);
     int64_t splits = 1;
     if (nt < kCus) splits = (2 * kCus) / nt;
-    if (splits > steps / 4) splits = steps / 4;
+    if (splits > a.nk / 4) splits = a.nk / 4;
     if (splits < 1) splits = 1;
-    a.per = (int)((steps + splits - 1) / splits);
-    a.splits = (int)((steps + a.per - 1) / a.per);
-    a.tm = (unsigned)((p.m + tile - 1) / tile);
+    a.per = (int)((a.nk + splits - 1) / splits);
+    a.splits = (a.nk + a.per - 1) / a.per;
+    a.tm = (unsigned)((p.m + bm - 1) / bm);
     a.tn = (unsigned)((p.n + tile - 1) / tile);
     if (a.splits > 1) a.part = ws.take<float>(a.splits * p.m * p.n);
     if (!ws.run) return;
-    if (p.dtype == SVM_F32) launch_any<SVM_BF16, SVM_F32>(a, tile, s);
-    else if (p.dtype == SVM_BF16) launch_any<SVM_BF16, SVM_BF16>(a, tile, s);
-    else launch_any<SVM_F16, SVM_F16>(a, tile, s);
+    if (f32) launch_product<SVM_F32>(a, tile, s);
+    else if (p.dtype == SVM_BF16) launch_product<SVM_BF16>(a, tile, s);
+    else launch_product<SVM_F16>(a, tile, s);
     if (a.splits > 1) {
         const int64_t nb = (p.m * ((p.n + 7) / 8) + 255) / 256;
         for_dtype(p.dtype, [&]<int DT>() {
