@@ -37,6 +37,13 @@ void for_dtype(int32_t t, F&& f)
         f.template operator()<SVM_F16>();
 }
 
+// t / n for 0 <= t < all, in 32 bits where they hold all (64-bit division is
+// long).
+__device__ __forceinline__ int64_t quotient(int64_t t, int64_t n, int64_t all)
+{
+    return all >> 31 ? t / n : (int64_t)((uint32_t)t / (uint32_t)n);
+}
+
 // Sum over the 64 lanes; every lane ends with it.
 __device__ __forceinline__ float wave_sum(float v)
 {

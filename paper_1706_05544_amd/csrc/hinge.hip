@@ -57,8 +57,7 @@ __global__ __launch_bounds__(THREADS) void k_hinge(HingeView p)
     for (int64_t e0 = ((int64_t)blockIdx.x * THREADS + threadIdx.x) * 8;
          e0 < total; e0 += (int64_t)gridDim.x * THREADS * 8) {
         const int count = eight_of(total, e0);
-        // (32 bits where they hold the index: 64-bit division is long)
-        int64_t i = total >> 31 ? e0 / p.n : (uint32_t)e0 / (uint32_t)p.n;
+        int64_t i = quotient(e0, p.n, total);
         int32_t c = (int32_t)(e0 - i * p.n);
         Eight<DT> x, d;
         const bool flat = p.lds == p.n;

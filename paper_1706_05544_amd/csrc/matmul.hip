@@ -289,7 +289,7 @@ __device__ __forceinline__ void mend(float (&v)[8], int count, F&& exact)
 template <int OT>
 __device__ __forceinline__ void finish(const Epilogue& e, Eight<OT>& x,
                                        const Eight<OT>& bias,
-                                       const Eight<OT>& res, int64_t i,
+                                       const RawEight<OT>& res, int64_t i,
                                        int64_t j, int count)
 {
 #pragma unroll
@@ -298,7 +298,7 @@ __device__ __forceinline__ void finish(const Epilogue& e, Eight<OT>& x,
     act_values(e.act, x.v);
     if (e.residual) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) x.v[c] += res.v[c];
+        for (int c = 0; c < 8; ++c) x.v[c] += res.at(c);
     }
     x.store(e.Y, i * e.ldy + j, count);
 }
@@ -348,6 +348,7 @@ __device__ __forceinline__ void write_tile(const Args& p,
 #pragma unroll
     for (int c = 0; c < 8; ++c) bias.v[c] = 0.0f;
     if (p.e.bias && p.splits == 1) bias.load(p.e.bias, j, count);
+    constexpr int kTurns = kRows / kAtOnce, kGroup = kTurns < 2 ? kTurns : 2;
 #pragma unroll
     for (int s = 0; s < FM * 16 / kRows; ++s) {
 #pragma unroll
@@ -359,38 +360,46 @@ __device__ __forceinline__ void write_tile(const Args& p,
                 *(floatx4*)(slab + r * kCols + ((c ^ (r & 7)) * 4)) =
                     acc[s * (kRows / 16) + f][g];
             }
-#pragma unroll 2
-        for (int r0 = 0; r0 < kRows; r0 += kAtOnce) {
-            const int r = r0 + lr;
-            const int64_t i = iw + s * kRows + r;
-            if (i < p.m && count > 0) {
-                Eight<OT> x, res;
+        // turns of kAtOnce rows, kGroup of them with their residuals loaded
+        // together, before any of them is written
+#pragma unroll 1
+        for (int t0 = 0; t0 < kTurns; t0 += kGroup) {
+            RawEight<OT> res[kGroup];
+            const int64_t i0 = iw + s * kRows + t0 * kAtOnce + lr;
+#pragma unroll
+            for (int u = 0; u < kGroup; ++u)
+                if (p.e.residual && p.splits == 1 && i0 + u * kAtOnce < p.m)
+                    res[u].load(p.e.residual,
+                                (i0 + u * kAtOnce) * p.e.ldr + j, count);
+#pragma unroll
+            for (int u = 0; u < kGroup; ++u) {
+                const int r = (t0 + u) * kAtOnce + lr;
+                const int64_t i = i0 + u * kAtOnce;
+                if (i >= p.m || count == 0) continue;
+                Eight<OT> x;
                 const float* q = slab + r * kCols;
-                const floatx4 u =
+                const floatx4 lo =
                     *(const floatx4*)(q + (((lc / 4) ^ (r & 7)) * 4));
-                const floatx4 v =
+                const floatx4 hi =
                     *(const floatx4*)(q + (((lc / 4 + 1) ^ (r & 7)) * 4));
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    x.v[c] = u[c];
-                    x.v[4 + c] = v[c];
+                    x.v[c] = lo[c];
+                    x.v[4 + c] = hi[c];
                 }
                 if (p.splits > 1) {
                     Eight<SVM_F32> y;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) y.v[c] = x.v[c];
-                    const int64_t at =
-                        ((int64_t)blockIdx.y * p.m + i) * p.n + j;
-                    y.store(p.part, at, count);
-                } else {
-                    if (p.e.residual)
-                        res.load(p.e.residual, i * p.e.ldr + j, count);
-                    if constexpr (OT == SVM_F32)
-                        mend(x.v, count, [&](int c) {
-                            return exact_sum(p.A, p.B, i, j + c, p.k);
-                        });
-                    finish<OT>(p.e, x, bias, res, i, j, count);
+                    y.store(p.part,
+                            ((int64_t)blockIdx.y * p.m + i) * p.n + j, count);
+                    continue;
                 }
+                if constexpr (OT == SVM_F32)
+                    mend(x.v, count, [&](int c) {
+                        return exact_sum(p.A, p.B, i, j + c, p.k);
+                    });
+                finish<OT>(p.e, x, bias, res[u], i, j, count);
             }
         }
     }
@@ -638,9 +647,11 @@ __global__ __launch_bounds__(256) void k_join(Args p)
     const int64_t all = p.m * groups;
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all;
          t += (int64_t)gridDim.x * 256) {
-        const int64_t i = t / groups, j = t % groups * 8;
+        const int64_t i = quotient(t, groups, all);
+        const int64_t j = (t - i * groups) * 8;
         const int count = eight_of(p.n, j);
-        Eight<OT> x, bias, res;
+        Eight<OT> x, bias;
+        RawEight<OT> res;
 #pragma unroll
         for (int c = 0; c < 8; ++c) x.v[c] = bias.v[c] = 0.0f;
 #pragma unroll 4
@@ -761,9 +772,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(FewArgs p)
     const int64_t j = j0 + c0;
     const int count = eight_of(p.n, j);
     if (row >= p.m || count == 0) return;
-    Eight<DT> v, bias, res;
+    Eight<DT> v, bias;
+    RawEight<DT> res;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) v.v[c] = bias.v[c] = res.v[c] = 0.0f;
+    for (int c = 0; c < 8; ++c) v.v[c] = bias.v[c] = 0.0f;
     if (p.e.bias) bias.load(p.e.bias, j, count);
     if (p.e.residual) res.load(p.e.residual, row * p.e.ldr + j, count);
 #pragma unroll
@@ -793,7 +805,8 @@ __global__ __launch_bounds__(256) void k_planes(const Elem<DT>* X, int64_t ld,
     const int64_t groups = ldp / 8, all = rows * groups;
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all;
          t += (int64_t)gridDim.x * 256) {
-        const int64_t i = t / groups, j = t % groups * 8;
+        const int64_t i = quotient(t, groups, all);
+        const int64_t j = (t - i * groups) * 8;
         Eight<DT> x;
         x.load(X, i * ld + j, eight_of(cols, j));
         store_factor<DT>(x.v, dst, i * ldp + j, plane);
