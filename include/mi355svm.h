@@ -395,7 +395,7 @@ typedef enum {
  * X m x k (m >= 0), W n x k, bias 1 x n, residual, Y and Z m x n; bias,
  * residual and Z are nullable.  Z receives what the gradient needs (for
  * every act but SVM_ACT_NONE).  residual may be Y itself (same data and
- * ld).  m < 2^31, n and k in [1, 2^22]. */
+ * ld).  m < 2^31, n and k in [1, 2^21]. */
 svm_status svm_linear(const svm_array *X, const svm_array *W,
                       const svm_array *bias, const svm_array *residual,
                       int32_t act, const svm_array *Y, const svm_array *Z,
@@ -428,7 +428,7 @@ svm_status svm_linear_backward_workspace(const svm_array *dY,
  * mean and rstd = 1 / sqrt(mean of (x - mean)^2 + eps).  weight and bias
  * (1 x cols) are nullable (1 and 0).  mean and rstd (rows floats each,
  * nullable) receive the statistics that the gradient needs.  Y may be X
- * itself (same data and ld).  cols in [1, 2^22]. */
+ * itself (same data and ld).  cols in [1, 2^21]. */
 svm_status svm_layer_norm(const svm_array *X, const svm_array *weight,
                           const svm_array *bias, double eps,
                           const svm_array *Y, float *mean, float *rstd,
@@ -459,7 +459,7 @@ svm_status svm_layer_norm_backward_workspace(int64_t rows, int64_t cols,
  * y_ic = +1 where c is labels[i], else -1; with one column, label 1 is +1
  * and label 0 is -1.  A label outside [0, C) (outside {0, 1} with one
  * column) leaves its row out: it adds nothing and its gradient is 0.  S and
- * dS rows x C, C in [1, 2^22]; dS is nullable and may be S itself.  labels:
+ * dS rows x C, C in [1, 2^21]; dS is nullable and may be S itself.  labels:
  * int32, rows of them; loss: one float; both on the device. */
 svm_status svm_hinge_loss(const svm_array *S, const int32_t *labels,
                           double scale, const svm_array *dS, float *loss,

@@ -193,73 +193,21 @@ __device__ __forceinline__ int eight_of(int64_t n, int64_t j)
     return n - j >= 8 ? 8 : n - j > 0 ? (int)(n - j) : 0;
 }
 
-// The three bf16 parts of a 32-bit value: x = h + m + l, each part what is
-// left rounded to nearest (to zero where rounding would overflow).
-__device__ __forceinline__ void three_parts(float x, __bf16& h, __bf16& m,
-                                            __bf16& l)
-{
-    h = (__bf16)x;
-    if (!(fabsf(x) <= 3.402823466e38f)) {  // infinity, NaN: h alone
-        m = l = (__bf16)0.0f;
-        return;
-    }
-    if (!(fabsf((float)h) <= 3.402823466e38f))
-        h = __builtin_bit_cast(
-            __bf16, (unsigned short)(__builtin_bit_cast(uint32_t, x) >> 16));
-    const float r = x - (float)h;
-    m = (__bf16)r;
-    l = (__bf16)(r - (float)m);
-}
-
+// The three bf16 parts of eight 32-bit values: x = h + m + l, each part what
+// is left rounded to nearest.  Where x is not finite, or rounds to a bf16
+// that is not, h is that and the others are 0.
 typedef __bf16 Bf16x8 __attribute__((ext_vector_type(8)));
 
-// The same for eight values; one that is not finite, or would round past the
-// largest bf16, sends its eight the long way.
-__device__ __forceinline__ void three_parts8(const float (&v)[8],
-                                             Bf16x8 (&part)[3])
+__device__ __forceinline__ void three_parts(const float (&v)[8],
+                                            Bf16x8 (&part)[3])
 {
-    uint32_t top = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const uint32_t a = __builtin_bit_cast(uint32_t, v[e]) & 0x7fffffffu;
-        top = a > top ? a : top;
-    }
-    if (top < 0x7f7f8000u) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            part[0][e] = (__bf16)v[e];
-            const float r = v[e] - (float)part[0][e];
-            part[1][e] = (__bf16)r;
-            part[2][e] = (__bf16)(r - (float)part[1][e]);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            __bf16 h, m, l;
-            three_parts(v[e], h, m, l);
-            part[0][e] = h, part[1][e] = m, part[2][e] = l;
-        }
-    }
-}
-
-// Eight values as a factor of a product keeps them: DT itself, or for 32 bits
-// three bf16 planes, `plane` values apart.
-template <int DT>
-__device__ __forceinline__ void store_factor(const float (&v)[8], void* dst,
-                                             int64_t at, int64_t plane)
-{
-    if constexpr (DT == SVM_F32) {
-        Bf16x8 part[3];
-        three_parts8(v, part);
-#pragma unroll
-        for (int q = 0; q < 3; ++q)
-            *(Bf16x8*)((__bf16*)dst + q * plane + at) = part[q];
-    } else {
-        typedef Elem<DT> T8 __attribute__((ext_vector_type(8)));
-        T8 x;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = (Elem<DT>)v[e];
-        *(T8*)((Elem<DT>*)dst + at) = x;
+        part[0][e] = (__bf16)v[e];
+        const float r =
+            fabsf(v[e]) < 3.38e38f ? v[e] - (float)part[0][e] : 0.0f;
+        part[1][e] = (__bf16)r;
+        part[2][e] = (__bf16)(r - (float)part[1][e]);
     }
 }
 

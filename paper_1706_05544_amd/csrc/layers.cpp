@@ -51,7 +51,7 @@ svm_status check_first(const svm_array* a, const char* name)
     if (a->rows < 0 || a->rows > ((int64_t)1 << 31) - 1)
         return fail(SVM_E_INVALID, n + ": rows must be in [0, 2^31)");
     if (a->cols < 1 || a->cols > msvm::kMaxWidth)
-        return fail(SVM_E_INVALID, n + ": cols must be in [1, 2^22]");
+        return fail(SVM_E_INVALID, n + ": cols must be in [1, 2^21]");
     return check_array(a, name, a->rows, a->cols, a->dtype);
 }
 
@@ -127,7 +127,7 @@ svm_status check_linear_inputs(const svm_array* X, const svm_array* W)
     CHECK(check_first(X, "X"));
     CHECK(check_first(W, "W"));
     if (W->rows < 1 || W->rows > msvm::kMaxWidth)
-        return fail(SVM_E_INVALID, "W: rows must be in [1, 2^22]");
+        return fail(SVM_E_INVALID, "W: rows must be in [1, 2^21]");
     return check_array(W, "W", W->rows, X->cols, X->dtype);
 }
 
@@ -304,7 +304,7 @@ svm_status svm_layer_norm_backward_workspace(int64_t rows, int64_t cols,
     if (rows < 0 || rows > ((int64_t)1 << 31) - 1)
         return fail(SVM_E_INVALID, "rows must be in [0, 2^31)");
     if (cols < 1 || cols > msvm::kMaxWidth)
-        return fail(SVM_E_INVALID, "cols must be in [1, 2^22]");
+        return fail(SVM_E_INVALID, "cols must be in [1, 2^21]");
     *bytes = msvm::norm_backward_bytes(rows, cols);
     return SVM_OK;
 }
@@ -367,7 +367,7 @@ svm_status svm_hinge_loss_workspace(int64_t rows, int64_t cols,
     if (rows < 0 || rows > ((int64_t)1 << 31) - 1)
         return fail(SVM_E_INVALID, "rows must be in [0, 2^31)");
     if (cols < 1 || cols > msvm::kMaxWidth)
-        return fail(SVM_E_INVALID, "cols must be in [1, 2^22]");
+        return fail(SVM_E_INVALID, "cols must be in [1, 2^21]");
     *bytes = msvm::hinge_bytes(rows, cols);
     return SVM_OK;
 }

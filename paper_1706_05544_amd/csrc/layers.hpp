@@ -6,7 +6,7 @@
 
 namespace msvm {
 
-constexpr int64_t kMaxWidth = (int64_t)1 << 22;  // columns of an array
+constexpr int64_t kMaxWidth = (int64_t)1 << 21;  // columns of an array
 constexpr int kAdamBlock = 256;  // values that share a scale (8-bit states)
 
 inline size_t dtype_bytes(int32_t t) { return t == SVM_F32 ? 4 : 2; }

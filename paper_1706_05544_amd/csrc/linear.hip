@@ -6,9 +6,8 @@ namespace msvm {
 
 namespace {
 
-// dZ = dY act'(Z) as a factor of the products (in 32 bits: three planes; its
-// rows end in zeros up to a multiple of 8), and the sums of its columns over
-// this block's rows.  One pass over dY and Z: 8 columns to a thread, 32
+// dZ = dY act'(Z) as a factor of the products (its rows end in zeros up to a
+// multiple of 8), and the sums of its columns over this block's rows.  One pass over dY and Z: 8 columns to a thread, 32
 // threads side by side, 8 rows at once.
 constexpr int kGradCols = 256, kGradLanes = 8;
 
@@ -16,7 +15,7 @@ struct GradArgs {
     const void *dY, *Z;
     int64_t ldg, ldz, m, n, rows;  // rows of a block
     void* dZ;
-    int64_t ldd, plane;
+    int64_t ldd;
     float* part;
     int act;
 };
@@ -45,7 +44,7 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs p)
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += g.v[e];
-            if (p.dZ) store_factor<DT>(g.v, p.dZ, i * p.ldd + j, p.plane);
+            if (p.dZ) g.store(p.dZ, i * p.ldd + j, 8);
         }
     }
     if (!p.part) return;
@@ -134,17 +133,14 @@ void launch_column_sums(const float* part0, const float* part1, int64_t np,
 namespace {
 
 // A factor of a product from an array: as it is where the product can read
-// it so, else a copy in the workspace (32 bits: in three planes).
+// it so, else a copy in the workspace.
 Factor factor_of(const svm_array& a, bool along, Pieces& ws, hipStream_t s)
 {
-    Factor f{a.data, a.ld, 0, along};
-    if (factor_fits(a, along)) return f;
-    f.ld = (a.cols + 7) / 8 * 8;
-    f.plane = a.rows * f.ld;
-    void* copy = ws.take<uint16_t>((a.dtype == SVM_F32 ? 3 : 1) * f.plane);
-    f.data = copy;
-    if (ws.run) launch_planes(a, copy, f.ld, f.plane, s);
-    return f;
+    if (factor_fits(a, along)) return {a.data, a.ld, along};
+    const int64_t ld = (a.cols + 7) / 8 * 8;
+    void* copy = ws.take<char>(a.rows * ld * dtype_bytes(a.dtype));
+    if (ws.run) launch_padded(a, copy, ld, s);
+    return {copy, ld, along};
 }
 
 Epilogue plain(const svm_array& out)
@@ -183,11 +179,10 @@ void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
     // read as they are; else one pass makes dZ, and the sums with it
     const bool copy =
         (dx || dw) && (slope || !factor_fits(a.dY, dx));
-    Factor dz{a.dY.data, a.dY.ld, 0, true};
+    Factor dz{a.dY.data, a.dY.ld, true};
     if (copy) {
         dz.ld = (n + 7) / 8 * 8;
-        dz.plane = m * dz.ld;
-        dz.data = ws.take<uint16_t>((t == SVM_F32 ? 3 : 1) * dz.plane);
+        dz.data = ws.take<char>(m * dz.ld * dtype_bytes(t));
     }
     const int64_t rows = grad_rows(m, n), np = (m + rows - 1) / rows;
     float* part = db ? ws.take<float>(np * n) : nullptr;
@@ -196,8 +191,8 @@ void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
                    a.dY.ld,   a.Z.ld,
                    m,         n,
                    rows,      copy ? const_cast<void*>(dz.data) : nullptr,
-                   dz.ld,     dz.plane,
-                   part,      a.act};
+                   dz.ld,     part,
+                   a.act};
         const dim3 grid((unsigned)((n + kGradCols - 1) / kGradCols),
                         (unsigned)np);
         for_dtype(t, [&]<int DT>() {

@@ -32,7 +32,7 @@ namespace msvm {
 namespace {
 
 constexpr int kStep16 = 64;  // summed values of a step: 16-bit factors,
-constexpr int kStep32 = 32;  // 32-bit ones (three planes)
+constexpr int kStep32 = 32;  // 32-bit ones (three parts)
 // An address past every descriptor: the rows of a tile end below it, and
 // added to a tile's own offsets it does not wrap.
 constexpr uint32_t kPast = 0x80000000u;
@@ -85,12 +85,11 @@ __device__ __forceinline__ void lds_load(intx4 rs, short* lds, uint32_t off,
         : "memory");
 }
 
-// The lane's share of a factor's tile loads: R rows (ALONG) or columns, BK
-// summed values.
-template <int R, int BK, int NW, bool ALONG>
+// The lane's share of a factor's tile loads: R rows (ALONG) or columns.
+template <int R, int NW, bool ALONG>
 struct Stage {
-    static constexpr int kInstr = R * BK / 512 / NW;  // of a wave, 1 KiB each
-    static constexpr int kRowLanes = (ALONG ? BK : R) / 8;  // 16-byte pieces
+    static constexpr int kInstr = R / 8 / NW;  // of a wave, 1 KiB each
+    static constexpr int kRowLanes = ALONG ? 8 : R / 8;  // 16-byte pieces
     static constexpr int kRows = 64 / kRowLanes;         // rows of a load
     uint32_t off[2];  // byte offset in the tile, for each kind of load
     int piece;        // first summed value of the piece (ALONG, kind 0)
@@ -101,11 +100,9 @@ struct Stage {
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
             int c;
-            if (ALONG && BK == 64) {
+            if (ALONG) {
                 // rows 8 q + row: key = (r & 3) | ((r >> 2 ^ r >> 4) & 1) << 2
                 c = pos ^ ((row & 3) | (((row >> 2) ^ v) & 1) << 2);
-            } else if (ALONG) {
-                c = pos ^ ((row >> 1) & 3);  // two rows to 128 bytes
             } else {
                 const int r = kRows == 2 ? v * 2 + row : row;
                 c = pos ^ (2 * (r & 3));
@@ -132,15 +129,13 @@ struct Stage {
         uint32_t o[2] = {off[0], off[1]};
         if (ALONG) {
             if (piece >= summed) o[0] = kPast;
-            if (BK == 64 && (piece ^ 32) >= summed) o[1] = kPast;
+            if ((piece ^ 32) >= summed) o[1] = kPast;
         }
 #pragma unroll
         for (int it = 0; it < kInstr; ++it) {
             const int q = wave * kInstr + it;
             // which kind load q is
-            const int v = ALONG ? (BK == 64 ? (q >> 1) & 1 : 0)
-                          : kRows == 2 ? q & 1
-                                       : 0;
+            const int v = ALONG ? (q >> 1) & 1 : kRows == 2 ? q & 1 : 0;
             lds_load(rs, lds + q * 512, v ? o[1] : o[0],
                      (uint32_t)(q * kRows) * (uint32_t)ld2);
         }
@@ -162,13 +157,14 @@ __device__ __forceinline__ void meet()
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// A factor's tile loads step by step: P planes, R rows or columns.
-template <int R, int BK, int NW, bool ALONG, int P>
+// A factor's tile loads step by step: R rows or columns.
+template <int R, int NW, bool ALONG>
 struct Walk {
-    Stage<R, BK, NW, ALONG> stage;
-    const char* at;  // the tile of the next step (first plane)
-    int64_t left;    // bytes from there to the plane's end
-    int64_t step, plane;
+    static constexpr int BK = kStep16;
+    Stage<R, NW, ALONG> stage;
+    const char* at;  // the tile of the next step
+    int64_t left;    // bytes from there to the factor's end
+    int64_t step;
     int ld2;
 
     // x0: first row or column of the tile, of n; t0: first step, of k values
@@ -178,7 +174,6 @@ struct Walk {
         stage.init(f.ld, lane);
         ld2 = (int)f.ld * 2;
         step = ALONG ? 2 * BK : (int64_t)BK * ld2;
-        plane = 2 * f.plane;
         const int64_t k0 = t0 * BK;
         at = (const char*)f.data + (ALONG ? x0 * ld2 + k0 * 2
                                           : k0 * ld2 + x0 * 2);
@@ -190,10 +185,7 @@ struct Walk {
     __device__ __forceinline__ void load(int summed, bool there, short* lds,
                                          int wave)
     {
-#pragma unroll
-        for (int q = 0; q < P; ++q)
-            stage.load(at + q * plane, there ? left : 0, ld2, summed,
-                       lds + q * R * BK, wave);
+        stage.load(at, there ? left : 0, ld2, summed, lds, wave);
         at += step;
         left -= step;
     }
@@ -246,25 +238,18 @@ struct Frag {
     }
 };
 
-// A sum of 32-bit factors that is not finite, again from the factors
-// themselves, which their planes add up to: an infinity has zeros in its
-// lower planes, and its products with another factor's differ in sign.
+// A sum of 32-bit factors that is not finite, again in 32 bits: an infinity
+// has zeros for its lower parts, its products with another factor's parts
+// differ in sign, and what rounds past the largest bf16 is none.
 __device__ __forceinline__ float exact_sum(const Factor& A, const Factor& B,
                                            int64_t i, int64_t j, int64_t k)
 {
-    const __bf16* a = (const __bf16*)A.data + (A.along ? i * A.ld : i);
-    const __bf16* b = (const __bf16*)B.data + (B.along ? j * B.ld : j);
+    const float* a = (const float*)A.data + (A.along ? i * A.ld : i);
+    const float* b = (const float*)B.data + (B.along ? j * B.ld : j);
     const int64_t sa = A.along ? 1 : A.ld, sb = B.along ? 1 : B.ld;
     float sum = 0.0f;
 #pragma unroll 1
-    for (int64_t r = 0; r < k; ++r) {
-        const __bf16 *x = a + r * sa, *y = b + r * sb;
-        const float u = (float)x[0] + ((float)x[A.plane] +
-                                       (float)x[2 * A.plane]);
-        const float v = (float)y[0] + ((float)y[B.plane] +
-                                       (float)y[2 * B.plane]);
-        sum = fmaf(u, v, sum);
-    }
+    for (int64_t r = 0; r < k; ++r) sum = fmaf(a[r * sa], b[r * sb], sum);
     return sum;
 }
 
@@ -436,8 +421,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
     fb.init(wj, lane);
     const int t0 = blockIdx.y * p.per;
     const int t1 = t0 + p.per < p.nk ? t0 + p.per : p.nk;
-    Walk<BM, kBK, NW, AALONG, 1> wa;
-    Walk<BN, kBK, NW, BALONG, 1> wb;
+    Walk<BM, NW, AALONG> wa;
+    Walk<BN, NW, BALONG> wb;
     wa.init(p.A, i0, p.m, t0, p.k, lane);
     wb.init(p.B, j0, p.n, t0, p.k, lane);
     int tl = t0;  // step of the next loads
@@ -520,26 +505,133 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product(Args p)
                            i0 + wi, j0 + wj, lane);
 }
 
-// 32-bit factors in three bf16 planes h, m, l: of the nine products of planes
-// the six that reach 2^-24 of the whole.  All six come from one reading of
-// the planes' fragments, so that here LDS is read half as much for each
+// A thread's share of a 32-bit factor's tile (R rows or columns, 32 summed
+// values, T threads): pieces of 8 values from memory to registers, split there
+// into three bf16 parts and written to LDS, a plane for each part.  Rows may
+// begin anywhere; what lies past the factor's end comes as zeros.  LDS rows
+// along the summed index have 4 pieces, two rows to 128 bytes: piece c of row
+// r lies at c ^ (r / 2 mod 4).
+template <int R, int T, bool ALONG>
+struct Split {
+    static constexpr int kN = R * 4 / T;  // pieces of a thread
+    struct Raw {
+        floatx4 v[kN][2];
+    };
+    uint32_t off[kN];  // byte offset in the tile
+    int lds[kN];
+    const char* at;    // the tile of the next step
+    int64_t left, step;
+
+    __device__ __forceinline__ void init(const Factor& f, int64_t x0, int64_t n,
+                                         int64_t t0, int64_t k)
+    {
+        const int64_t k0 = t0 * kStep32;
+        step = 4 * (ALONG ? kStep32 : kStep32 * f.ld);
+        at = (const char*)f.data + 4 * (ALONG ? x0 * f.ld + k0
+                                              : k0 * f.ld + x0);
+        left = 4 * (ALONG ? (n - 1 - x0) * f.ld + k - k0
+                          : (k - 1 - k0) * f.ld + n - x0);
+#pragma unroll
+        for (int q = 0; q < kN; ++q) {
+            const int c = q * T + (int)threadIdx.x;
+            const int across = ALONG ? 4 : R / 8;
+            const int row = c / across, piece = c % across;
+            off[q] = (uint32_t)((int64_t)row * f.ld * 4 + piece * 32);
+            lds[q] = ALONG ? row * kStep32 + (piece ^ ((row >> 1) & 3)) * 8
+                           : row * R + (piece ^ (2 * (row & 3))) * 8;
+        }
+    }
+
+    // The next step's pieces (all of its summed values are there, or with
+    // there = false none: zeros).
+    __device__ __forceinline__ void load(Raw& raw, bool there)
+    {
+        const uint32_t range = !there || left <= 0 ? 0u
+                               : left < 0xffffffff ? (uint32_t)left
+                                                   : 0xffffffffu;
+        __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<char*>(at), 0, (int)range, 0x00020000);
+#pragma unroll
+        for (int q = 0; q < kN; ++q)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                raw.v[q][h] = __builtin_bit_cast(
+                    floatx4, __builtin_amdgcn_raw_buffer_load_b128(
+                              rs, (int)(off[q] + 16 * h), 0, 0));
+        at += step;
+        left -= step;
+    }
+
+    static __device__ __forceinline__ void split(const Raw& raw,
+                                                 Bf16x8 (&part)[kN][3])
+    {
+#pragma unroll
+        for (int q = 0; q < kN; ++q) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = raw.v[q][e / 4][e % 4];
+            three_parts(v, part[q]);
+        }
+    }
+
+    __device__ __forceinline__ void write(const Bf16x8 (&part)[kN][3],
+                                          short* buf) const
+    {
+#pragma unroll
+        for (int q = 0; q < kN; ++q)
+#pragma unroll
+            for (int s = 0; s < 3; ++s)
+                *(Bf16x8*)(buf + s * R * kStep32 + lds[q]) = part[q][s];
+    }
+
+    // The last, partial step: `summed` summed values from k0 on, the others
+    // zeros, straight to LDS.
+    __device__ __forceinline__ void tail(const Factor& f, int64_t x0, int64_t n,
+                                         int64_t k0, int summed, short* buf)
+    {
+#pragma unroll
+        for (int q = 0; q < kN; ++q) {
+            const int c = q * T + (int)threadIdx.x;
+            const int across = ALONG ? 4 : R / 8;
+            const int row = c / across, piece = c % across;
+            Eight<SVM_F32> x;
+            Bf16x8 part[3];
+            if (ALONG)
+                x.load(f.data, (x0 + row) * f.ld + k0 + piece * 8,
+                       x0 + row < n ? eight_of(summed, piece * 8) : 0);
+            else
+                x.load(f.data, (k0 + row) * f.ld + x0 + piece * 8,
+                       row < summed ? eight_of(n, x0 + piece * 8) : 0);
+            three_parts(x.v, part);
+#pragma unroll
+            for (int s = 0; s < 3; ++s)
+                *(Bf16x8*)(buf + s * R * kStep32 + lds[q]) = part[s];
+        }
+    }
+};
+
+// 32-bit factors, each in three bf16 parts h, m, l: of the nine products of
+// parts the six that reach 2^-24 of the whole.  All six come from one reading
+// of the parts' fragments, so that here LDS is read half as much for each
 // matrix instruction as with 16-bit factors.  A step (32 summed values):
 //   h and h' are in registers; read m and m', multiply h h';  read l and l',
-//   multiply h m', m h', m m';  meet the other waves, start the loads of the
-//   step after next, read the next h and h', multiply h l', l h'.
-template <int BM, int BN, int WGM, int WGN, int ST, bool AALONG, bool BALONG>
+//   split the values that have come for the step after next, multiply h m',
+//   m h', m m';  meet the other waves, write those to the buffer that this
+//   step has left, load values of a later step, read the next h and h',
+//   multiply h l', l h'.
+// AHEAD: steps whose values are under way to registers.
+template <int BM, int BN, int WGM, int WGN, int AHEAD, bool AALONG,
+          bool BALONG>
 __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
 {
-    constexpr int NW = WGM * WGN;
+    constexpr int NW = WGM * WGN, T = 64 * NW;
     constexpr int FM = BM / WGM / 16, FN = BN / WGN / 16;
     constexpr int kBK = kStep32, kSlab = slab_rows(FM) * FN * 16;
     constexpr int kB = 3 * BM * kBK;            // where B's planes begin
     constexpr int kLds = 3 * (BM + BN) * kBK;   // values of a buffer
     __shared__ __align__(1024) short lds0[kLds];
     __shared__ __align__(1024) short lds1[kLds];
-    __shared__ __align__(1024) short lds2[ST > 2 ? kLds : 8];
-    static_assert(ST == 2 || ST == 3, "buffers");
-    constexpr int kLoads = kLds / 512 / NW;  // of a wave in a step
+    static_assert(AHEAD == 1 || AHEAD == 2 || AHEAD == 4, "ring");
 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -552,19 +644,32 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
     Frag<BN, kBK, BALONG> fb;
     fa.init(wi, lane);
     fb.init(wj, lane);
+    // whole steps t0 .. t1 - 1; a last one that is not whole comes apart
     const int t0 = blockIdx.y * p.per;
-    const int t1 = t0 + p.per < p.nk ? t0 + p.per : p.nk;
-    Walk<BM, kBK, NW, AALONG, 3> wa;
-    Walk<BN, kBK, NW, BALONG, 3> wb;
-    wa.init(p.A, i0, p.m, t0, p.k, lane);
-    wb.init(p.B, j0, p.n, t0, p.k, lane);
+    const int whole = (int)(p.k / kBK);
+    const int t1 = t0 + p.per < whole ? t0 + p.per : whole;
+    using SA = Split<BM, T, AALONG>;
+    using SB = Split<BN, T, BALONG>;
+    SA sa;
+    SB sb;
+    sa.init(p.A, i0, p.m, t0, p.k);
+    sb.init(p.B, j0, p.n, t0, p.k);
+    typename SA::Raw ra[AHEAD];
+    typename SB::Raw rb[AHEAD];
+    Bf16x8 pa[SA::kN][3], pb[SB::kN][3];
     int tl = t0;  // step of the next loads
-    auto load = [&](short* lds) {
-        const int64_t summed = p.k - (int64_t)tl * kBK;
-        const int have = summed < kBK ? (int)summed : kBK;
-        wa.load(have, tl < t1, lds, wave);
-        wb.load(have, tl < t1, lds + kB, wave);
+    auto load = [&](int r) {
+        sa.load(ra[r], tl < t1);
+        sb.load(rb[r], tl < t1);
         ++tl;
+    };
+    auto split = [&](int r) {
+        SA::split(ra[r], pa);
+        SB::split(rb[r], pb);
+    };
+    auto write = [&](short* lds) {
+        sa.write(pa, lds);
+        sb.write(pb, lds + kB);
     };
 
     floatx4 acc[FM][FN];
@@ -590,50 +695,77 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
                 acc[f][g] = mfma<SVM_BF16>(b[g], a[f], acc[f][g]);
     };
     constexpr int kReads = (AALONG ? FM : 2 * FM) + (BALONG ? FN : 2 * FN);
-    // the reads spread over the products of a part of the step
-    auto spread = [&]() {
+    constexpr int kMul = FM * FN;
+    // reads, and with `valu` other arithmetic, between n matrix instructions
+    auto spread = [&](int n, int valu) {
 #pragma unroll
-        for (int r = 0; r < kReads; ++r) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        for (int r = 0; r < n; ++r) {
+            if (r < kReads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (valu) __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
         }
     };
-    auto step = [&](short* cur, short* oth) {
+    // ah, bh: this step's first parts, an, bn: where the next one's go
+    auto step = [&](short* cur, short* oth, int r, short8v* ah, short8v* bh,
+                    short8v* an, short8v* bn) {
         __builtin_amdgcn_sched_barrier(0);
         frags(cur, 1, am, bm);
         multiply(ah, bh);
-        spread();
+        spread(kMul, 0);
         __builtin_amdgcn_sched_barrier(0);
         frags(cur, 2, al, bl);
+        split(r);
         multiply(ah, bm);
         multiply(am, bh);
         multiply(am, bm);
-        spread();
-        meet<(ST - 2) * kLoads>();
-        load(cur);
+        spread(3 * kMul, 1);
+        meet<63>();
+        write(cur);
+        load(r);
         __builtin_amdgcn_sched_barrier(0);
         frags(oth, 0, an, bn);
         multiply(ah, bl);
         multiply(al, bh);
-        spread();
+        spread(2 * kMul, 0);
         __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int f = 0; f < FM; ++f) ah[f] = an[f];
-#pragma unroll
-        for (int g = 0; g < FN; ++g) bh[g] = bn[g];
     };
 
-    load(lds0);
-    load(lds1);
-    if (ST > 2) load(lds2);
-    meet<(ST - 1) * kLoads>();
+    load(0);
+    split(0);
+    write(lds0);
+    load(0);
+    split(0);
+    write(lds1);
+#pragma unroll
+    for (int r = 0; r < AHEAD; ++r) load(r);
+    meet<63>();
     frags(lds0, 0, ah, bh);
-    for (int t = t0; t < t1; t += ST) {
-        step(lds0, lds1);
-        if (t + 1 < t1) step(lds1, ST > 2 ? lds2 : lds0);
-        if (ST > 2 && t + 2 < t1) step(lds2, lds0);
+    for (int t = t0; t < t1; t += AHEAD > 2 ? 4 : 2) {
+        step(lds0, lds1, 0, ah, bh, an, bn);
+        if (t + 1 < t1) step(lds1, lds0, AHEAD > 1 ? 1 : 0, an, bn, ah, bh);
+        if (AHEAD > 2) {
+            if (t + 2 < t1) step(lds0, lds1, AHEAD - 2, ah, bh, an, bn);
+            if (t + 3 < t1) step(lds1, lds0, AHEAD - 1, an, bn, ah, bh);
+        }
     }
-    meet<0>();
+    if (t0 + p.per > whole && p.k % kBK) {
+        const int64_t k0 = (int64_t)whole * kBK;
+        const int summed = (int)(p.k - k0);
+        meet<63>();
+        sa.tail(p.A, i0, p.m, k0, summed, lds0);
+        sb.tail(p.B, j0, p.n, k0, summed, lds0 + kB);
+        meet<63>();
+        frags(lds0, 0, ah, bh);
+        frags(lds0, 1, am, bm);
+        frags(lds0, 2, al, bl);
+        multiply(ah, bl);
+        multiply(al, bh);
+        multiply(am, bm);
+        multiply(ah, bm);
+        multiply(am, bh);
+        multiply(ah, bh);
+    }
+    meet<63>();
     write_tile<SVM_F32, FM, FN>(p, acc,
                                 wave_slab<kSlab, NW, kLds>(lds0, lds1, wave),
                                 i0 + wi, j0 + wj, lane);
@@ -709,7 +841,7 @@ struct Sixteen {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = raw[u].at(e);
                 Bf16x8 part[3];
-                three_parts8(v, part);
+                three_parts(v, part);
                 h[u] = __builtin_bit_cast(short8v, part[0]);
                 m[u] = __builtin_bit_cast(short8v, part[1]);
                 l[u] = __builtin_bit_cast(short8v, part[2]);
@@ -797,10 +929,9 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(FewArgs p)
 // ---- factors that cannot be read as they are
 
 template <int DT>
-__global__ __launch_bounds__(256) void k_planes(const Elem<DT>* X, int64_t ld,
+__global__ __launch_bounds__(256) void k_padded(const Elem<DT>* X, int64_t ld,
                                                 int64_t rows, int64_t cols,
-                                                void* dst, int64_t ldp,
-                                                int64_t plane)
+                                                Elem<DT>* dst, int64_t ldp)
 {
     const int64_t groups = ldp / 8, all = rows * groups;
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < all;
@@ -809,7 +940,7 @@ __global__ __launch_bounds__(256) void k_planes(const Elem<DT>* X, int64_t ld,
         const int64_t j = (t - i * groups) * 8;
         Eight<DT> x;
         x.load(X, i * ld + j, eight_of(cols, j));
-        store_factor<DT>(x.v, dst, i * ldp + j, plane);
+        x.store(dst, i * ldp + j, 8);
     }
 }
 
@@ -836,9 +967,9 @@ template <int OT>
 void launch_product(const Args& a, int tile, hipStream_t s)
 {
     if constexpr (OT == SVM_F32) {
-        if (tile == 256) launch_tiles<OT, 128, 256, 2, 4, 2>(a, s);
-        else if (tile == 128) launch_tiles<OT, 128, 128, 2, 2, 3>(a, s);
-        else launch_tiles<OT, 64, 64, 2, 2, 3>(a, s);
+        if (tile == 256) launch_tiles<OT, 128, 256, 2, 4, 1>(a, s);
+        else if (tile == 128) launch_tiles<OT, 128, 128, 2, 2, 2>(a, s);
+        else launch_tiles<OT, 64, 64, 2, 2, 4>(a, s);
     } else {
         if (tile == 256) launch_tiles<OT, 256, 256, 2, 4, 2>(a, s);
         else if (tile == 128) launch_tiles<OT, 128, 128, 2, 2, 4>(a, s);
@@ -857,21 +988,22 @@ constexpr int kCus = 256;
 
 bool factor_fits(const svm_array& a, bool along)
 {
-    return a.dtype != SVM_F32 && ((uintptr_t)a.data & 15) == 0 &&
-           a.ld % 8 == 0 && a.ld <= kMaxWidth && (!along || a.cols % 8 == 0);
+    return a.ld <= kMaxWidth &&
+           (a.dtype == SVM_F32 ||
+            (((uintptr_t)a.data & 15) == 0 && a.ld % 8 == 0 &&
+             (!along || a.cols % 8 == 0)));
 }
 
-void launch_planes(const svm_array& a, void* dst, int64_t ldp, int64_t plane,
-                   hipStream_t s)
+void launch_padded(const svm_array& a, void* dst, int64_t ldp, hipStream_t s)
 {
     const int64_t all = a.rows * (ldp / 8);
     if (all == 0) return;
     const int64_t nb = (all + 255) / 256;
+    const dim3 grid((unsigned)(nb < 16384 ? nb : 16384)), block(256);
     for_dtype(a.dtype, [&]<int DT>() {
-        hipLaunchKernelGGL((k_planes<DT>),
-                           dim3((unsigned)(nb < 16384 ? nb : 16384)),
-                           dim3(256), 0, s, (const Elem<DT>*)a.data, a.ld,
-                           a.rows, a.cols, dst, ldp, plane);
+        hipLaunchKernelGGL((k_padded<DT>), grid, block, 0, s,
+                           (const Elem<DT>*)a.data, a.ld, a.rows, a.cols,
+                           (Elem<DT>*)dst, ldp);
     });
 }
 

@@ -7,13 +7,11 @@
 
 namespace msvm {
 
-// One factor, in a 16-bit type.  along = true: element (i, r) at
-// data[i ld + r] (the summed index along a row); else at data[r ld + i].
-// 32-bit factors come as three bf16 planes whose sum is the factor.
+// One factor.  along = true: element (i, r) at data[i ld + r] (the summed
+// index along a row); else at data[r ld + i].
 struct Factor {
     const void* data;
     int64_t ld;
-    int64_t plane;  // elements from one plane to the next
     bool along;
 };
 
@@ -28,12 +26,13 @@ struct Epilogue {
 struct Product {
     Factor A, B;
     int64_t m, n, k;
-    int32_t dtype;  // of the outputs; SVM_F32: factors in three planes
+    int32_t dtype;
     Epilogue e;
 };
 
-// Whether the product reads these values as they are: rows at multiples of
-// 16 bytes, ld at most kMaxWidth, and (along) a multiple of 8 summed values.
+// Whether the product reads these values as they are: with ld at most
+// kMaxWidth, 16-bit ones in rows at multiples of 16 bytes and (along) of a
+// multiple of 8 summed values, or with zeros up to one.
 bool factor_fits(const svm_array& a, bool along);
 
 // Queues the product; with ws.run false only counts its workspace.
@@ -45,9 +44,8 @@ bool few_rows(int64_t m, int64_t n, int64_t k);
 void few_rows_product(const svm_array& X, const svm_array& W,
                       const Epilogue& e, hipStream_t s);
 
-// Copies rows of a into dst (ldp values to a row, a multiple of 8, zeros
-// past the columns); float32 rows into three bf16 planes, `plane` apart.
-void launch_planes(const svm_array& a, void* dst, int64_t ldp, int64_t plane,
-                   hipStream_t s);
+// Copies the rows of an array into dst: ldp values to a row, a multiple of 8,
+// zeros past the columns.
+void launch_padded(const svm_array& a, void* dst, int64_t ldp, hipStream_t s);
 
 }  // namespace msvm
