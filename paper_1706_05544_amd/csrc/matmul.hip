@@ -24,6 +24,9 @@
 // consecutive columns of an output row.  The sums go through LDS once more,
 // to be finished (bias, activation, residual) and written in whole rows of
 // 16 bytes a lane from a rolled loop.
+#include <algorithm>
+#include <cmath>
+
 #include "elem.hpp"
 #include "matmul.hpp"
 
@@ -977,11 +980,6 @@ void launch_product(const Args& a, int tile, hipStream_t s)
     }
 }
 
-int64_t tiles(int64_t m, int64_t n, int bm, int bn)
-{
-    return ((m + bm - 1) / bm) * ((n + bn - 1) / bn);
-}
-
 constexpr int kCus = 256;
 
 }  // namespace
@@ -1025,6 +1023,63 @@ void few_rows_product(const svm_array& X, const svm_array& W,
     });
 }
 
+namespace {
+
+// What a block of a tile costs, measured on this card in us: a step with one
+// block to a CU, what each block more adds to a step (those that run at once
+// share the matrix cores; large tiles run one after another), and the rest of
+// a block (first loads, last writes).
+struct TileCost {
+    int tile, bm;  // columns; rows
+    double one, more, rest;
+};
+constexpr TileCost kCost16[3] = {{256, 256, 1.65, 1.65, 5.0},
+                                 {128, 128, 0.55, 0.55, 4.0},
+                                 {64, 64, 0.26, 0.19, 1.5}};
+constexpr TileCost kCost32[3] = {{256, 128, 2.50, 2.50, 10.0},
+                                 {128, 128, 1.56, 1.56, 8.0},
+                                 {64, 64, 0.65, 0.48, 2.0}};
+
+struct Choice {
+    const TileCost* t;
+    int64_t splits;
+};
+
+// The tile and the number of parts of the summed index that cost least: of a
+// product with many tiles the largest, whose factors are read least; of one
+// with few, smaller tiles or parts of the summed index keep all CUs at work
+// (8192 x 2048 over 2048, bf16: 61 us in tiles of 256, 65 in tiles of 128;
+// 2048 x 2048 over 8192 in 32 bits: 335 us in two parts, 408 in smaller
+// tiles; 6656 x 209 over 2347: 66 us in four parts, 76 in smaller tiles).
+// Parts cost a launch more, and their sums are written and read once.
+Choice choose(const Product& p, int nk)
+{
+    const TileCost* table = p.dtype == SVM_F32 ? kCost32 : kCost16;
+    Choice best{table, 1};
+    double least = 1e300;
+    for (int q = 0; q < 3; ++q) {
+        const TileCost& t = table[q];
+        const double nt = (double)((p.m + t.bm - 1) / t.bm) *
+                          (double)((p.n + t.tile - 1) / t.tile);
+        for (int64_t s = 1; s <= 64 && (s == 1 || 2 * s <= nk);
+             s += s < 4 ? 1 : s / 2) {
+            const double blocks = std::ceil(nt * (double)s / kCus);
+            const double step =
+                std::max(blocks * t.more, t.one + (blocks - 1) * 0.5 * t.more);
+            double us = (double)((nk + s - 1) / s) * step + blocks * t.rest;
+            if (s > 1)
+                us += 5.0 + (double)s * (double)p.m * (double)p.n * 8 / 3.5e6;
+            if (us < least) {
+                least = us;
+                best = {&t, s};
+            }
+        }
+    }
+    return best;
+}
+
+}  // namespace
+
 void product(const Product& p, Pieces& ws, hipStream_t s)
 {
     if (p.m == 0 || p.n == 0) return;
@@ -1038,17 +1093,9 @@ void product(const Product& p, Pieces& ws, hipStream_t s)
     const bool f32 = p.dtype == SVM_F32;
     const int bk = f32 ? kStep32 : kStep16;
     a.nk = (int)((p.k + bk - 1) / bk);
-    // Tiles: the largest of which there are enough for every CU; then, where
-    // there are still too few, the steps are split over blocks.
-    int tile = 256, bm = f32 ? 128 : 256;
-    if (tiles(p.m, p.n, bm, tile) < kCus) bm = tile = 128;
-    if (tile == 128 && tiles(p.m, p.n, 128, 128) < kCus) bm = tile = 64;
-    const int64_t nt = tiles(p.m, p.n, bm, tile);
-    int64_t splits = 1;
-    if (nt < kCus) splits = (2 * kCus) / nt;
-    if (splits > a.nk / 4) splits = a.nk / 4;
-    if (splits < 1) splits = 1;
-    a.per = (int)((a.nk + splits - 1) / splits);
+    const Choice c = choose(p, a.nk);
+    const int tile = c.t->tile, bm = c.t->bm;
+    a.per = (int)((a.nk + c.splits - 1) / c.splits);
     a.splits = (a.nk + a.per - 1) / a.per;
     a.tm = (unsigned)((p.m + bm - 1) / bm);
     a.tn = (unsigned)((p.n + tile - 1) / tile);
