@@ -620,11 +620,10 @@ struct Split {
 //   h and h' are in registers; read m and m', multiply h h';  read l and l',
 //   split the values that have come for the step after next, multiply h m',
 //   m h', m m';  meet the other waves, write those to the buffer that this
-//   step has left, load values of a later step, read the next h and h',
-//   multiply h l', l h'.
-// AHEAD: steps whose values are under way to registers.
-template <int BM, int BN, int WGM, int WGN, int AHEAD, bool AALONG,
-          bool BALONG>
+//   step has left, load the values of the step after those, read the next h
+//   and h', multiply h l', l h'.
+// (Values two or four steps ahead made no step shorter, at any tile.)
+template <int BM, int BN, int WGM, int WGN, bool AALONG, bool BALONG>
 __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
 {
     constexpr int NW = WGM * WGN, T = 64 * NW;
@@ -634,7 +633,6 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
     constexpr int kLds = 3 * (BM + BN) * kBK;   // values of a buffer
     __shared__ __align__(1024) short lds0[kLds];
     __shared__ __align__(1024) short lds1[kLds];
-    static_assert(AHEAD == 1 || AHEAD == 2 || AHEAD == 4, "ring");
 
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
@@ -657,18 +655,18 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
     SB sb;
     sa.init(p.A, i0, p.m, t0, p.k);
     sb.init(p.B, j0, p.n, t0, p.k);
-    typename SA::Raw ra[AHEAD];
-    typename SB::Raw rb[AHEAD];
+    typename SA::Raw ra;
+    typename SB::Raw rb;
     Bf16x8 pa[SA::kN][3], pb[SB::kN][3];
     int tl = t0;  // step of the next loads
-    auto load = [&](int r) {
-        sa.load(ra[r], tl < t1);
-        sb.load(rb[r], tl < t1);
+    auto load = [&]() {
+        sa.load(ra, tl < t1);
+        sb.load(rb, tl < t1);
         ++tl;
     };
-    auto split = [&](int r) {
-        SA::split(ra[r], pa);
-        SB::split(rb[r], pb);
+    auto split = [&]() {
+        SA::split(ra, pa);
+        SB::split(rb, pb);
     };
     auto write = [&](short* lds) {
         sa.write(pa, lds);
@@ -709,7 +707,7 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
         }
     };
     // ah, bh: this step's first parts, an, bn: where the next one's go
-    auto step = [&](short* cur, short* oth, int r, short8v* ah, short8v* bh,
+    auto step = [&](short* cur, short* oth, short8v* ah, short8v* bh,
                     short8v* an, short8v* bn) {
         __builtin_amdgcn_sched_barrier(0);
         frags(cur, 1, am, bm);
@@ -717,14 +715,14 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
         spread(kMul, 0);
         __builtin_amdgcn_sched_barrier(0);
         frags(cur, 2, al, bl);
-        split(r);
+        split();
         multiply(ah, bm);
         multiply(am, bh);
         multiply(am, bm);
         spread(3 * kMul, 1);
         meet<63>();
         write(cur);
-        load(r);
+        load();
         __builtin_amdgcn_sched_barrier(0);
         frags(oth, 0, an, bn);
         multiply(ah, bl);
@@ -733,23 +731,18 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    load(0);
-    split(0);
+    load();
+    split();
     write(lds0);
-    load(0);
-    split(0);
+    load();
+    split();
     write(lds1);
-#pragma unroll
-    for (int r = 0; r < AHEAD; ++r) load(r);
+    load();
     meet<63>();
     frags(lds0, 0, ah, bh);
-    for (int t = t0; t < t1; t += AHEAD > 2 ? 4 : 2) {
-        step(lds0, lds1, 0, ah, bh, an, bn);
-        if (t + 1 < t1) step(lds1, lds0, AHEAD > 1 ? 1 : 0, an, bn, ah, bh);
-        if (AHEAD > 2) {
-            if (t + 2 < t1) step(lds0, lds1, AHEAD - 2, ah, bh, an, bn);
-            if (t + 3 < t1) step(lds1, lds0, AHEAD - 1, an, bn, ah, bh);
-        }
+    for (int t = t0; t < t1; t += 2) {
+        step(lds0, lds1, ah, bh, an, bn);
+        if (t + 1 < t1) step(lds1, lds0, an, bn, ah, bh);
     }
     if (t0 + p.per > whole && p.k % kBK) {
         const int64_t k0 = (int64_t)whole * kBK;
@@ -947,36 +940,47 @@ __global__ __launch_bounds__(256) void k_padded(const Elem<DT>* X, int64_t ld,
     }
 }
 
-template <int OT, int BM, int BN, int WGM, int WGN, int ST>
-void launch_tiles(const Args& a, hipStream_t s)
+// launch(AALONG, BALONG) for the ways that the factors of a product lie.
+template <class F>
+void for_factors(const Args& a, F&& launch)
 {
-    const dim3 grid(a.tm * a.tn, (unsigned)a.splits), block(64 * WGM * WGN);
-    auto go = [&]<bool AALONG, bool BALONG>() {
-        if constexpr (OT == SVM_F32)
-            hipLaunchKernelGGL(
-                (k_product32<BM, BN, WGM, WGN, ST, AALONG, BALONG>), grid,
-                block, 0, s, a);
-        else
-            hipLaunchKernelGGL(
-                (k_product<OT, BM, BN, WGM, WGN, ST, AALONG, BALONG>), grid,
-                block, 0, s, a);
-    };
-    if (a.A.along && a.B.along) go.template operator()<true, true>();
-    else if (a.A.along) go.template operator()<true, false>();
-    else go.template operator()<false, false>();
+    if (a.A.along && a.B.along) launch.template operator()<true, true>();
+    else if (a.A.along) launch.template operator()<true, false>();
+    else launch.template operator()<false, false>();
+}
+
+template <int OT, int BM, int BN, int WGM, int WGN, int ST>
+void launch16(const Args& a, hipStream_t s)
+{
+    for_factors(a, [&]<bool AALONG, bool BALONG>() {
+        hipLaunchKernelGGL(
+            (k_product<OT, BM, BN, WGM, WGN, ST, AALONG, BALONG>),
+            dim3(a.tm * a.tn, (unsigned)a.splits), dim3(64 * WGM * WGN), 0, s,
+            a);
+    });
+}
+
+template <int BM, int BN, int WGM, int WGN>
+void launch32(const Args& a, hipStream_t s)
+{
+    for_factors(a, [&]<bool AALONG, bool BALONG>() {
+        hipLaunchKernelGGL((k_product32<BM, BN, WGM, WGN, AALONG, BALONG>),
+                           dim3(a.tm * a.tn, (unsigned)a.splits),
+                           dim3(64 * WGM * WGN), 0, s, a);
+    });
 }
 
 template <int OT>
 void launch_product(const Args& a, int tile, hipStream_t s)
 {
     if constexpr (OT == SVM_F32) {
-        if (tile == 256) launch_tiles<OT, 128, 256, 2, 4, 1>(a, s);
-        else if (tile == 128) launch_tiles<OT, 128, 128, 2, 2, 2>(a, s);
-        else launch_tiles<OT, 64, 64, 2, 2, 4>(a, s);
+        if (tile == 256) launch32<128, 256, 2, 4>(a, s);
+        else if (tile == 128) launch32<128, 128, 2, 4>(a, s);
+        else launch32<64, 64, 2, 2>(a, s);
     } else {
-        if (tile == 256) launch_tiles<OT, 256, 256, 2, 4, 2>(a, s);
-        else if (tile == 128) launch_tiles<OT, 128, 128, 2, 2, 4>(a, s);
-        else launch_tiles<OT, 64, 64, 2, 2, 4>(a, s);
+        if (tile == 256) launch16<OT, 256, 256, 2, 4, 2>(a, s);
+        else if (tile == 128) launch16<OT, 128, 128, 2, 2, 4>(a, s);
+        else launch16<OT, 64, 64, 2, 2, 4>(a, s);
     }
 }
 
@@ -1037,7 +1041,7 @@ constexpr TileCost kCost16[3] = {{256, 256, 1.65, 1.65, 5.0},
                                  {128, 128, 0.55, 0.55, 4.0},
                                  {64, 64, 0.26, 0.19, 1.5}};
 constexpr TileCost kCost32[3] = {{256, 128, 2.50, 2.50, 10.0},
-                                 {128, 128, 1.56, 1.56, 8.0},
+                                 {128, 128, 1.45, 1.42, 7.0},
                                  {64, 64, 0.65, 0.48, 2.0}};
 
 struct Choice {
