@@ -16,7 +16,8 @@ struct GradArgs {
     int64_t ldg, ldz, m, n, rows;  // rows of a block
     void* dZ;
     int64_t ldd;
-    float* part;
+    float* part;  // the blocks' sums,
+    void* sums;   // or the sums themselves, where one block has all rows
     int act;
 };
 
@@ -47,7 +48,7 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs p)
             if (p.dZ) g.store(p.dZ, i * p.ldd + j, 8);
         }
     }
-    if (!p.part) return;
+    if (!p.sums) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) red[ty][tx * 8 + e] = sum[e];
     __syncthreads();
@@ -56,12 +57,15 @@ __global__ __launch_bounds__(256) void k_act_grad(GradArgs p)
     float s = 0.0f;
 #pragma unroll
     for (int r = 0; r < kGradLanes; ++r) s += red[r][threadIdx.x];
-    p.part[blockIdx.y * p.n + c] = s;
+    if (gridDim.y == 1) ((Elem<DT>*)p.sums)[c] = (Elem<DT>)s;
+    else p.part[blockIdx.y * p.n + c] = s;
 }
 
-// Rows of a block: some 2048 blocks in all, at least 16 rows to one.
+// Rows of a block: some 2048 blocks in all, at least 16 rows to one; up to 64
+// rows are left to one block, which spares the launch that joins the sums.
 int64_t grad_rows(int64_t m, int64_t n)
 {
+    if (m <= 64) return 64;
     const int64_t across = (n + kGradCols - 1) / kGradCols;
     int64_t rows = (m * across + 2047) / 2048;
     rows = (rows + kGradLanes - 1) / kGradLanes * kGradLanes;
@@ -185,21 +189,21 @@ void linear_backward(const LinearGradArgs& a, Pieces& ws, hipStream_t s)
         dz.data = ws.take<char>(m * dz.ld * dtype_bytes(t));
     }
     const int64_t rows = grad_rows(m, n), np = (m + rows - 1) / rows;
-    float* part = db ? ws.take<float>(np * n) : nullptr;
+    float* part = db && np > 1 ? ws.take<float>(np * n) : nullptr;
     if (ws.run && m > 0 && (copy || db)) {
         GradArgs g{a.dY.data, slope ? a.Z.data : nullptr,
                    a.dY.ld,   a.Z.ld,
                    m,         n,
                    rows,      copy ? const_cast<void*>(dz.data) : nullptr,
                    dz.ld,     part,
-                   a.act};
+                   a.dbias.data, a.act};
         const dim3 grid((unsigned)((n + kGradCols - 1) / kGradCols),
                         (unsigned)np);
         for_dtype(t, [&]<int DT>() {
             hipLaunchKernelGGL((k_act_grad<DT>), grid, dim3(256), 0, s, g);
         });
     }
-    if (ws.run && db)
+    if (ws.run && db && np != 1)
         launch_column_sums(part, nullptr, np, n, t, a.dbias.data, nullptr, s);
     if (!dx && !dw) return;
     if (m == 0) {

@@ -804,11 +804,15 @@ def svm_adamw_parts(params):
     """Where each tensor's states begin in the flat states of
     svm_adamw_step, and their total length: the tensors follow one another,
     each from a multiple of SVM_ADAMW_BLOCK."""
-    at, total = [], 0
-    for p in params:
-        at.append(total)
-        total += -(-p.numel() // SVM_ADAMW_BLOCK) * SVM_ADAMW_BLOCK
-    return np.array(at, dtype=np.int64), total
+    return _parts_of([p.numel() for p in params])
+
+
+def _parts_of(sizes):
+    ends = np.cumsum(-(-np.array(sizes, dtype=np.int64) // SVM_ADAMW_BLOCK)
+                     * SVM_ADAMW_BLOCK)
+    at = np.zeros(len(sizes), dtype=np.int64)
+    at[1:] = ends[:-1]
+    return at, int(ends[-1]) if len(ends) else 0
 
 
 def svm_adamw_states(params, bits: int = 32, master: bool = False):
@@ -854,7 +858,8 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
         return
     lib = load()
     c = _Call(params[0], stream)
-    at, total = svm_adamw_parts(params)
+    sizes = [p.numel() for p in params]
+    at, total = _parts_of(sizes)
     bits = 8 if m.dtype == torch.int8 else 32
     want = [("m", m, torch.int8 if bits == 8 else torch.float32, total),
             ("v", v, torch.uint8 if bits == 8 else torch.float32, total)]
@@ -871,13 +876,15 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
                            "of %d values on the parameters' device"
                            % (what, dtype, n))
         c.keep.append(t)
-    if not all(p.is_contiguous() for p in params) or \
-            [p.shape for p in params] != [g.shape for g in grads]:
+    T = torch.Tensor
+    if not all(map(T.is_contiguous, params)) or \
+            not all(map(T.is_same_size, params, grads)):
         raise SvmError(SVM_E_INVALID, "parameters must be contiguous, "
                        "gradients of their shapes")
-    grads = [g if g.is_contiguous() else g.contiguous() for g in grads]
-    if {t.get_device() for t in params} | {t.get_device() for t in grads} \
-            != {c.index}:
+    if not all(map(T.is_contiguous, grads)):
+        grads = [g.contiguous() for g in grads]
+    if set(map(T.get_device, params)) | set(map(T.get_device, grads)) != \
+            {c.index}:
         raise SvmError(SVM_E_INVALID, "the tensors are on several devices")
     pd = [_DTYPES.get(p.dtype) for p in params]
     gd = [_DTYPES.get(g.dtype) for g in grads]
@@ -887,9 +894,9 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
     c.keep += params
     c.keep += grads
     tab = np.zeros(len(params), dtype=_ADAMW_ROW)
-    tab["param"] = [p.data_ptr() for p in params]
-    tab["grad"] = [g.data_ptr() for g in grads]
-    tab["n"] = [p.numel() for p in params]
+    tab["param"] = list(map(T.data_ptr, params))
+    tab["grad"] = list(map(T.data_ptr, grads))
+    tab["n"] = sizes
     tab["dtype"], tab["grad_dtype"] = pd, gd
     esize = 1 if bits == 8 else 4
     tab["m"], tab["v"] = m.data_ptr() + at * esize, v.data_ptr() + at * esize

@@ -118,7 +118,9 @@ def backward(dY=_SAME, X=_SAME, W=_SAME, Z=None, act=0, dX=_SAME, dW=_SAME,
     dict(dX=arr(6, 4, at=2 << 20)), dict(dW=arr(5, 4, at=3 << 20)),
     dict(db=arr(1, 5)), dict(dX=arr(6, 4, at=5 << 20)),
     dict(dW=arr(5, 4, at=5 << 20, dtype=1)),
-    dict(work=None, nbytes=0), dict(nbytes=8)])
+    # (with an activation dZ needs a workspace)
+    dict(act=1, Z=arr(6, 5, at=7 << 20), work=None, nbytes=0),
+    dict(act=1, Z=arr(6, 5, at=7 << 20), nbytes=8)])
 def test_linear_backward_refusals(kw):
     assert backward(**kw) == INV
     assert nv.svm_last_error()
