@@ -1101,13 +1101,28 @@ void product(const Product& p, Pieces& ws, hipStream_t s)
     const int tile = c.t->tile, bm = c.t->bm;
     a.per = (int)((a.nk + c.splits - 1) / c.splits);
     a.splits = (a.nk + a.per - 1) / a.per;
-    a.tm = (unsigned)((p.m + bm - 1) / bm);
     a.tn = (unsigned)((p.n + tile - 1) / tile);
     if (a.splits > 1) a.part = ws.take<float>(a.splits * p.m * p.n);
     if (!ws.run) return;
-    if (f32) launch_product<SVM_F32>(a, tile, s);
-    else if (p.dtype == SVM_BF16) launch_product<SVM_BF16>(a, tile, s);
-    else launch_product<SVM_F16>(a, tile, s);
+    // A launch has fewer than 2^32 threads: rows in slices of at most 2^22
+    // tiles (more than one slice of them is never split).
+    const int64_t slice = std::max<int64_t>((1 << 22) / a.tn, 1) * bm;
+    for (int64_t i0 = 0; i0 < p.m; i0 += slice) {
+        Args q = a;
+        const int64_t eb = (int64_t)dtype_bytes(p.dtype);
+        q.m = std::min(p.m - i0, slice);
+        q.tm = (unsigned)((q.m + bm - 1) / bm);
+        auto on = [&](const void* x, int64_t ld) {
+            return x ? (const char*)x + i0 * ld * eb : nullptr;
+        };
+        q.A.data = on(a.A.data, a.A.along ? a.A.ld : 1);
+        q.e.Y = (void*)on(a.e.Y, a.e.ldy);
+        q.e.Z = (void*)on(a.e.Z, a.e.ldz);
+        q.e.residual = on(a.e.residual, a.e.ldr);
+        if (f32) launch_product<SVM_F32>(q, tile, s);
+        else if (p.dtype == SVM_BF16) launch_product<SVM_BF16>(q, tile, s);
+        else launch_product<SVM_F16>(q, tile, s);
+    }
     if (a.splits > 1) {
         const int64_t nb = (p.m * ((p.n + 7) / 8) + 255) / 256;
         for_dtype(p.dtype, [&]<int DT>() {

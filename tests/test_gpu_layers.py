@@ -337,6 +337,20 @@ def test_linear_offsets_past_32_bits(t):
     assert bool((db == 3.0).all())
 
 
+def test_linear_more_rows_than_a_launch_has_threads_for():
+    # 1.1e9 rows: 2^32 threads would not cover them in tiles of any size
+    m = 1100000001
+    X = torch.ones(m, 1, dtype=torch.bfloat16, device=DEV)
+    X[-1] = 3.0
+    X[1 << 30] = 5.0
+    W = torch.tensor([[2.0]], dtype=torch.bfloat16, device=DEV)
+    Y = nv.svm_linear(X, W)
+    at = torch.tensor([0, 268435455, 268435456, 1 << 30, m - 2, m - 1],
+                      device=DEV)
+    assert Y[at, 0].tolist() == [2.0, 2.0, 2.0, 10.0, 2.0, 6.0]
+    assert int((Y != 2.0).sum()) == 2
+
+
 # ------------------------------------------------------------- layer norm
 
 
