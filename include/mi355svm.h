@@ -388,7 +388,7 @@ typedef enum {
                            N(0, 2 gamma I), bias from U[0, 2 pi) and n
                            features, (2/n) phi(u).phi(v) tends to the RBF
                            kernel (train with SVM_KERNEL_POLY, degree 1,
-                           gamma = 2/n) */
+                           gamma = 2/n).  Angles up to 1e8 in magnitude */
 } svm_act;
 
 /* One layer: Z = X W^T + bias, Y = act(Z) + residual.

@@ -64,18 +64,35 @@ __device__ __forceinline__ void adam_value(const AdamConst& k, float g,
     p = p * k.keep - k.rate * (fabsf(q) <= 3.402823466e38f ? q : m / d);
 }
 
-// The code of x (magnitude a) in a block with `by` = steps^2 / largest.
-__device__ __forceinline__ int encode8(float x, float by, bool live, int steps,
-                                       int bad, bool least_one)
+// The codes of four values in a block with `by` = steps^2 / largest:
+// sqrt(|x| by) to the nearest whole number, ties to even.  The hardware's
+// square root is good to a unit of its last place, below 2e-5 here: only
+// where it comes within 1e-4 of a tie is the correctly rounded one needed.
+template <bool SIGNED>
+__device__ __forceinline__ void encode8(const floatx4& x, float by, bool live,
+                                        int (&code)[4])
 {
 #pragma clang fp contract(off)
-    const float a = fabsf(x);
-    if (!(a <= 3.402823466e38f)) return bad;
-    if (!live) return 0;
-    int c = (int)rintf(sqrtf(a * by));
-    c = c < steps ? c : steps;
-    if (least_one && a > 0.0f && c < 1) c = 1;
-    return x < 0.0f ? -c : c;
+    constexpr int kSteps = SIGNED ? 127 : 254, kBad = SIGNED ? -128 : 255;
+    float y[4], near = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        y[e] = __builtin_amdgcn_sqrtf(fabsf(x[e]) * by);
+        near = fmaxf(near, fabsf(y[e] - rintf(y[e])));
+    }
+    if (near > 0.4999f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = sqrtf(fabsf(x[e]) * by);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float a = fabsf(x[e]);
+        int c = (int)fminf(rintf(y[e]), (float)kSteps);
+        if (!SIGNED && a > 0.0f && c < 1) c = 1;
+        if (!live) c = 0;
+        c = SIGNED && x[e] < 0.0f ? -c : c;
+        code[e] = a <= 3.402823466e38f ? c : kBad;
+    }
 }
 
 // Four consecutive values: 4 times their size at once where all are there.
@@ -180,11 +197,11 @@ __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
         const float br = lr ? 64516.0f / tr : 0.0f;
         Four<int8_t>::Wide cm;
         Four<uint8_t>::Wide cv;
+        int im[4], iv[4];
+        encode8<true>(m, bm, lm, im);
+        encode8<false>(r, br, lr, iv);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            cm[e] = (int8_t)encode8(m[e], bm, lm, 127, -128, false);
-            cv[e] = (uint8_t)encode8(r[e], br, lr, 254, 255, true);
-        }
+        for (int e = 0; e < 4; ++e) cm[e] = (int8_t)im[e], cv[e] = (uint8_t)iv[e];
         *(Four<int8_t>::Wide*)((int8_t*)t.m[lo] + at) = cm;
         *(Four<uint8_t>::Wide*)((uint8_t*)t.v[lo] + at) = cv;
         if (lane == 0) {

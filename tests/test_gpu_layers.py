@@ -288,6 +288,37 @@ def test_linear_not_finite_stays_in_its_row(m, t):
     close(torch.where(fine, Y, 0), torch.where(fine, y, 0), ty, t)
 
 
+@pytest.mark.parametrize("m", [11, 66])  # few rows, and tiles
+@pytest.mark.parametrize("act", ACTS)
+def test_activations_at_the_ends_of_the_range(act, m):
+    inf = float("inf")
+    vals = [0.0, -0.0, 1e-30, -1e-30, 0.2, 30.0, -30.0, 88.0, -88.0, 1e4,
+            -1e4] + [inf, -inf, float("nan"), 1e30, -1e30] * (m > 16)
+    z = torch.tensor(vals, device=DEV)[:, None]
+    X = torch.cat([z, torch.zeros(m - len(vals), 1, device=DEV)])
+    W = torch.ones(3, 1, device=DEV)
+    Y, Z = nv.svm_linear(X, W, act=act, save=True)
+    assert torch.equal(torch.nan_to_num(Z, 7.0),
+                       torch.nan_to_num(X.expand(m, 3), 7.0))
+    G = torch.ones(m, 3, device=DEV)
+    dX = nv.svm_linear_backward(G, X, W, Z, act=act,
+                                need=(True, False, False))[0]
+    x = X.double()
+    y, d = act64(act, x)
+    if act == "cos":  # angles past 1e8 are left open
+        y, d = (torch.where(x.abs() > 1e8, 0, v) for v in (y, d))
+        Y, dX = (torch.where(X.abs() > 1e8, 0, v) for v in (Y, dX))
+    # (gelu and silu at -inf, and their slopes at both ends, are products of
+    # an infinity with 0: NaN, as the formulas in 32 bits are)
+    near = 4 * E * (1 + torch.nan_to_num(x, 0, 0, 0).clamp(-40, 40) ** 2
+                    + torch.nan_to_num(y.abs(), 0, 0, 0))
+    for got, want, tol in ((Y[:, :1], y, near), (dX, 3 * d, 8 * near)):
+        fine = torch.isfinite(want)
+        assert torch.equal(torch.isfinite(got), fine), (got, want)
+        close(torch.where(fine, got, 0), torch.where(fine, want, 0),
+              torch.where(fine, tol, 1), "f32")
+
+
 def test_linear_32_bit_range():
     # factors near the ends of the 32-bit range: products that are fine stay
     # exact to 32 bits
