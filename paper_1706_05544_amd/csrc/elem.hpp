@@ -264,7 +264,7 @@ __device__ __forceinline__ float act_value(int act, float z)
 __device__ __forceinline__ float act_slope(int act, float z)
 {
     switch (act) {
-    case SVM_ACT_RELU: return z > 0.0f ? 1.0f : (z != z ? z : 0.0f);
+    case SVM_ACT_RELU: return z > 0.0f ? 1.0f : 0.0f;
     case SVM_ACT_GELU: {
         float e;
         const float q = upper_tail(z, e);
