@@ -594,25 +594,34 @@ class _Call:
         where it is an input that has none."""
         if t is None:
             return None
-        d = _DTYPES.get(getattr(t, "dtype", None)) if _is_torch(t) else None
-        if d is None or t.get_device() < 0:
-            raise SvmError(SVM_E_UNSUPPORTED, "%s must be a float32, bfloat16 "
-                           "or float16 tensor in device memory" % what)
-        if t.get_device() != self.index:
-            raise SvmError(SVM_E_INVALID, "%s is on another device" % what)
-        r = _rows_of(t)
-        if r is None:
-            if out:
-                raise SvmError(SVM_E_INVALID, "%s: its rows must be at one "
-                               "stride, the values of a row side by side"
+        try:
+            d, index = _DTYPES[t.dtype], t.get_device()
+        except (AttributeError, KeyError, TypeError):
+            d, index = None, -1
+        if index != self.index:
+            if index < 0:
+                raise SvmError(SVM_E_UNSUPPORTED, "%s must be a float32, "
+                               "bfloat16 or float16 tensor in device memory"
                                % what)
-            t = t.contiguous()
+            raise SvmError(SVM_E_INVALID, "%s is on another device" % what)
+        if t.is_contiguous() and t.numel() and t.dim():
+            cols = ld = t.shape[-1]
+            rows = t.numel() // cols
+        else:
             r = _rows_of(t)
             if r is None:
-                raise SvmError(SVM_E_INVALID, "%s must have a dimension"
-                               % what)
+                if out:
+                    raise SvmError(SVM_E_INVALID, "%s: its rows must be at "
+                                   "one stride, the values of a row side by "
+                                   "side" % what)
+                t = t.contiguous()
+                r = _rows_of(t)
+                if r is None:
+                    raise SvmError(SVM_E_INVALID, "%s must have a dimension"
+                                   % what)
+            rows, cols, ld = r
         self.keep.append(t)
-        return svm_array(t.data_ptr(), r[0], r[1], r[2], d, 1)
+        return svm_array(t.data_ptr(), rows, cols, ld, d, 1)
 
     def floats(self, t, rows: int, what: str) -> int:
         """Address of a float32 value for each row."""
@@ -673,8 +682,8 @@ def svm_linear(X, W, bias=None, residual=None, act="none", save: bool = False,
     c = _Call(X, stream)
     a, w = c.arr(X, "X"), c.arr(W, "W")
     shape = X.shape[:-1] + (w.rows,)
-    Y = out if out is not None else c.empty(shape, X.dtype)
-    Z = c.empty(shape, X.dtype) if save else None
+    Y = out if out is not None else X.new_empty(shape)
+    Z = X.new_empty(shape) if save else None
     need = ct.c_int64()
     _check(lib.svm_linear_workspace(ct.byref(a), ct.byref(w),
                                     ct.byref(need)))
@@ -697,9 +706,9 @@ def svm_linear_backward(dY, X, W, Z=None, act="none", need=(True, True, True),
     lib = load()
     c = _Call(dY, stream)
     g, a, w = c.arr(dY, "dY"), c.arr(X, "X"), c.arr(W, "W")
-    dX = c.empty(X.shape, dY.dtype) if need[0] else None
-    dW = c.empty(W.shape, dY.dtype) if need[1] else None
-    db = c.empty((g.cols,), dY.dtype) if need[2] else None
+    dX = dY.new_empty(X.shape) if need[0] else None
+    dW = dY.new_empty(W.shape) if need[1] else None
+    db = dY.new_empty(g.cols) if need[2] else None
     rx, rw, rb = (c.arr(dX, "dX", True), c.arr(dW, "dW", True),
                   c.arr(db, "dbias", True))
     size = ct.c_int64()
@@ -725,7 +734,7 @@ def svm_layer_norm(X, weight=None, bias=None, eps: float = 1e-5,
     lib = load()
     c = _Call(X, stream)
     a = c.arr(X, "X")
-    Y = out if out is not None else c.empty(X.shape, X.dtype)
+    Y = out if out is not None else X.new_empty(X.shape)
     mean = c.empty(X.shape[:-1], torch.float32) if save else None
     rstd = c.empty(X.shape[:-1], torch.float32) if save else None
     w, b = c.arr(weight, "weight"), c.arr(bias, "bias")
@@ -747,9 +756,9 @@ def svm_layer_norm_backward(dY, X, mean, rstd, weight=None, residual=None,
     g, a = c.arr(dY, "dY"), c.arr(X, "X")
     mp = c.floats(mean, g.rows, "mean")
     rp = c.floats(rstd, g.rows, "rstd")
-    dX = c.empty(X.shape, dY.dtype) if need[0] else None
-    dw = c.empty((g.cols,), dY.dtype) if need[1] else None
-    db = c.empty((g.cols,), dY.dtype) if need[2] else None
+    dX = dY.new_empty(X.shape) if need[0] else None
+    dw = dY.new_empty(g.cols) if need[1] else None
+    db = dY.new_empty(g.cols) if need[2] else None
     size = ct.c_int64()
     if need[1] or need[2]:
         _check(lib.svm_layer_norm_backward_workspace(g.rows, g.cols,
@@ -786,7 +795,7 @@ def svm_hinge_loss(S, labels, scale: Optional[float] = None,
     labels = labels.contiguous()
     c.keep.append(labels)
     loss = c.empty((), torch.float32)
-    dS = c.empty(S.shape, S.dtype) if need_grad else None
+    dS = S.new_empty(S.shape) if need_grad else None
     size = ct.c_int64()
     _check(lib.svm_hinge_loss_workspace(a.rows, a.cols, ct.byref(size)))
     ws = c.work(size.value)
@@ -808,11 +817,11 @@ def svm_adamw_parts(params):
 
 
 def _parts_of(sizes):
-    ends = np.cumsum(-(-np.array(sizes, dtype=np.int64) // SVM_ADAMW_BLOCK)
-                     * SVM_ADAMW_BLOCK)
-    at = np.zeros(len(sizes), dtype=np.int64)
-    at[1:] = ends[:-1]
-    return at, int(ends[-1]) if len(ends) else 0
+    at, total = [], 0
+    for n in sizes:
+        at.append(total)
+        total += -(-n // SVM_ADAMW_BLOCK) * SVM_ADAMW_BLOCK
+    return np.array(at, dtype=np.int64), total
 
 
 def svm_adamw_states(params, bits: int = 32, master: bool = False):
