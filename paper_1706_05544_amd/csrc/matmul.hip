@@ -949,13 +949,15 @@ void for_factors(const Args& a, F&& launch)
     else launch.template operator()<false, false>();
 }
 
-template <int OT, int BM, int BN, int WGM, int WGN, int ST>
+// WGX: waves across a tile where both factors lie across the summed index.
+template <int OT, int BM, int BN, int WGM, int WGN, int WGX, int ST>
 void launch16(const Args& a, hipStream_t s)
 {
     for_factors(a, [&]<bool AALONG, bool BALONG>() {
+        constexpr int kWgn = AALONG || BALONG ? WGN : WGX;
         hipLaunchKernelGGL(
-            (k_product<OT, BM, BN, WGM, WGN, ST, AALONG, BALONG>),
-            dim3(a.tm * a.tn, (unsigned)a.splits), dim3(64 * WGM * WGN), 0, s,
+            (k_product<OT, BM, BN, WGM, kWgn, ST, AALONG, BALONG>),
+            dim3(a.tm * a.tn, (unsigned)a.splits), dim3(64 * WGM * kWgn), 0, s,
             a);
     });
 }
@@ -978,9 +980,14 @@ void launch_product(const Args& a, int tile, hipStream_t s)
         else if (tile == 128) launch32<128, 128, 2, 4>(a, s);
         else launch32<64, 64, 2, 2>(a, s);
     } else {
-        if (tile == 256) launch16<OT, 256, 256, 2, 4, 2>(a, s);
-        else if (tile == 128) launch16<OT, 128, 128, 2, 2, 4>(a, s);
-        else launch16<OT, 64, 64, 2, 2, 4>(a, s);
+        // Tiles of 128: eight waves, two to a SIMD, each of which waits while
+        // the other multiplies (4096 x 1024 over 1024: 15.0 us, with four
+        // waves 16.3); where both factors lie across, the reads of eight
+        // waves' fragments cost more than that gains (2048 x 2048 over 8192:
+        // 92 us with eight, 87 with four).
+        if (tile == 256) launch16<OT, 256, 256, 2, 4, 4, 2>(a, s);
+        else if (tile == 128) launch16<OT, 128, 128, 2, 4, 2, 4>(a, s);
+        else launch16<OT, 64, 64, 2, 2, 2, 4>(a, s);
     }
 }
 
