@@ -45,53 +45,85 @@ __device__ __forceinline__ float decode8(int c, float scale, int steps)
     return (t * fabsf(t)) * scale;
 }
 
-// One step of one value.  Not contracted, so that the states are the same
-// wherever they are computed.
-__device__ __forceinline__ void adam_value(const AdamConst& k, float g,
-                                           float& p, float& m, float& v,
-                                           float& r)
+constexpr float kMost = 3.402823466e38f;
+
+// One step of four values; r: about sqrt(v).  Not contracted, so that the
+// states are the same wherever they are computed.  They are the definition's
+// bit for bit; the weight's step is good to a few units of the quotient's last
+// place (square root and reciprocal are the hardware's, each good to a unit).
+__device__ __forceinline__ void adam_step(const AdamConst& k, const floatx4& g0,
+                                          floatx4& p, floatx4& m, floatx4& v,
+                                          floatx4& r)
 {
 #pragma clang fp contract(off)
-    g = g * k.gscale;
-    m = m * k.b1 + g * k.c1;
-    v = v * k.b2 + (g * g) * k.c2;
-    r = sqrtf(v);
-    // (the states above are the definition's bit for bit; the weight's step
-    // is good to a few units of the quotient's last place)
-    const float d = r * k.root + k.eps;
-    float q = m * __builtin_amdgcn_rcpf(d);
-    q = fmaf(fmaf(-d, q, m), __builtin_amdgcn_rcpf(d), q);
-    p = p * k.keep - k.rate * (fabsf(q) <= 3.402823466e38f ? q : m / d);
+    bool small = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float g = g0[e] * k.gscale;
+        m[e] = m[e] * k.b1 + g * k.c1;
+        v[e] = v[e] * k.b2 + (g * g) * k.c2;
+        const float ve = v[e];
+        r[e] = __builtin_amdgcn_sqrtf(ve);
+        small |= __builtin_amdgcn_classf(ve, 0x80);  // subnormal
+    }
+    if (small) {  // (the hardware's square root takes them for 0)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r[e] = sqrtf(v[e]);
+    }
+    float q[4], d[4];
+    bool far = false;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        d[e] = r[e] * k.root + k.eps;
+        const float i = __builtin_amdgcn_rcpf(d[e]);
+        q[e] = m[e] * i;
+        q[e] = fmaf(fmaf(-d[e], q[e], m[e]), i, q[e]);
+        far |= !(fabsf(q[e]) <= kMost);
+    }
+    if (far) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (!(fabsf(q[e]) <= kMost)) q[e] = m[e] / d[e];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) p[e] = p[e] * k.keep - k.rate * q[e];
 }
 
-// The codes of four values in a block with `by` = steps^2 / largest:
-// sqrt(|x| by) to the nearest whole number, ties to even.  The hardware's
-// square root is good to a unit of its last place, below 2e-5 here: only
-// where it comes within 1e-4 of a tie is the correctly rounded one needed.
-template <bool SIGNED>
-__device__ __forceinline__ void encode8(const floatx4& x, float by, bool live,
-                                        int (&code)[4])
+// The codes of four values x (ROOT: of their square roots, r about those) in
+// a block with `by` = steps^2 / largest: sqrt(|x| by) to the nearest whole
+// number, ties to even.  The hardware's square root is good to a unit of its
+// last place, so y to 2e-5, and to 8e-5 where r is one too: only where y comes
+// within 2e-4 of a tie are the correctly rounded ones needed.
+template <bool ROOT>
+__device__ __forceinline__ void encode8(const floatx4& x, const floatx4& r,
+                                        float by, bool live, int (&code)[4])
 {
 #pragma clang fp contract(off)
-    constexpr int kSteps = SIGNED ? 127 : 254, kBad = SIGNED ? -128 : 255;
+    constexpr int kSteps = ROOT ? 254 : 127, kBad = ROOT ? 255 : -128;
     float y[4], near = 0.0f;
+    bool odd = false;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        y[e] = __builtin_amdgcn_sqrtf(fabsf(x[e]) * by);
+        y[e] = __builtin_amdgcn_sqrtf((ROOT ? r[e] : fabsf(x[e])) * by);
         near = fmaxf(near, fabsf(y[e] - rintf(y[e])));
+        odd |= !(fabsf(x[e]) <= kMost);
     }
-    if (near > 0.4999f) {
+    if (near > 0.4998f) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = sqrtf(fabsf(x[e]) * by);
+        for (int e = 0; e < 4; ++e)
+            y[e] = sqrtf((ROOT ? sqrtf(x[e]) : fabsf(x[e])) * by);
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const float a = fabsf(x[e]);
-        int c = (int)fminf(rintf(y[e]), (float)kSteps);
-        if (!SIGNED && a > 0.0f && c < 1) c = 1;
-        if (!live) c = 0;
-        c = SIGNED && x[e] < 0.0f ? -c : c;
-        code[e] = a <= 3.402823466e38f ? c : kBad;
+        float c = fminf(rintf(y[e]), (float)kSteps);
+        if (ROOT) c = fmaxf(c, live && x[e] > 0.0f ? 1.0f : 0.0f);
+        else c = copysignf(c, x[e]);
+        code[e] = (int)c;
+    }
+    if (odd) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (!(fabsf(x[e]) <= kMost)) code[e] = kBad;
     }
 }
 
@@ -171,35 +203,35 @@ __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
         m = *(const floatx4*)((const float*)t.m[lo] + at);
         v = *(const floatx4*)((const float*)t.v[lo] + at);
     }
+    floatx4 g4;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        float pe = p[e], me = m[e], ve = v[e], re;
-        adam_value(k, (float)g[e], pe, me, ve, re);
-        p[e] = pe, m[e] = me, v[e] = ve, r[e] = re;
-    }
+    for (int e = 0; e < 4; ++e) g4[e] = (float)g[e];
+    adam_step(k, g4, p, m, v, r);
     if (MASTER) *(floatx4*)(master + at) = p;
     typename Four<P>::Wide out;
 #pragma unroll
     for (int e = 0; e < 4; ++e) out[e] = (P)p[e];
     Four<P>::store(param, at, left, out);
     if (BITS == 8) {
-        float tm = 0.0f, tr = 0.0f;
+        // (the rounded square root is monotone: that of the largest value is
+        // the largest of them)
+        float tm = 0.0f, tv = 0.0f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float am = fabsf(m[e]);
-            if (am <= 3.402823466e38f) tm = fmaxf(tm, am);
-            if (r[e] <= 3.402823466e38f) tr = fmaxf(tr, r[e]);
+            tm = fmaxf(tm, am <= kMost ? am : 0.0f);
+            tv = fmaxf(tv, v[e] <= kMost ? v[e] : 0.0f);
         }
         tm = wave_max(tm);
-        tr = wave_max(tr);
+        const float tr = sqrtf(wave_max(tv));
         const bool lm = tm > kTiny, lr = tr > kTiny;
         const float bm = lm ? 16129.0f / tm : 0.0f;
         const float br = lr ? 64516.0f / tr : 0.0f;
         Four<int8_t>::Wide cm;
         Four<uint8_t>::Wide cv;
         int im[4], iv[4];
-        encode8<true>(m, bm, lm, im);
-        encode8<false>(r, br, lr, iv);
+        encode8<false>(m, r, bm, lm, im);
+        encode8<true>(v, r, br, lr, iv);
 #pragma unroll
         for (int e = 0; e < 4; ++e) cm[e] = (int8_t)im[e], cv[e] = (uint8_t)iv[e];
         *(Four<int8_t>::Wide*)((int8_t*)t.m[lo] + at) = cm;
