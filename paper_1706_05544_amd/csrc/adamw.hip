@@ -1,5 +1,6 @@
 // One AdamW step over many tensors, states in 32 bits or in 8.
 #include <cmath>
+#include <type_traits>
 
 #include "elem.hpp"
 #include "layers.hpp"
@@ -246,32 +247,46 @@ __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
     }
 }
 
-// Four values to a thread.
+// Four values to a thread in each of kTurns turns, whose codes are all loaded
+// before the first is decoded.
+constexpr int kTurns = 4;
+
+template <int STEPS>
+__device__ __forceinline__ void decode_turns(
+    const std::conditional_t<STEPS == 127, int8_t, uint8_t>* code,
+    const float* scale, int64_t at, int64_t n, float* out)
+{
+    using F = Four<std::conditional_t<STEPS == 127, int8_t, uint8_t>>;
+    typename F::Wide c[kTurns];
+    float s[kTurns];
+    int left[kTurns];
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+        const int64_t i = at + t * 1024, more = n - i;
+        left[t] = more >= 4 ? 4 : more > 0 ? (int)more : 0;
+        c[t] = F::load(code, i, left[t]);
+        s[t] = more > 0 ? scale[i / kAdamBlock] : 0.0f;
+    }
+#pragma unroll
+    for (int t = 0; t < kTurns; ++t) {
+        Four<float>::Wide x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float r = decode8(c[t][e], s[t], STEPS);
+            x[e] = STEPS == 127 ? r : r * r;
+        }
+        Four<float>::store(out, at + t * 1024, left[t], x);
+    }
+}
+
 __global__ __launch_bounds__(256) void k_adamw_state(
     const int8_t* m, const uint8_t* v, const float* ms, const float* vs,
     int64_t n, float* mo, float* vo)
 {
-    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (at >= n) return;
-    const int left = n - at >= 4 ? 4 : (int)(n - at);
-    Four<float>::Wide x;
-    if (mo) {
-        const auto c = Four<int8_t>::load(m, at, left);
-        const float s = ms[at / kAdamBlock];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = decode8(c[e], s, 127);
-        Four<float>::store(mo, at, left, x);
-    }
-    if (vo) {
-        const auto c = Four<uint8_t>::load(v, at, left);
-        const float s = vs[at / kAdamBlock];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float r = decode8(c[e], s, 254);
-            x[e] = r * r;
-        }
-        Four<float>::store(vo, at, left, x);
-    }
+    const int64_t at =
+        (int64_t)blockIdx.x * (1024 * kTurns) + threadIdx.x * 4;
+    if (mo) decode_turns<127>(m, ms, at, n, mo);
+    if (vo) decode_turns<254>(v, vs, at, n, vo);
 }
 
 template <int PT, int GT>
@@ -382,13 +397,14 @@ void adamw_state(const int8_t* m, const uint8_t* v, const float* ms,
                  const float* vs, int64_t n, float* mo, float* vo,
                  hipStream_t s)
 {
-    // at most 2^30 blocks to a launch, each a whole number of scales
+    // 2^32 values to a launch, a whole number of blocks and scales
     const int64_t most = (int64_t)256 << 24;
     for (int64_t at = 0; at < n; at += most) {
         const int64_t len = n - at < most ? n - at : most;
         hipLaunchKernelGGL(k_adamw_state,
-                           dim3((unsigned)((len + 1023) / 1024)), dim3(256), 0,
-                           s, m ? m + at : nullptr, v ? v + at : nullptr,
+                           dim3((unsigned)((len + kTurns * 1024 - 1) /
+                                           (kTurns * 1024))),
+                           dim3(256), 0, s, m ? m + at : nullptr, v ? v + at : nullptr,
                            ms ? ms + at / kAdamBlock : nullptr,
                            vs ? vs + at / kAdamBlock : nullptr, len,
                            mo ? mo + at : nullptr, vo ? vo + at : nullptr);
