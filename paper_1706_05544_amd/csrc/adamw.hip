@@ -156,9 +156,12 @@ struct Four {
     }
 };
 
-// A block of kAdamBlock values to a wave, four of them to a lane.  One read
-// and one write of all that a step touches; bound by memory (and, with
-// states in 8 bits, nearly as much by the square roots).
+// A block of kAdamBlock values to a wave, four of them to a lane, so that the
+// scales of 8-bit states are a matter of one wave.  One read and one write of
+// all that a step touches.  Bound by memory: 67 million values in bf16 with
+// master weights and 8-bit states 201 us, 5.3 TB/s; in 32 bits 347 us, 5.4
+// TB/s (a large copy: 5.2).  With correctly rounded square roots and divisions
+// for every value the former took 249: the vector instructions bound it.
 template <int PT, int GT, int BITS, bool MASTER>
 __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
 {
@@ -248,7 +251,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
 }
 
 // Four values to a thread in each of kTurns turns, whose codes are all loaded
-// before the first is decoded.
+// before the first is decoded.  Bound by memory: 67 million values 130 us, 5.2
+// TB/s (150 with one turn).
 constexpr int kTurns = 4;
 
 template <int STEPS>
@@ -404,7 +408,8 @@ void adamw_state(const int8_t* m, const uint8_t* v, const float* ms,
         hipLaunchKernelGGL(k_adamw_state,
                            dim3((unsigned)((len + kTurns * 1024 - 1) /
                                            (kTurns * 1024))),
-                           dim3(256), 0, s, m ? m + at : nullptr, v ? v + at : nullptr,
+                           dim3(256), 0, s, m ? m + at : nullptr,
+                           v ? v + at : nullptr,
                            ms ? ms + at / kAdamBlock : nullptr,
                            vs ? vs + at / kAdamBlock : nullptr, len,
                            mo ? mo + at : nullptr, vo ? vo + at : nullptr);

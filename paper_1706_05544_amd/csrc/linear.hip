@@ -7,8 +7,12 @@ namespace msvm {
 namespace {
 
 // dZ = dY act'(Z) as a factor of the products (its rows end in zeros up to a
-// multiple of 8), and the sums of its columns over this block's rows.  One pass over dY and Z: 8 columns to a thread, 32
-// threads side by side, 8 rows at once.
+// multiple of 8), and the sums of its columns over this block's rows.  One
+// pass over dY and Z: 8 columns to a thread, 32 threads side by side, 8 rows
+// at once.  dZ is rounded to the arrays' type, as the 16-bit products need
+// their factors; the sums take it unrounded.  Bound by memory: 8192 x 2048 in
+// bf16 19.1 us, 5.3 TB/s.  (Done while the products load their tiles it would
+// be computed once for each tile of W's columns, with the slopes of gelu.)
 constexpr int kGradCols = 256, kGradLanes = 8;
 
 struct GradArgs {
@@ -93,7 +97,9 @@ void launch_zero(const svm_array& a, hipStream_t s)
     });
 }
 
-// 16 columns to a block, 16 threads to a column.
+// Joins the blocks' sums in a fixed order, two arrays of them in one launch:
+// 16 columns to a block, 16 threads to a column.  Bound by latency: 4 to 5 us,
+// 9 for the two arrays of 768 rows by 4096.
 template <int DT>
 __global__ __launch_bounds__(256) void k_column_sums(
     const float* part0, const float* part1, int64_t np, int64_t cols,
