@@ -786,6 +786,35 @@ def test_adamw_8_bit_codes_are_those_of_the_definition():
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_second_moments_below_the_normal_range(bits):
+    # v of some 1e-42 to 1e-40 is subnormal, its square root is not: codes
+    # and steps as from that square root (of v as 32 bits hold it)
+    g = torch.Generator().manual_seed(10)
+    x = (3e-20 * 10 ** torch.rand(1024, generator=g)) \
+        * torch.randn(1024, generator=g).sign()
+    x[::7] = 0.0
+    p = torch.zeros(1024, device=DEV)
+    st = nv.svm_adamw_states([p], bits=bits)
+    nv.svm_adamw_step([p], [x.to(DEV)], *st, lr=1.0, eps=0.0,
+                      weight_decay=0.0, step=1)
+    v = x * x * torch.tensor(1.0 - 0.999, dtype=torch.float32)
+    assert float(v.max()) < 2.0 ** -126
+    r = v.double().sqrt()
+    live = x != 0
+    want = -(0.1 * x.double() / 0.1) / (r / math.sqrt(1.0 - 0.999))
+    off = (p.cpu().double() - want).abs()[live]
+    assert bool((off <= 16 * E * want.abs()[live]).all())
+    assert bool(p.cpu()[~live].isnan().all())  # 0 / 0: eps is 0
+    if bits == 8:
+        y = 254 * (r.view(-1, 256) / r.view(-1, 256).amax(1, keepdim=True)
+                   ).sqrt().view(-1)
+        near = ((y % 1) - 0.5).abs() < 2.0 ** -10
+        code = st[1].cpu().double()
+        assert bool((code == y.round())[~near].all())
+        assert int(near.sum()) < 32
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_adamw_not_finite_and_zero_gradients(bits):
     p = torch.ones(600, device=DEV)
     q = p.clone()
