@@ -1065,8 +1065,8 @@ struct TileCost {
     double one, more, rest;
 };
 constexpr TileCost kCost16[3] = {{256, 256, 1.65, 1.65, 5.0},
-                                 {128, 128, 0.55, 0.55, 4.0},
-                                 {64, 64, 0.26, 0.19, 1.5}};
+                                 {128, 128, 0.57, 0.57, 4.0},
+                                 {64, 64, 0.26, 0.23, 1.5}};
 constexpr TileCost kCost32[3] = {{256, 128, 2.50, 2.50, 10.0},
                                  {128, 128, 1.45, 1.42, 7.0},
                                  {64, 64, 0.65, 0.48, 2.0}};
@@ -1082,7 +1082,10 @@ struct Choice {
 // (8192 x 2048 over 2048, bf16: 61 us in tiles of 256, 65 in tiles of 128;
 // 2048 x 2048 over 8192 in 32 bits: 335 us in two parts, 408 in smaller
 // tiles; 6656 x 209 over 2347: 66 us in four parts, 76 in smaller tiles).
-// Parts cost a launch more, and their sums are written and read once.
+// Parts cost a launch more (8 us with the host's share: 476 x 64 over 2304,
+// bf16, takes 14.6 us whole and 19.0 in nine parts), and their sums are
+// written and read once (5000 x 1000 over 5000, bf16: 72 us in three parts of
+// tiles of 256; over 97 whole, in tiles of 64 or 128).
 Choice choose(const Product& p, int nk)
 {
     const TileCost* table = p.dtype == SVM_F32 ? kCost32 : kCost16;
@@ -1099,7 +1102,7 @@ Choice choose(const Product& p, int nk)
                 std::max(blocks * t.more, t.one + (blocks - 1) * 0.5 * t.more);
             double us = (double)((nk + s - 1) / s) * step + blocks * t.rest;
             if (s > 1)
-                us += 5.0 + (double)s * (double)p.m * (double)p.n * 8 / 3.5e6;
+                us += 8.0 + (double)s * (double)p.m * (double)p.n * 8 / 5e6;
             if (us < least) {
                 least = us;
                 best = {&t, s};
