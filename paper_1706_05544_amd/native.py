@@ -688,11 +688,10 @@ def svm_linear(X, W, bias=None, residual=None, act="none", save: bool = False,
     _check(lib.svm_linear_workspace(ct.byref(a), ct.byref(w),
                                     ct.byref(need)))
     ws = c.work(need.value)
+    b, r = c.arr(bias, "bias"), c.arr(residual, "residual")
     c.ready()
-    _check(lib.svm_linear(ct.byref(a), ct.byref(w),
-                          _ref(c.arr(bias, "bias")),
-                          _ref(c.arr(residual, "residual")), _act(act),
-                          ct.byref(c.arr(Y, "out", True)),
+    _check(lib.svm_linear(ct.byref(a), ct.byref(w), _ref(b), _ref(r),
+                          _act(act), ct.byref(c.arr(Y, "out", True)),
                           _ref(c.arr(Z, "Z", True)), ws, need.value,
                           c.index, c.handle))
     c.done()

@@ -1,0 +1,69 @@
+"""The Python binding of the feature-map calls, without a GPU: CPU tensors
+and a library that only records its calls stand in for the real ones."""
+import pytest
+import torch
+
+from paper_1706_05544_amd import native as nv
+
+
+class Recorded(nv._Call):
+    """A call whose arrays may lie in host memory, and which knows what was
+    copied after its stream began to wait for torch's."""
+
+    late: list = []
+
+    def __init__(self, t, stream):
+        nv._DTYPES.update({torch.float32: nv.SVM_F32,
+                           torch.bfloat16: nv.SVM_BF16,
+                           torch.float16: nv.SVM_F16})
+        self.device, self.index = t.device, t.get_device()
+        self.stream, self.handle, self.other = stream, 0, False
+        self.keep, self.waited = [], False
+
+    def arr(self, t, what, out=False):
+        a = super().arr(t, what, out)
+        if self.waited and a is not None and a.data != t.data_ptr():
+            self.late.append(what)
+        return a
+
+    def floats(self, t, rows, what):
+        c = t.contiguous()
+        if self.waited and c is not t:
+            self.late.append(what)
+        self.keep.append(c)
+        return c.data_ptr()
+
+    def ready(self):
+        self.waited = True
+
+
+class Library:
+    """Accepts every call."""
+
+    def __getattr__(self, name):
+        return lambda *args: 0
+
+
+@pytest.fixture
+def late(monkeypatch):
+    monkeypatch.setattr(nv, "_Call", Recorded)
+    monkeypatch.setattr(nv, "load", Library)
+    monkeypatch.setattr(Recorded, "late", [])
+    return Recorded.late
+
+
+def test_inputs_are_copied_before_the_stream_waits(late):
+    # a copy of an input without a row layout is queued on torch's stream:
+    # another stream waits for it only if it is queued before the wait
+    m, k, n = 6, 8, 10
+    x = lambda rows, cols: torch.randn(cols, rows).t()  # noqa: E731
+    v = lambda cols: torch.randn(2 * cols)[::2]  # noqa: E731
+    nv.svm_linear(x(m, k), x(n, k), v(n), x(m, n), act="gelu", save=True)
+    nv.svm_linear_backward(x(m, n), x(m, k), x(n, k), x(m, n), act="gelu")
+    nv.svm_layer_norm(x(m, n), v(n), v(n), save=True)
+    nv.svm_layer_norm_backward(x(m, n), x(m, n), v(m), v(m), v(n),
+                               residual=x(m, n))
+    nv.svm_hinge_loss(x(m, n), torch.zeros(2 * m, dtype=torch.int32)[::2])
+    p = [torch.randn(n, k), torch.randn(n)]
+    nv.svm_adamw_step(p, [x(n, k), v(n)], *nv.svm_adamw_states(p, bits=8))
+    assert late == []
