@@ -361,7 +361,9 @@ svm_status svm_tune(const svm_matrix *X, const float *y,
  *   - All arrays of a call have one type (svm_dtype), except where stated.
  *     Products, sums, statistics and states are held in 32 bits and rounded
  *     to that type once, when they are written (SVM_F32 products are made
- *     of three 8-bit parts of each factor: as exact as 32-bit products).
+ *     of three 8-bit parts of each factor: as exact as 32-bit products for
+ *     factors from 2^-109 (1.5e-33) up to the largest; a smaller one is
+ *     held to within 2^-134).
  *   - Outputs must not overlap inputs or each other, except where stated.
  *   - work: device memory of the caller, 16-byte aligned, of at least the
  *     bytes that the call's _workspace function writes to *bytes for the

@@ -195,7 +195,9 @@ __device__ __forceinline__ int eight_of(int64_t n, int64_t j)
 
 // The three bf16 parts of eight 32-bit values: x = h + m + l, each part what
 // is left rounded to nearest.  Where x is not finite, or rounds to a bf16
-// that is not, h is that and the others are 0.
+// that is not, h is that and the others are 0.  From |x| = 2^-109 on they hold
+// all 24 bits; below, l falls under bf16's smallest step, and the sum is off
+// by up to half of it, 2^-134.
 typedef __bf16 Bf16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ void three_parts(const float (&v)[8],
@@ -204,8 +206,8 @@ __device__ __forceinline__ void three_parts(const float (&v)[8],
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         part[0][e] = (__bf16)v[e];
-        const float r =
-            fabsf(v[e]) < 3.38e38f ? v[e] - (float)part[0][e] : 0.0f;
+        const float h = (float)part[0][e];
+        const float r = fabsf(h) <= 3.402823466e38f ? v[e] - h : 0.0f;
         part[1][e] = (__bf16)r;
         part[2][e] = (__bf16)(r - (float)part[1][e]);
     }
