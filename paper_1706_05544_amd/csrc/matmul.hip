@@ -249,35 +249,151 @@ struct Frag {
     }
 };
 
-// A sum of 32-bit factors that is not finite, again in 32 bits: an infinity
-// has zeros for its lower parts, its products with another factor's parts
-// differ in sign, and what rounds past the largest bf16 is none.
-__device__ __forceinline__ float exact_sum(const Factor& A, const Factor& B,
-                                           int64_t i, int64_t j, int64_t k)
+// ---- 32-bit sums that are not finite
+//
+// An infinity has zeros for its lower parts, its products with another
+// factor's parts differ in sign, and what rounds past the largest bf16 is
+// none: sums of three parts that come out not finite are formed again from
+// the values as they are, by the 32-bit matrix instruction, a fragment of 16 x
+// 16 outputs at a time.  A wave loads 64 summed values of both at once for it
+// and shares nothing with the others, so that it is bound by the caches'
+// latency: a product all of whose outputs are NaN takes 3 to 10 times one of
+// finite values (50000 x 2048 over 784: 1.2 ms, all NaN 5.8; 256 x 256 over
+// 100000: 112 us, all NaN 700; formed a sum to a lane it was some 300 times).
+
+__device__ __forceinline__ bool is_finite(float v)
 {
-    const float* a = (const float*)A.data + (A.along ? i * A.ld : i);
-    const float* b = (const float*)B.data + (B.along ? j * B.ld : j);
-    const int64_t sa = A.along ? 1 : A.ld, sb = B.along ? 1 : B.ld;
-    float sum = 0.0f;
+    return fabsf(v) <= 3.402823466e38f;
+}
+
+// 16 rows of a factor from x0 on (of n), for the matrix instruction: a lane
+// has row lane mod 16 and four of every 16 summed values.
+template <bool ALONG>
+struct Rows16;
+
+template <>
+struct Rows16<true> {
+    const float* row;
+    bool there;
+
+    __device__ __forceinline__ Rows16(const void* data, int64_t ld, int64_t x0,
+                                      int64_t n, int lane)
+        : row((const float*)data + (x0 + (lane & 15)) * ld),
+          there(x0 + (lane & 15) < n)
+    {
+    }
+
+    // Summed values r0 .. r0 + 63, zeros from `end` on.
+    __device__ __forceinline__ void load(int64_t r0, int64_t end, int lane,
+                                         floatx4 (&v)[4]) const
+    {
+        typedef floatx4 Loose __attribute__((aligned(4)));
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t r = r0 + u * 16 + (lane >> 4) * 4;
+            v[u] = floatx4{0, 0, 0, 0};
+            if (!there) continue;
+            if (r + 4 <= end) {
+                v[u] = *(const Loose*)(row + r);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (r + e < end) v[u][e] = row[r + e];
+            }
+        }
+    }
+};
+
+template <>
+struct Rows16<false> {
+    const float* col;  // x0 in the factor's first row (the same in all lanes)
+    int64_t ld, width;
+
+    __device__ __forceinline__ Rows16(const void* data, int64_t ld, int64_t x0,
+                                      int64_t n, int)
+        : col((const float*)data + x0), ld(ld), width(n - x0)
+    {
+    }
+
+    // (row `end` and those after it lie past the descriptor's range: zeros)
+    __device__ __forceinline__ void load(int64_t r0, int64_t end, int lane,
+                                         floatx4 (&v)[4]) const
+    {
+        const int64_t left = 4 * ((end - 1 - r0) * ld + width);
+        __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<float*>(col + r0 * ld), 0,
+            (int)(left < 0xffffffff ? (uint32_t)left : 0xffffffffu),
+            0x00020000);
+        const int ld4 = (int)ld * 4;
+        const int off = (lane >> 4) * 4 * ld4 + (lane & 15) * 4;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[u][e] = __builtin_bit_cast(
+                    float, __builtin_amdgcn_raw_buffer_load_b32(
+                               rs, off, (u * 16 + e) * ld4, 0));
+    }
+};
+
+// The sums of 16 x 16 outputs over summed values r0, r0 + step .., 64 from
+// each, up to `end`.
+template <bool AALONG, bool BALONG>
+__device__ __forceinline__ floatx4 sums_32(const Rows16<AALONG>& a,
+                                           const Rows16<BALONG>& b, int64_t r0,
+                                           int64_t end, int step, int lane)
+{
+    floatx4 sum = {0, 0, 0, 0};
 #pragma unroll 1
-    for (int64_t r = 0; r < k; ++r) sum = fmaf(a[r * sa], b[r * sb], sum);
+    for (int64_t r = r0; r < end; r += step) {
+        floatx4 av[4], bv[4];
+        a.load(r, end, lane, av);
+        b.load(r, end, lane, bv);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sum = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[u][e], av[u][e],
+                                                           sum, 0, 0, 0);
+    }
     return sum;
 }
 
-// Replaces those of eight sums that are not finite by exact(c).
-template <class F>
-__device__ __forceinline__ void mend(float (&v)[8], int count, F&& exact)
+// Forms those sums of a wave's tile again that are not finite: FM x FN
+// fragments from row iw and column jw on, summed values [r0, end).
+template <int FM, int FN, bool AALONG, bool BALONG>
+__device__ __forceinline__ void mend_tile(const Args& p, floatx4 (&acc)[FM][FN],
+                                          int64_t iw, int64_t jw, int64_t r0,
+                                          int64_t end, int lane)
 {
-    bool fine = true;
+    static_assert(FM * FN <= 32, "a bit for each fragment");
+    const int64_t il = iw + (lane & 15), jl = jw + (lane >> 4) * 4;
+    unsigned bad = 0;  // fragments with such a sum, the same in every lane
 #pragma unroll
-    for (int c = 0; c < 8; ++c) fine &= fabsf(v[c]) <= 3.402823466e38f;
-    if (fine) return;
-#pragma unroll 1
-    for (int c = 0; c < count; ++c) {
-        const float s = exact(c);
+    for (int f = 0; f < FM; ++f)
 #pragma unroll
-        for (int d = 0; d < 8; ++d)
-            if (d == c && !(fabsf(v[d]) <= 3.402823466e38f)) v[d] = s;
+        for (int g = 0; g < FN; ++g) {
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                any |= !is_finite(acc[f][g][e]) && jl + g * 16 + e < p.n;
+            if (__ballot(any && il + f * 16 < p.m)) bad |= 1u << (f * FN + g);
+        }
+    while (bad) {
+        const int q = __builtin_ctz(bad);
+        bad &= bad - 1;
+        const floatx4 sum = sums_32(
+            Rows16<AALONG>(p.A.data, p.A.ld, iw + q / FN * 16, p.m, lane),
+            Rows16<BALONG>(p.B.data, p.B.ld, jw + q % FN * 16, p.n, lane), r0,
+            end, 64, lane);
+#pragma unroll
+        for (int f = 0; f < FM; ++f)
+#pragma unroll
+            for (int g = 0; g < FN; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (q == f * FN + g && !is_finite(acc[f][g][e]))
+                        acc[f][g][e] = sum[e];
     }
 }
 
@@ -391,10 +507,6 @@ __device__ __forceinline__ void write_tile(const Args& p,
                             ((int64_t)blockIdx.y * p.m + i) * p.n + j, count);
                     continue;
                 }
-                if constexpr (OT == SVM_F32)
-                    mend(x.v, count, [&](int c) {
-                        return exact_sum(p.A, p.B, i, j + c, p.k);
-                    });
                 finish<OT>(p.e, x, bias, res[u], i, j, count);
             }
         }
@@ -778,6 +890,10 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
         multiply(am, bh);
         multiply(ah, bh);
     }
+    const int64_t end = (int64_t)(t0 + p.per) * kBK;
+    mend_tile<FM, FN, AALONG, BALONG>(p, acc, i0 + wi, j0 + wj,
+                                      (int64_t)t0 * kBK, end < p.k ? end : p.k,
+                                      lane);
     meet<63>();
     write_tile<SVM_F32, FM, FN>(p, acc,
                                 wave_slab<kSlab, NW, kLds>(lds0, lds1, wave),
@@ -809,10 +925,6 @@ __global__ __launch_bounds__(256) void k_join(Args p)
         }
         if (p.e.bias) bias.load(p.e.bias, j, count);
         if (p.e.residual) res.load(p.e.residual, i * p.e.ldr + j, count);
-        if constexpr (OT == SVM_F32)
-            mend(x.v, count, [&](int c) {
-                return exact_sum(p.A, p.B, i, j + c, p.k);
-            });
         finish<OT>(p.e, x, bias, res, i, j, count);
     }
 }
@@ -911,6 +1023,23 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(FewArgs p)
                 acc[t] = mfma<IT>(w.h[u], x[t].h[u], acc[t]);
             }
     }
+    if constexpr (DT == SVM_F32) {  // the wave's sums that are not finite
+        const Rows16<true> wr(p.W, p.ldw, j0, p.n, lane);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            bool any = false;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                any |= !is_finite(acc[t][e]) && j0 + g * 4 + e < p.n;
+            if (!__ballot(any && t * 16 + i < p.m)) continue;
+            const floatx4 sum =
+                sums_32(Rows16<true>(p.X, p.ldx, t * 16, p.m, lane), wr,
+                        wave * 64, p.k, 64 * kFewWaves, lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (!is_finite(acc[t][e])) acc[t][e] = sum[e];
+        }
+    }
 #pragma unroll
     for (int t = 0; t < MT; ++t)
         *(floatx4*)&red[wave][t * 16 + i][g * 4] = acc[t];
@@ -930,15 +1059,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(FewArgs p)
     for (int w = 0; w < kFewWaves; ++w)
 #pragma unroll
         for (int c = 0; c < 8; ++c) v.v[c] += red[w][row][c0 + c];
-    if constexpr (DT == SVM_F32)
-        mend(v.v, count, [&](int c) {
-            const float* x = (const float*)p.X + row * p.ldx;
-            const float* w = (const float*)p.W + (j + c) * p.ldw;
-            float s = 0.0f;
-#pragma unroll 1
-            for (int64_t r = 0; r < p.k; ++r) s = fmaf(x[r], w[r], s);
-            return s;
-        });
     finish<DT>(p.e, v, bias, res, row, j, count);
 }
 
