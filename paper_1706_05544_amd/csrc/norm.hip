@@ -225,14 +225,13 @@ __global__ __launch_bounds__(kThreads<G>) void k_norm_grad(NormGradView p)
         float xh[IT][8], g[IT][8];
         const float mu = p.mean[i], rs = p.rstd[i];
         float s1 = 0.0f, s2 = 0.0f;
-        // Past the row's end X and dY are 0: what is added is 0, or NaN in a
-        // row whose mean or rstd is not finite, and such rows are NaN anyway.
+        // (past the row's end X is 0, but (0 - mean) rstd may overflow)
 #pragma unroll
         for (int t = 0; t < IT; ++t) {
             r[t] = nr[t];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                xh[t][e] = (nx[t].at(e) - mu) * rs;
+                xh[t][e] = e < count[t] ? (nx[t].at(e) - mu) * rs : 0.0f;
                 g[t][e] = ng[t].at(e);
             }
         }
