@@ -358,6 +358,7 @@ svm_status svm_tune(const svm_matrix *X, const float *y,
  *   - The work is queued on `stream` (hipStream_t; NULL: the null stream)
  *     and NOT waited for.  Nothing is allocated or freed and nothing is
  *     copied to the host, so the calls can be captured into a HIP graph.
+ *     The thread's current device is left as it was.
  *   - All arrays of a call have one type (svm_dtype), except where stated.
  *     Products, sums, statistics and states are held in 32 bits and rounded
  *     to that type once, when they are written (SVM_F32 products are made

@@ -24,6 +24,27 @@ struct ClearHipError {
     ~ClearHipError() { (void)hipGetLastError(); }
 };
 
+// The thread's device is `dev` while this lives, and what it was afterwards:
+// for calls that come between a caller's own device calls.
+class OnDevice {
+public:
+    explicit OnDevice(int dev)
+    {
+        HIP_TRY(hipGetDevice(&before_));
+        if (before_ != dev) HIP_TRY(hipSetDevice(dev));
+        else before_ = -1;
+    }
+    ~OnDevice()
+    {
+        if (before_ >= 0) (void)hipSetDevice(before_);
+    }
+    OnDevice(const OnDevice&) = delete;
+    OnDevice& operator=(const OnDevice&) = delete;
+
+private:
+    int before_ = -1;
+};
+
 }  // namespace msvm
 
 #define GUARD_BEGIN \

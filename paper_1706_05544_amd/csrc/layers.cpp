@@ -207,7 +207,7 @@ svm_status svm_linear(const svm_array* X, const svm_array* W,
     CHECK(check_work(work, work_bytes, count.used));
     CHECK(check_ordinal(device));
     if (m == 0) return SVM_OK;
-    HIP_TRY(hipSetDevice(device));
+    msvm::OnDevice on(device);
     msvm::Pieces ws{static_cast<unsigned char*>(work), true};
     msvm::linear_forward(a, ws, (hipStream_t)stream);
     HIP_TRY(hipPeekAtLastError());
@@ -262,7 +262,7 @@ svm_status svm_linear_backward(const svm_array* dY, const svm_array* X,
     CHECK(check_work(work, work_bytes, count.used));
     CHECK(check_ordinal(device));
     if (!dX && !dW && !dbias) return SVM_OK;
-    HIP_TRY(hipSetDevice(device));
+    msvm::OnDevice on(device);
     msvm::Pieces ws{static_cast<unsigned char*>(work), true};
     msvm::linear_backward(a, ws, (hipStream_t)stream);
     HIP_TRY(hipPeekAtLastError());
@@ -287,7 +287,7 @@ svm_status svm_layer_norm(const svm_array* X, const svm_array* weight,
     CHECK(check_ordinal(device));
     if (m == 0) return SVM_OK;
     GUARD_BEGIN
-    HIP_TRY(hipSetDevice(device));
+    msvm::OnDevice on(device);
     msvm::NormArgs a{*X, or_none(weight), or_none(bias), *Y, (float)eps, mean,
                      rstd};
     msvm::norm_forward(a, (hipStream_t)stream);
@@ -346,7 +346,7 @@ svm_status svm_layer_norm_backward(const svm_array* dY, const svm_array* X,
         CHECK(check_work(work, work_bytes, msvm::norm_backward_bytes(m, n)));
     CHECK(check_ordinal(device));
     GUARD_BEGIN
-    HIP_TRY(hipSetDevice(device));
+    msvm::OnDevice on(device);
     msvm::NormGradArgs a{*dY,         *X,
                          or_none(weight),  or_none(residual),
                          or_none(dX),      or_none(dweight),
@@ -390,7 +390,7 @@ svm_status svm_hinge_loss(const svm_array* S, const int32_t* labels,
                      msvm::hinge_bytes(S->rows, S->cols)));
     CHECK(check_ordinal(device));
     GUARD_BEGIN
-    HIP_TRY(hipSetDevice(device));
+    msvm::OnDevice on(device);
     msvm::Pieces ws{static_cast<unsigned char*>(work), true};
     msvm::hinge_loss(*S, labels, (float)scale, or_none(dS), loss, ws,
                      (hipStream_t)stream);
@@ -451,7 +451,7 @@ svm_status svm_adamw_step(const svm_adamw_tensor* tensors, int32_t n_tensors,
     }
     CHECK(check_ordinal(device));
     GUARD_BEGIN
-    HIP_TRY(hipSetDevice(device));
+    msvm::OnDevice on(device);
     msvm::adamw_step(tensors, n_tensors, *p, (hipStream_t)stream);
     HIP_TRY(hipPeekAtLastError());
     return SVM_OK;
@@ -470,7 +470,7 @@ svm_status svm_adamw_state(const int8_t* m, const uint8_t* v,
     CHECK(check_ordinal(device));
     if (n == 0 || (!m_out && !v_out)) return SVM_OK;
     GUARD_BEGIN
-    HIP_TRY(hipSetDevice(device));
+    msvm::OnDevice on(device);
     msvm::adamw_state(m, v, m_scale, v_scale, n, m_out, v_out,
                       (hipStream_t)stream);
     HIP_TRY(hipPeekAtLastError());
