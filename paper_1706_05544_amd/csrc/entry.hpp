@@ -24,9 +24,32 @@ struct ClearHipError {
     ~ClearHipError() { (void)hipGetLastError(); }
 };
 
+// Status and message of the exception at hand; nothing leaves it.  (The short
+// text needs no memory of its own: it is what is told where there is none.)
+inline svm_status caught() noexcept
+{
+    static const char* const kNoMemory = "no host memory";
+    try {
+        try {
+            throw;
+        } catch (const Error& e) {
+            return fail(e.status, e.msg);
+        } catch (const std::bad_alloc&) {
+            return fail(SVM_E_NOMEM, kNoMemory);
+        } catch (const std::exception& e) {
+            return fail(SVM_E_INTERNAL, e.what());
+        } catch (...) {
+            return fail(SVM_E_INTERNAL, "unknown error");
+        }
+    } catch (...) {
+        return fail(SVM_E_NOMEM, kNoMemory);
+    }
+}
+
 // The thread's device is `dev` while this lives, and what it was afterwards:
-// for calls that come between a caller's own device calls.
-class OnDevice {
+// for calls that come between a caller's own device calls.  HIP's last error
+// is left clean.
+class OnDevice : ClearHipError {
 public:
     explicit OnDevice(int dev)
     {
@@ -47,16 +70,13 @@ private:
 
 }  // namespace msvm
 
+// Around a whole entry: no exception leaves it.  GUARD_BEGIN keeps HIP's last
+// error clean too; ENTRY_BEGIN makes no HIP call by itself, so that a call that
+// is refused makes none.
+#define ENTRY_BEGIN try {
 #define GUARD_BEGIN \
     msvm::ClearHipError clear_hip_error_on_exit_; \
-    try {
-#define GUARD_END                                                      \
-    }                                                                  \
-    catch (const msvm::Error& e) { return msvm::fail(e.status, e.msg); } \
-    catch (const std::bad_alloc&) {                                    \
-        return msvm::fail(SVM_E_NOMEM, "host allocation failed");      \
-    }                                                                  \
-    catch (const std::exception& e) {                                  \
-        return msvm::fail(SVM_E_INTERNAL, e.what());                   \
-    }                                                                  \
-    catch (...) { return msvm::fail(SVM_E_INTERNAL, "unknown error"); }
+    ENTRY_BEGIN
+#define GUARD_END \
+    } \
+    catch (...) { return msvm::caught(); }

@@ -111,6 +111,7 @@ svm_status check_work(const void* work, int64_t work_bytes, int64_t need)
 svm_status check_ordinal(int32_t device)
 {
     if (device < 0) return fail(SVM_E_INVALID, "device must be >= 0");
+    msvm::ClearHipError clear;
     return check_device(device);
 }
 
@@ -168,10 +169,10 @@ extern "C" {
 svm_status svm_linear_workspace(const svm_array* X, const svm_array* W,
                                 int64_t* bytes)
 {
+    ENTRY_BEGIN
     if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
     *bytes = 0;
     CHECK(check_linear_inputs(X, W));
-    GUARD_BEGIN
     msvm::LinearArgs a{*X, *W, kNone, kNone, kNone, kNone, SVM_ACT_NONE};
     msvm::Pieces count;
     msvm::linear_forward(a, count, nullptr);
@@ -186,6 +187,7 @@ svm_status svm_linear(const svm_array* X, const svm_array* W,
                       void* work, int64_t work_bytes, int32_t device,
                       void* stream)
 {
+    ENTRY_BEGIN
     CHECK(check_act(act));
     CHECK(check_linear_inputs(X, W));
     const int64_t m = X->rows, n = W->rows;
@@ -199,7 +201,6 @@ svm_status svm_linear(const svm_array* X, const svm_array* W,
         CHECK(check_array(Z, "Z", m, n, t));
         CHECK(check_apart(Z, "Z", {X, W, bias, residual}));
     }
-    GUARD_BEGIN
     msvm::LinearArgs a{*X,           *W, *Y, or_none(Z), or_none(bias),
                        or_none(residual), act};
     msvm::Pieces count;
@@ -223,10 +224,10 @@ svm_status svm_linear_backward_workspace(const svm_array* dY,
                                          const svm_array* dbias,
                                          int64_t* bytes)
 {
+    ENTRY_BEGIN
     if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
     *bytes = 0;
     CHECK(check_linear_grad(dY, X, W, act, dX, dW, dbias));
-    GUARD_BEGIN
     msvm::LinearGradArgs a{*dY,         or_none(X),  or_none(W),
                            kNone,       or_none(dX), or_none(dW),
                            or_none(dbias), act};
@@ -244,6 +245,7 @@ svm_status svm_linear_backward(const svm_array* dY, const svm_array* X,
                                void* work, int64_t work_bytes, int32_t device,
                                void* stream)
 {
+    ENTRY_BEGIN
     CHECK(check_linear_grad(dY, X, W, act, dX, dW, dbias));
     const int64_t m = dY->rows, n = dY->cols;
     if (Z)
@@ -253,7 +255,6 @@ svm_status svm_linear_backward(const svm_array* dY, const svm_array* X,
     if (dX) CHECK(check_apart(dX, "dX", {dY, X, W, Z, dW, dbias}));
     if (dW) CHECK(check_apart(dW, "dW", {dY, X, W, Z, dbias}));
     if (dbias) CHECK(check_apart(dbias, "dbias", {dY, X, W, Z}));
-    GUARD_BEGIN
     msvm::LinearGradArgs a{*dY,         or_none(X),  or_none(W),
                            or_none(Z),  or_none(dX), or_none(dW),
                            or_none(dbias), act};
@@ -275,6 +276,7 @@ svm_status svm_layer_norm(const svm_array* X, const svm_array* weight,
                           const svm_array* Y, float* mean, float* rstd,
                           int32_t device, void* stream)
 {
+    ENTRY_BEGIN
     CHECK(check_first(X, "X"));
     const int64_t m = X->rows, n = X->cols;
     if (weight) CHECK(check_array(weight, "weight", 1, n, X->dtype));
@@ -286,7 +288,6 @@ svm_status svm_layer_norm(const svm_array* X, const svm_array* weight,
     if (!same(Y, X)) CHECK(check_apart(Y, "Y", {X}));
     CHECK(check_ordinal(device));
     if (m == 0) return SVM_OK;
-    GUARD_BEGIN
     msvm::OnDevice on(device);
     msvm::NormArgs a{*X, or_none(weight), or_none(bias), *Y, (float)eps, mean,
                      rstd};
@@ -299,6 +300,7 @@ svm_status svm_layer_norm(const svm_array* X, const svm_array* weight,
 svm_status svm_layer_norm_backward_workspace(int64_t rows, int64_t cols,
                                              int64_t* bytes)
 {
+    ENTRY_BEGIN
     if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
     *bytes = 0;
     if (rows < 0 || rows > ((int64_t)1 << 31) - 1)
@@ -307,6 +309,7 @@ svm_status svm_layer_norm_backward_workspace(int64_t rows, int64_t cols,
         return fail(SVM_E_INVALID, "cols must be in [1, 2^21]");
     *bytes = msvm::norm_backward_bytes(rows, cols);
     return SVM_OK;
+    GUARD_END
 }
 
 svm_status svm_layer_norm_backward(const svm_array* dY, const svm_array* X,
@@ -319,6 +322,7 @@ svm_status svm_layer_norm_backward(const svm_array* dY, const svm_array* X,
                                    int64_t work_bytes, int32_t device,
                                    void* stream)
 {
+    ENTRY_BEGIN
     CHECK(check_first(dY, "dY"));
     const int64_t m = dY->rows, n = dY->cols;
     const int32_t t = dY->dtype;
@@ -345,7 +349,6 @@ svm_status svm_layer_norm_backward(const svm_array* dY, const svm_array* X,
     if (dweight || dbias)
         CHECK(check_work(work, work_bytes, msvm::norm_backward_bytes(m, n)));
     CHECK(check_ordinal(device));
-    GUARD_BEGIN
     msvm::OnDevice on(device);
     msvm::NormGradArgs a{*dY,         *X,
                          or_none(weight),  or_none(residual),
@@ -362,6 +365,7 @@ svm_status svm_layer_norm_backward(const svm_array* dY, const svm_array* X,
 svm_status svm_hinge_loss_workspace(int64_t rows, int64_t cols,
                                     int64_t* bytes)
 {
+    ENTRY_BEGIN
     if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
     *bytes = 0;
     if (rows < 0 || rows > ((int64_t)1 << 31) - 1)
@@ -370,6 +374,7 @@ svm_status svm_hinge_loss_workspace(int64_t rows, int64_t cols,
         return fail(SVM_E_INVALID, "cols must be in [1, 2^21]");
     *bytes = msvm::hinge_bytes(rows, cols);
     return SVM_OK;
+    GUARD_END
 }
 
 svm_status svm_hinge_loss(const svm_array* S, const int32_t* labels,
@@ -377,6 +382,7 @@ svm_status svm_hinge_loss(const svm_array* S, const int32_t* labels,
                           void* work, int64_t work_bytes, int32_t device,
                           void* stream)
 {
+    ENTRY_BEGIN
     CHECK(check_first(S, "S"));
     if (S->rows > 0 && !labels) return fail(SVM_E_INVALID, "labels is NULL");
     if (!loss) return fail(SVM_E_INVALID, "loss is NULL");
@@ -389,7 +395,6 @@ svm_status svm_hinge_loss(const svm_array* S, const int32_t* labels,
     CHECK(check_work(work, work_bytes,
                      msvm::hinge_bytes(S->rows, S->cols)));
     CHECK(check_ordinal(device));
-    GUARD_BEGIN
     msvm::OnDevice on(device);
     msvm::Pieces ws{static_cast<unsigned char*>(work), true};
     msvm::hinge_loss(*S, labels, (float)scale, or_none(dS), loss, ws,
@@ -403,6 +408,7 @@ svm_status svm_adamw_step(const svm_adamw_tensor* tensors, int32_t n_tensors,
                           const svm_adamw_params* p, int32_t device,
                           void* stream)
 {
+    ENTRY_BEGIN
     if (!p) return fail(SVM_E_INVALID, "params is NULL");
     if (n_tensors < 0) return fail(SVM_E_INVALID, "n_tensors must be >= 0");
     if (n_tensors > 0 && !tensors)
@@ -450,7 +456,6 @@ svm_status svm_adamw_step(const svm_adamw_tensor* tensors, int32_t n_tensors,
                         at + "m, v and master must be aligned to 16 bytes");
     }
     CHECK(check_ordinal(device));
-    GUARD_BEGIN
     msvm::OnDevice on(device);
     msvm::adamw_step(tensors, n_tensors, *p, (hipStream_t)stream);
     HIP_TRY(hipPeekAtLastError());
@@ -463,13 +468,13 @@ svm_status svm_adamw_state(const int8_t* m, const uint8_t* v,
                            int64_t n, float* m_out, float* v_out,
                            int32_t device, void* stream)
 {
+    ENTRY_BEGIN
     if (n < 0 || n > (int64_t)1 << 40)
         return fail(SVM_E_INVALID, "n must be in [0, 2^40]");
     if (n > 0 && ((m_out && (!m || !m_scale)) || (v_out && (!v || !v_scale))))
         return fail(SVM_E_INVALID, "codes or scales are NULL");
     CHECK(check_ordinal(device));
     if (n == 0 || (!m_out && !v_out)) return SVM_OK;
-    GUARD_BEGIN
     msvm::OnDevice on(device);
     msvm::adamw_state(m, v, m_scale, v_scale, n, m_out, v_out,
                       (hipStream_t)stream);

@@ -9,7 +9,7 @@ import pytest
 HERE = os.path.join(os.path.dirname(os.path.abspath(__file__)), "host")
 
 
-def run_driver(tmp_path, name):
+def run_driver(tmp_path, name, more=None):
     from paper_1706_05544_amd import build as b
     cxx = "/opt/rocm/llvm/bin/clang++"
     if not os.path.exists(cxx):
@@ -20,8 +20,9 @@ def run_driver(tmp_path, name):
     for cmd in ([cxx, "-std=c++20", "-O1", "-g", "-Wall",
                  "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include",
                  "-I" + b.INCLUDE, "-I" + b.CSRC,
-                 os.path.join(HERE, name + ".cpp"),
-                 os.path.join(b.CSRC, "layers.cpp"), "-o", exe], [exe]):
+                 os.path.join(HERE, name + ".cpp")] +
+                (more or [os.path.join(b.CSRC, "layers.cpp")]) +
+                ["-o", exe], [exe]):
         r = subprocess.run(cmd, capture_output=True, text=True, timeout=300)
         assert r.returncode == 0, r.stdout + r.stderr
     assert "all checks passed" in r.stdout
@@ -29,3 +30,12 @@ def run_driver(tmp_path, name):
 
 def test_calls_leave_the_threads_device_as_it_was(tmp_path):
     run_driver(tmp_path, "layers_device_driver")
+
+
+def test_no_exception_leaves_a_call_that_finds_no_memory(tmp_path):
+    # (the executable's operator new stands in for the library's)
+    from paper_1706_05544_amd import native as nv
+    nv.load()
+    run_driver(tmp_path, "layers_memory_driver",
+               [nv.LIB_PATH, "-rdynamic",
+                "-Wl,-rpath," + os.path.dirname(nv.LIB_PATH)])
