@@ -81,19 +81,22 @@ struct Args {
 // 16 bytes for each lane from the buffer `rs` at off + soff into LDS, lane
 // after lane.  In assembly, so that the compiler does not wait for loads
 // under way before LDS reads that it takes to depend on them; meet() waits
-// for those that a step needs.  It has no output register; nothing else in
-// this file uses m0 (LDS reads and writes of gfx950 do not).
+// for those that a step needs.  It has no output register, and tells the
+// compiler that m0 (where in LDS the loads go) is overwritten.
 __device__ __forceinline__ void lds_load(intx4 rs, short* lds, uint32_t off,
                                          uint32_t soff)
 {
     const uint32_t to =
         (uint32_t)(uintptr_t)(__attribute__((address_space(3))) short*)lds;
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"  // (m0 is never allocated)
     asm volatile(
         "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
         "buffer_load_dwordx4 %1, %2, %3 offen lds"
         :
         : "s"(to), "v"(off), "s"(rs), "s"(soff)
-        : "memory");
+        : "memory", "m0");
+#pragma clang diagnostic pop
 }
 
 // The lane's share of a factor's tile loads: R rows (ALONG) or columns.
