@@ -522,6 +522,9 @@ def svm_model_get(model: Model, output: int = 0, with_alpha: bool = False):
 # None) and do not wait for it.  A tensor's last dimension is its columns, the
 # rest its rows; inputs whose rows are not at one stride, or whose values in a
 # row are not side by side, are copied first.
+# Outside of autograd: outputs carry no graph, whatever the inputs require;
+# gradients come from the _backward calls.  What a call writes in place is
+# marked as changed, so that autograd sees a tensor that it saved go stale.
 # ---------------------------------------------------------------------------
 
 _ACTS = {"none": SVM_ACT_NONE, "relu": SVM_ACT_RELU, "gelu": SVM_ACT_GELU,
@@ -666,6 +669,12 @@ class _Call:
                 t.record_stream(self.stream)
 
 
+def _written(tensors):
+    """Marks tensors that a call has written in place as changed."""
+    import torch
+    torch.autograd.graph.increment_version(tensors)
+
+
 def _ref(a):
     return None if a is None else ct.byref(a)
 
@@ -677,7 +686,8 @@ def _ptr(t):
 def svm_linear(X, W, bias=None, residual=None, act="none", save: bool = False,
                out=None, stream=None):
     """act(X W^T + bias) + residual -> Y, or (Y, Z) with the pre-activations
-    Z when `save`.  `out` receives Y when given (it may be `residual`)."""
+    Z when `save`.  `out` receives Y when given (it may be `residual`).
+    No autograd graph is made: svm_linear_backward gives the gradients."""
     lib = load()
     c = _Call(X, stream)
     a, w = c.arr(X, "X"), c.arr(W, "W")
@@ -695,6 +705,8 @@ def svm_linear(X, W, bias=None, residual=None, act="none", save: bool = False,
                           _ref(c.arr(Z, "Z", True)), ws, need.value,
                           c.index, c.handle))
     c.done()
+    if out is not None:
+        _written(out)
     return (Y, Z) if save else Y
 
 
@@ -742,6 +754,8 @@ def svm_layer_norm(X, weight=None, bias=None, eps: float = 1e-5,
                               ct.byref(c.arr(Y, "out", True)), _ptr(mean),
                               _ptr(rstd), c.index, c.handle))
     c.done()
+    if out is not None:
+        _written(out)
     return (Y, mean, rstd) if save else Y
 
 
@@ -900,6 +914,7 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
         raise SvmError(SVM_E_UNSUPPORTED, "parameters and gradients must be "
                        "float32, bfloat16 or float16")
     c.keep += params
+    written = c.keep[:]  # (the states, and these)
     c.keep += grads
     tab = np.zeros(len(params), dtype=_ADAMW_ROW)
     tab["param"] = list(map(T.data_ptr, params))
@@ -921,6 +936,7 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
     _check(lib.svm_adamw_step(_np_ptr(tab), len(params), ct.byref(h), c.index,
                               c.handle))
     c.done()
+    _written(written)
 
 
 def svm_adamw_state(m, v, m_scale, v_scale, stream=None):

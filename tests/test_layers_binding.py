@@ -67,3 +67,45 @@ def test_inputs_are_copied_before_the_stream_waits(late):
     p = [torch.randn(n, k), torch.randn(n)]
     nv.svm_adamw_step(p, [x(n, k), v(n)], *nv.svm_adamw_states(p, bits=8))
     assert late == []
+
+
+def test_what_is_written_in_place_is_seen_as_changed(late):
+    # a tensor that autograd saved and a call then wrote over: its gradient
+    # would come from the new values without a word
+    def stale(*written):
+        a = torch.ones((), requires_grad=True)
+        return [(a * x).sum() for x in written]
+
+    X, W, out = torch.ones(4, 6), torch.ones(5, 6), torch.ones(4, 5)
+    p = [torch.ones(5, 6), torch.ones(5)]
+    st = nv.svm_adamw_states(p, bits=8)
+    st32 = nv.svm_adamw_states(p, bits=32)
+    for written, call in (
+            ([out], lambda: nv.svm_linear(X, W, out=out)),
+            ([X], lambda: nv.svm_layer_norm(X, out=X)),
+            (p, lambda: nv.svm_adamw_step(p, [x.clone() for x in p], *st)),
+            ([*p, st32[0], st32[1]], lambda: nv.svm_adamw_step(
+                p, [x.clone() for x in p], *st32))):
+        losses = stale(*written)
+        call()
+        for loss in losses:
+            with pytest.raises(RuntimeError, match="modified by an inplace"):
+                loss.backward()
+    before = [x._version for x in st[:4]]
+    nv.svm_adamw_step(p, [x.clone() for x in p], *st)
+    assert [x._version > b for x, b in zip(st, before)] == [True] * 4
+    # and what is only read is not
+    a = torch.ones((), requires_grad=True)
+    loss = (a * X).sum() + (a * W).sum()
+    nv.svm_linear(X, W)
+    nv.svm_layer_norm(X)
+    loss.backward()
+
+
+def test_parameters_that_require_gradients_are_updated(late):
+    p = [torch.nn.Parameter(torch.ones(5, 6))]
+    nv.svm_adamw_step(p, [torch.ones(5, 6)], *nv.svm_adamw_states(p))
+    with torch.inference_mode():
+        x = torch.ones(3, 6)
+        nv.svm_layer_norm(x, out=x)
+    nv.svm_layer_norm(x, out=x)
