@@ -713,12 +713,18 @@ def svm_linear(X, W, bias=None, residual=None, act="none", save: bool = False,
 def svm_linear_backward(dY, X, W, Z=None, act="none", need=(True, True, True),
                         stream=None):
     """Gradients (dX, dW, dbias) of svm_linear; None where `need` is false.
-    The residual's gradient is dY itself."""
+    The residual's gradient is dY itself.  X may be None without dW, W
+    without dX."""
     lib = load()
     c = _Call(dY, stream)
     g, a, w = c.arr(dY, "dY"), c.arr(X, "X"), c.arr(W, "W")
-    dX = dY.new_empty(X.shape) if need[0] else None
-    dW = dY.new_empty(W.shape) if need[1] else None
+    if (a is None and need[1]) or (w is None and need[0]):
+        raise SvmError(SVM_E_INVALID, "dW needs X, and dX needs W")
+    dX = dW = None
+    if need[0]:
+        dX = dY.new_empty(dY.shape[:-1] + (w.cols,) if a is None else X.shape)
+    if need[1]:
+        dW = dY.new_empty(W.shape if w is not None else (g.cols, a.cols))
     db = dY.new_empty(g.cols) if need[2] else None
     rx, rw, rb = (c.arr(dX, "dX", True), c.arr(dW, "dW", True),
                   c.arr(db, "dbias", True))

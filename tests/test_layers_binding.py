@@ -109,3 +109,18 @@ def test_parameters_that_require_gradients_are_updated(late):
         x = torch.ones(3, 6)
         nv.svm_layer_norm(x, out=x)
     nv.svm_layer_norm(x, out=x)
+
+
+def test_gradients_without_the_factor_that_they_do_not_need(late):
+    dY, X, W = torch.ones(3, 2, 5), torch.ones(3, 2, 7), torch.ones(5, 7)
+    dX, dW, db = nv.svm_linear_backward(dY, None, W, need=(True, False, True))
+    assert dX.shape == X.shape and dW is None and db.shape == (5,)
+    dX, dW, db = nv.svm_linear_backward(dY, X, None, need=(False, True, True))
+    assert dX is None and dW.shape == W.shape and db.shape == (5,)
+    dX, dW, db = nv.svm_linear_backward(dY, None, None,
+                                        need=(False, False, True))
+    assert dX is None and dW is None and db.shape == (5,)
+    for args in ((None, W), (X, None)):
+        with pytest.raises(nv.SvmError) as e:
+            nv.svm_linear_backward(dY, *args)
+        assert e.value.status == nv.SVM_E_INVALID
