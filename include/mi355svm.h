@@ -361,7 +361,8 @@ svm_status svm_tune(const svm_matrix *X, const float *y,
  *     The thread's current device is left as it was.
  *   - All arrays of a call have one type (svm_dtype), except where stated.
  *     Products, sums, statistics and states are held in 32 bits and rounded
- *     to that type once, when they are written (SVM_F32 products are made
+ *     to that type once, when they are written; the one value rounded in
+ *     between is dZ of svm_linear_backward (SVM_F32 products are made
  *     of three 8-bit parts of each factor: as exact as 32-bit products for
  *     factors from 2^-109 (1.5e-33) up to the largest; a smaller one is
  *     held to within 2^-134).
@@ -383,7 +384,8 @@ typedef struct {
 
 typedef enum {
     SVM_ACT_NONE = 0,
-    SVM_ACT_RELU = 1,   /* max(z, 0); its slope at 0 is 0 */
+    SVM_ACT_RELU = 1,   /* max(z, 0), NaN for NaN; its slope is 1 where
+                           z > 0, else 0 (at 0 and for NaN too) */
     SVM_ACT_GELU = 2,   /* z (1 + erf(z / sqrt 2)) / 2 */
     SVM_ACT_SILU = 3,   /* z / (1 + exp(-z)) */
     SVM_ACT_TANH = 4,
@@ -412,7 +414,12 @@ svm_status svm_linear_workspace(const svm_array *X, const svm_array *W,
  * The residual's gradient is dY itself.  Z is what svm_linear wrote (may be
  * NULL for SVM_ACT_NONE).  dX, dW and dbias are nullable: those not asked
  * for cost nothing.  X may be NULL when dW is, W when dX is.  With m = 0,
- * dW and dbias are set to 0. */
+ * dW and dbias are set to 0.
+ * With 16-bit types and an activation, dX and dW are made from dZ rounded to
+ * that type, as the matrix instructions need their factors (dbias from the
+ * unrounded one): each term is off by up to 2^-8 (SVM_BF16) or 2^-11
+ * (SVM_F16) of itself.  In SVM_F16 a dZ past 65504 is infinite and one below
+ * 6e-5 is held in steps of 6e-8: scale the loss so that dZ lies between. */
 svm_status svm_linear_backward(const svm_array *dY, const svm_array *X,
                                const svm_array *W, const svm_array *Z,
                                int32_t act, const svm_array *dX,

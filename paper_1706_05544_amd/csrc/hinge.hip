@@ -3,10 +3,11 @@
 // One read of the scores and one write of their gradient, 8 values of the
 // flattened matrix to a thread; the squares are summed in 64 bits, in a fixed
 // order.  Up to kOneBlock scores one block does it all, in one launch: the
-// launch is then what the call costs (256 x 1: 3.2 us of 12.6); beyond, the
+// launch is then what the call costs (256 x 1: 3.2 us of 11 to 12); beyond, the
 // blocks' sums are joined by a second one.  500000 x 10 in 32 bits: 11.3 us
-// and 2.2 for the join, where 42 MB at a large copy's rate are 8.2: a call so
-// short does not reach that rate.  Whether a score is its row's own class is
+// and 2.2 for the join, where 42 MB at a large copy's rate are 8.2: of the 2048
+// blocks 394 have a second turn, for which the others do not wait but the join
+// does.  Whether a score is its row's own class is
 // found from the flat index (one division, in 32 bits, for 8 scores), so
 // that loads and stores are whole lines for any number of classes.
 #include "elem.hpp"

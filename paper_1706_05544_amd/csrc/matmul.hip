@@ -25,13 +25,13 @@
 // to be finished (bias, activation, residual) and written in whole rows of
 // 16 bytes a lane from a rolled loop.
 //
-// What bounds it: the matrix cores, which this card's power limit slows (a
-// loop of nothing but 16-bit matrix instructions reaches 1630 TFLOP/s, with
-// the LDS reads of these tiles 1521, with their loads as well 1210 to 1340; a
-// large library product reaches 1312).  16384 x 4096 over 4096 in bf16 with
-// bias, gelu, residual and Z: 491 to 502 us, of which the finishing takes
-// some 65, against 433 for a library product alone; 8192^3: 772 us, 1425
-// TFLOP/s where both factors lie across, 832 us where one does.
+// What bounds it: the feeding of the matrix cores, which are at work in half
+// of the cycles.  In a row of a hundred calls, normal values in bf16: 8192^3
+// 795 us, 1380 TFLOP/s, where a factor lies along, 757 us, 1450, where both
+// lie across (a library's product 677 us, 1620; after a pause its first ten
+// calls run at 1290).  16384 x 4096 over 4096: 411 us, 1340 (library 358; 430
+// after a pause), with bias, gelu, residual and Z 483 to 502, of which the
+// finishing takes some 75.
 #include <algorithm>
 #include <cmath>
 
@@ -940,7 +940,8 @@ __global__ __launch_bounds__(256) void k_join(Args p)
 // once), with no LDS between: each is used once, and W is all that counts.
 // Rows may begin anywhere, and 32-bit values are split in registers.
 // Bound by the read of W where W is large, by latency where it is not: 1 x
-// 1024 over 784 in bf16 takes 6.1 us (11.5 with the call around it).
+// 1024 over 784 in bf16 takes 6.1 us (11.5 with the call around it, in 32 bits
+// too); 1 x 4096 over 4096 a call of 11.5 us in bf16, 23.2 in 32 bits.
 constexpr int kFewWaves = 8;
 
 struct FewArgs {
