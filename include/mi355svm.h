@@ -468,9 +468,10 @@ svm_status svm_layer_norm_backward_workspace(int64_t rows, int64_t cols,
  *   dS_ic = -2 scale y_ic max(0, 1 - y_ic S_ic),
  * y_ic = +1 where c is labels[i], else -1; with one column, label 1 is +1
  * and label 0 is -1.  A label outside [0, C) (outside {0, 1} with one
- * column) leaves its row out: it adds nothing and its gradient is 0.  S and
- * dS rows x C, C in [1, 2^21]; dS is nullable and may be S itself.  labels:
- * int32, rows of them; loss: one float; both on the device. */
+ * column) leaves its row out: it adds nothing and its gradient is 0.  2 scale
+ * has to be finite in 32 bits.  S and dS rows x C, C in [1, 2^21]; dS is
+ * nullable and may be S itself.  labels: int32, rows of them; loss: one
+ * float; both on the device. */
 svm_status svm_hinge_loss(const svm_array *S, const int32_t *labels,
                           double scale, const svm_array *dS, float *loss,
                           void *work, int64_t work_bytes, int32_t device,

@@ -386,8 +386,8 @@ svm_status svm_hinge_loss(const svm_array* S, const int32_t* labels,
     CHECK(check_first(S, "S"));
     if (S->rows > 0 && !labels) return fail(SVM_E_INVALID, "labels is NULL");
     if (!loss) return fail(SVM_E_INVALID, "loss is NULL");
-    if (!std::isfinite(scale))
-        return fail(SVM_E_INVALID, "scale must be finite");
+    if (!std::isfinite(2.0f * (float)scale))
+        return fail(SVM_E_INVALID, "2 scale must be finite in 32 bits");
     if (dS) {
         CHECK(check_array(dS, "dS", S->rows, S->cols, S->dtype));
         if (!same(dS, S)) CHECK(check_apart(dS, "dS", {S}));

@@ -295,3 +295,10 @@ def test_rows_of_strided_tensors():
     assert nv._rows_of(b[1:2, :, :3]) == (4, 3, 8)
     assert nv._rows_of(torch.zeros(3, 0, 5)) == (0, 5, 5)
     assert nv._rows_of(torch.zeros(())) is None
+
+
+@pytest.mark.parametrize("scale", [1e39, -1e39, 2e38, 1e300])
+def test_hinge_scale_past_32_bits(scale):
+    # (the slope 2 scale would be infinite, and NaN where the loss is 0)
+    assert hinge(scale=scale) == INV
+    assert nv.svm_last_error()
