@@ -876,7 +876,7 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
                    weight_decay: float = 0.01, step: int = 1,
                    grad_scale: float = 1.0, stream=None):
     """One AdamW step over the tensors `params` (contiguous, updated in
-    place) with the gradients `grads`.  The states are flat tensors as
+    place, no two of them overlapping) with the gradients `grads`.  The states are flat tensors as
     svm_adamw_states makes them: m and v in float32, or int8 and uint8 with
     float32 scales, and optionally the master weights."""
     import torch
