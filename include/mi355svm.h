@@ -532,6 +532,37 @@ svm_status svm_adamw_state(const int8_t *m, const uint8_t *v,
                            int64_t n, float *m_out, float *v_out,
                            int32_t device, void *stream);
 
+/* One tensor of svm_grad_norm: n contiguous values.  n = 0 is allowed. */
+typedef struct {
+    const void *data;
+    int64_t n;
+    int32_t dtype;  /* svm_dtype, each tensor its own */
+} svm_grad;
+
+/* The norm of the gradients of a host array (read during the call), taken as
+ * one vector, and the factor that brings it down to max_norm:
+ *   *norm = |grad_scale| sqrt(sum of all g^2),
+ *   *factor = max_norm / *norm where that is above max_norm, else 1,
+ * one float each on the device; factor is nullable.  Squares and sums are
+ * held in 64 bits.  Where a gradient is NaN or infinite, *norm is not finite
+ * and *factor NaN.  max_norm >= 0, or infinite (a factor of 1 or NaN). */
+svm_status svm_grad_norm(const svm_grad *grads, int32_t n_grads,
+                         double grad_scale, double max_norm, float *norm,
+                         float *factor, void *work, int64_t work_bytes,
+                         int32_t device, void *stream);
+svm_status svm_grad_norm_workspace(const svm_grad *grads, int32_t n_grads,
+                                   int64_t *bytes);
+
+/* svm_adamw_step on clipped gradients: g = (grad_scale *factor) grad, with
+ * the factor (one float, from svm_grad_norm) read on the device as the step
+ * runs.  Where it is not finite nothing is written: the step is left out.
+ * factor NULL: svm_adamw_step. */
+svm_status svm_adamw_step_clipped(const svm_adamw_tensor *tensors,
+                                  int32_t n_tensors,
+                                  const svm_adamw_params *params,
+                                  const float *factor, int32_t device,
+                                  void *stream);
+
 const char *svm_last_error(void);
 
 /* ------------------------------------------------------------------------

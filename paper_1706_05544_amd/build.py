@@ -20,8 +20,8 @@ ARCH = "gfx950"
 DEVICE_SOURCES = ["kernels.hip", "rows.hip", "lockstep.hip", "select.hip",
                   "predict.hip", "noalloc.hip", "iterate.hip", "factor.hip",
                   "resident.hip", "linear.hip", "matmul.hip", "norm.hip", "hinge.hip",
-                  "adamw.hip"]
-HOST_SOURCES = ["solver.cpp", "api.cpp", "layers.cpp"]
+                  "adamw.hip", "gradnorm.hip"]
+HOST_SOURCES = ["solver.cpp", "api.cpp", "layers.cpp", "network.cpp"]
 
 # Packed fp32 instructions are disabled for every compilation that has a
 # device pass (hipcc runs one for the .cpp sources too).

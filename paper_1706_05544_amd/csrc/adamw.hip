@@ -32,6 +32,7 @@ struct AdamConst {
     float rate;            // lr / (1 - b1^t)
     float root;            // 1 / sqrt(1 - b2^t)
     float eps, gscale;
+    const float* factor;   // nullable: multiplies gscale
 };
 
 constexpr float kTiny = 1e-30f;
@@ -173,6 +174,11 @@ __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (t.first[mid] <= blk) lo = mid; else hi = mid - 1;
+    }
+    if (k.factor) {
+        const float f = *k.factor;
+        if (!(fabsf(f) <= kMost)) return;  // the step is left out
+        k.gscale *= f;
     }
     using P = Elem<PT>;
     using G = Elem<GT>;
@@ -318,7 +324,15 @@ void launch_group(const AdamTable& t, const AdamConst& k, int bits,
 void adamw_step(const svm_adamw_tensor* t, int32_t n,
                 const svm_adamw_params& p, hipStream_t s)
 {
+    adamw_step_clipped(t, n, p, nullptr, s);
+}
+
+void adamw_step_clipped(const svm_adamw_tensor* t, int32_t n,
+                        const svm_adamw_params& p, const float* factor,
+                        hipStream_t s)
+{
     AdamConst k;
+    k.factor = factor;
     k.b1 = (float)p.beta1;
     k.c1 = (float)(1.0 - p.beta1);
     k.b2 = (float)p.beta2;

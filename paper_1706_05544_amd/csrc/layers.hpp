@@ -66,8 +66,20 @@ void hinge_loss(const svm_array& S, const int32_t* labels, float scale,
 
 void adamw_step(const svm_adamw_tensor* t, int32_t n,
                 const svm_adamw_params& p, hipStream_t s);
+// ... with the gradients' factor on the device (nullable): where it is not
+// finite the step is left out.
+void adamw_step_clipped(const svm_adamw_tensor* t, int32_t n,
+                        const svm_adamw_params& p, const float* factor,
+                        hipStream_t s);
 void adamw_state(const int8_t* m, const uint8_t* v, const float* ms,
                  const float* vs, int64_t n, float* mo, float* vo,
                  hipStream_t s);
+
+
+// The norm of n gradients as one vector, times |scale|, and the factor that
+// brings it down to `most` (nullable).  Lays out `ws`, and queues with
+// ws.run set.
+void grad_norm(const svm_grad* g, int32_t n, double scale, double most,
+               float* norm, float* factor, Pieces& ws, hipStream_t s);
 
 }  // namespace msvm

@@ -50,7 +50,8 @@ EXPORTS = [
     "svm_linear_backward_workspace", "svm_layer_norm",
     "svm_layer_norm_backward", "svm_layer_norm_backward_workspace",
     "svm_hinge_loss", "svm_hinge_loss_workspace", "svm_adamw_step",
-    "svm_adamw_state",
+    "svm_adamw_state", "svm_grad_norm", "svm_grad_norm_workspace",
+    "svm_adamw_step_clipped",
 ]
 
 
@@ -133,6 +134,11 @@ class svm_adamw_tensor(ct.Structure):
                 ("v", ct.c_void_p), ("m_scale", ct.c_void_p),
                 ("v_scale", ct.c_void_p), ("n", ct.c_int64),
                 ("dtype", ct.c_int32), ("grad_dtype", ct.c_int32)]
+
+
+class svm_grad(ct.Structure):
+    _fields_ = [("data", ct.c_void_p), ("n", ct.c_int64),
+                ("dtype", ct.c_int32)]
 
 
 class svm_adamw_params(ct.Structure):
@@ -220,6 +226,11 @@ def load(path: Optional[str] = None):
     lib.svm_hinge_loss_workspace.argtypes = [i64, i64, P(i64)]
     lib.svm_adamw_step.argtypes = [vp, i32, P(svm_adamw_params), i32, vp]
     lib.svm_adamw_state.argtypes = [vp, vp, vp, vp, i64, vp, vp, i32, vp]
+    f64 = ct.c_double
+    lib.svm_grad_norm.argtypes = [vp, i32, f64, f64, vp, vp, vp, i64, i32, vp]
+    lib.svm_grad_norm_workspace.argtypes = [vp, i32, P(i64)]
+    lib.svm_adamw_step_clipped.argtypes = [vp, i32, P(svm_adamw_params), vp,
+                                           i32, vp]
     for name in EXPORTS:  # fail now, not at first use, if one is missing
         getattr(lib, name)
     _lib = lib
@@ -238,6 +249,11 @@ def _check(rc: int) -> int:
 
 def _is_torch(x) -> bool:
     return type(x).__module__.startswith("torch")
+
+
+def _is_tensor(x) -> bool:
+    import torch
+    return isinstance(x, torch.Tensor)
 
 
 def _torch_sparse_csr():
@@ -874,11 +890,14 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
                    master=None, lr: float = 1e-3, beta1: float = 0.9,
                    beta2: float = 0.999, eps: float = 1e-8,
                    weight_decay: float = 0.01, step: int = 1,
-                   grad_scale: float = 1.0, stream=None):
+                   grad_scale: float = 1.0, factor=None, stream=None):
     """One AdamW step over the tensors `params` (contiguous, updated in
     place, no two of them overlapping) with the gradients `grads`.  The states are flat tensors as
     svm_adamw_states makes them: m and v in float32, or int8 and uint8 with
-    float32 scales, and optionally the master weights."""
+    float32 scales, and optionally the master weights.  `factor`: the clipping
+    factor of svm_grad_norm, a float32 scalar on the device that multiplies
+    the gradients; where it is not finite the step is left out and nothing
+    changes."""
     import torch
     if len(params) != len(grads):
         raise SvmError(SVM_E_INVALID, "params and grads differ in number")
@@ -938,9 +957,14 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
                                  master.data_ptr() + at * 4)
     h = svm_adamw_params(lr, beta1, beta2, eps, weight_decay, grad_scale,
                          step, bits)
+    fp = None if factor is None else c.floats(factor, 1, "factor")
     c.ready()
-    _check(lib.svm_adamw_step(_np_ptr(tab), len(params), ct.byref(h), c.index,
-                              c.handle))
+    if fp is None:
+        _check(lib.svm_adamw_step(_np_ptr(tab), len(params), ct.byref(h),
+                                  c.index, c.handle))
+    else:
+        _check(lib.svm_adamw_step_clipped(_np_ptr(tab), len(params),
+                                          ct.byref(h), fp, c.index, c.handle))
     c.done()
     _written(written)
 
@@ -967,6 +991,50 @@ def svm_adamw_state(m, v, m_scale, v_scale, stream=None):
                                vo.data_ptr(), c.index, c.handle))
     c.done()
     return mo, vo
+
+
+_GRAD_ROW = np.dtype([("data", "u8"), ("n", "i8"), ("dtype", "i4"),
+                      ("pad", "i4")])
+
+
+def svm_grad_norm(grads, max_norm: float = float("inf"),
+                  grad_scale: float = 1.0, stream=None):
+    """The norm of the tensors `grads` taken as one vector, times
+    |grad_scale|, and the factor that brings it down to `max_norm` ->
+    (norm, factor), float32 scalars on the device.  The factor is 1 where the
+    norm is not above `max_norm`, and NaN where a gradient is not finite."""
+    import torch
+    if not len(grads):
+        raise SvmError(SVM_E_INVALID, "there are no gradients")
+    lib = load()
+    c = _Call(grads[0], stream)
+    T = torch.Tensor
+    if not all(map(_is_tensor, grads)) or \
+            set(map(T.get_device, grads)) != {c.index}:
+        raise SvmError(SVM_E_INVALID, "the gradients must be tensors on one "
+                       "device")
+    if not all(map(T.is_contiguous, grads)):
+        grads = [g.contiguous() for g in grads]
+    types = [_DTYPES.get(g.dtype) for g in grads]
+    if None in types:
+        raise SvmError(SVM_E_UNSUPPORTED, "gradients must be float32, bfloat16 "
+                       "or float16")
+    c.keep += grads
+    tab = np.zeros(len(grads), dtype=_GRAD_ROW)
+    tab["data"] = list(map(T.data_ptr, grads))
+    tab["n"] = list(map(T.numel, grads))
+    tab["dtype"] = types
+    norm, factor = c.empty((), torch.float32), c.empty((), torch.float32)
+    size = ct.c_int64()
+    _check(lib.svm_grad_norm_workspace(_np_ptr(tab), len(tab),
+                                       ct.byref(size)))
+    ws = c.work(size.value)
+    c.ready()
+    _check(lib.svm_grad_norm(_np_ptr(tab), len(tab), grad_scale, max_norm,
+                             norm.data_ptr(), factor.data_ptr(), ws,
+                             size.value, c.index, c.handle))
+    c.done()
+    return norm, factor
 
 
 class Solver:
