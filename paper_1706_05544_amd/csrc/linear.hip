@@ -140,8 +140,6 @@ void launch_column_sums(const float* part0, const float* part1, int64_t np,
     });
 }
 
-namespace {
-
 // A factor of a product from an array: as it is where the product can read
 // it so, else a copy in the workspace.
 Factor factor_of(const svm_array& a, bool along, Pieces& ws, hipStream_t s)
@@ -152,6 +150,8 @@ Factor factor_of(const svm_array& a, bool along, Pieces& ws, hipStream_t s)
     if (ws.run) launch_padded(a, copy, ld, s);
     return {copy, ld, along};
 }
+
+namespace {
 
 Epilogue plain(const svm_array& out)
 {

@@ -35,6 +35,10 @@ struct Product {
 // multiple of 8 summed values, or with zeros up to one.
 bool factor_fits(const svm_array& a, bool along);
 
+// A factor of a product from an array: as it is where the product can read
+// it so, else a copy in the workspace.
+Factor factor_of(const svm_array& a, bool along, Pieces& ws, hipStream_t s);
+
 // Queues the product; with ws.run false only counts its workspace.
 void product(const Product& p, Pieces& ws, hipStream_t s);
 

@@ -1,6 +1,7 @@
 // C entry points around a feature network's training step and its serving:
 // argument checks, status codes and dispatch.  Every check comes before any
-// device call; the arithmetic is in gradnorm.hip and adamw.hip.
+// device call; the arithmetic is in gradnorm.hip, adamw.hip and
+// linear4.hip.
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -36,6 +37,53 @@ svm_status check_float(const void* p, const char* name)
     if ((uintptr_t)p % 4)
         return fail(SVM_E_INVALID, std::string(name) + " is not aligned");
     return SVM_OK;
+}
+
+svm_status check_shape4(int64_t rows, int64_t cols, int32_t group,
+                        int32_t dtype)
+{
+    if (rows < 1 || rows > kMaxWidth || cols < 1 || cols > kMaxWidth)
+        return fail(SVM_E_INVALID,
+                    "packed weights: rows and cols must be in [1, 2^21]");
+    if (group != 32 && group != 64 && group != 128)
+        return fail(SVM_E_INVALID,
+                    "packed weights: group must be 32, 64 or 128");
+    if (dtype < SVM_F32 || dtype > SVM_F16)
+        return fail(SVM_E_INVALID, "packed weights: unknown type");
+    return SVM_OK;
+}
+
+svm_status check_packed4(const svm_packed4* w)
+{
+    if (!w) return fail(SVM_E_INVALID, "packed weights are NULL");
+    CHECK(check_shape4(w->rows, w->cols, w->group, w->dtype));
+    if (!w->data) return fail(SVM_E_INVALID, "packed weights have no data");
+    if ((uintptr_t)w->data & 15)
+        return fail(SVM_E_INVALID,
+                    "packed weights must be aligned to 16 bytes");
+    const int64_t need = Shape4(*w).bytes;
+    if (w->bytes < need)
+        return fail(SVM_E_INVALID, "packed weights must have " +
+                                       std::to_string(need) + " bytes, have " +
+                                       std::to_string(w->bytes));
+    return SVM_OK;
+}
+
+// Whether the array has bytes in common with packed weights.
+bool overlap4(const svm_array* a, const svm_packed4* w)
+{
+    if (!a || !a->data || !a->rows) return false;
+    const uintptr_t pa = (uintptr_t)a->data, pw = (uintptr_t)w->data;
+    const uintptr_t na = ((uintptr_t)(a->rows - 1) * a->ld + a->cols) *
+                         dtype_bytes(a->dtype);
+    return pa < pw + (uintptr_t)Shape4(*w).bytes && pw < pa + na;
+}
+
+svm_status check_linear4_inputs(const svm_array* X, const svm_packed4* W)
+{
+    CHECK(check_first(X, "X"));
+    CHECK(check_packed4(W));
+    return check_array(X, "X", X->rows, W->cols, W->dtype);
 }
 
 }  // namespace
@@ -97,6 +145,97 @@ svm_status svm_adamw_step_clipped(const svm_adamw_tensor* tensors,
     CHECK(check_ordinal(device));
     OnDevice on(device);
     adamw_step_clipped(tensors, n_tensors, *p, factor, (hipStream_t)stream);
+    HIP_TRY(hipPeekAtLastError());
+    return SVM_OK;
+    GUARD_END
+}
+
+svm_status svm_pack4_bytes(int64_t rows, int64_t cols, int32_t group,
+                           int32_t dtype, int64_t* bytes)
+{
+    ENTRY_BEGIN
+    if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
+    *bytes = 0;
+    CHECK(check_shape4(rows, cols, group, dtype));
+    *bytes = Shape4(rows, cols, group, dtype).bytes;
+    return SVM_OK;
+    GUARD_END
+}
+
+svm_status svm_pack4(const svm_array* W, const svm_packed4* to, int32_t device,
+                     void* stream)
+{
+    ENTRY_BEGIN
+    CHECK(check_first(W, "W"));
+    CHECK(check_packed4(to));
+    CHECK(check_array(W, "W", to->rows, to->cols, to->dtype));
+    if (overlap4(W, to))
+        return fail(SVM_E_INVALID, "W overlaps the packed weights");
+    CHECK(check_ordinal(device));
+    OnDevice on(device);
+    pack4(*W, *to, (hipStream_t)stream);
+    HIP_TRY(hipPeekAtLastError());
+    return SVM_OK;
+    GUARD_END
+}
+
+svm_status svm_unpack4(const svm_packed4* packed, const svm_array* W,
+                       int32_t device, void* stream)
+{
+    ENTRY_BEGIN
+    CHECK(check_packed4(packed));
+    CHECK(check_array(W, "W", packed->rows, packed->cols, packed->dtype));
+    if (overlap4(W, packed))
+        return fail(SVM_E_INVALID, "W overlaps the packed weights");
+    CHECK(check_ordinal(device));
+    OnDevice on(device);
+    unpack4(*packed, *W, (hipStream_t)stream);
+    HIP_TRY(hipPeekAtLastError());
+    return SVM_OK;
+    GUARD_END
+}
+
+svm_status svm_linear4_workspace(const svm_array* X, const svm_packed4* W,
+                                 int64_t* bytes)
+{
+    ENTRY_BEGIN
+    if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
+    *bytes = 0;
+    CHECK(check_linear4_inputs(X, W));
+    Linear4Call a{*X, *W, kNone, kNone, kNone, SVM_ACT_NONE};
+    Pieces count;
+    linear4(a, count, nullptr);
+    *bytes = count.used;
+    return SVM_OK;
+    GUARD_END
+}
+
+svm_status svm_linear4(const svm_array* X, const svm_packed4* W,
+                       const svm_array* bias, const svm_array* residual,
+                       int32_t act, const svm_array* Y, void* work,
+                       int64_t work_bytes, int32_t device, void* stream)
+{
+    ENTRY_BEGIN
+    CHECK(check_act(act));
+    CHECK(check_linear4_inputs(X, W));
+    const int64_t m = X->rows, n = W->rows;
+    const int32_t t = X->dtype;
+    if (bias) CHECK(check_array(bias, "bias", 1, n, t));
+    if (residual) CHECK(check_array(residual, "residual", m, n, t));
+    CHECK(check_array(Y, "Y", m, n, t));
+    CHECK(check_apart(Y, "Y", {X, bias}));
+    if (overlap4(Y, W))
+        return fail(SVM_E_INVALID, "Y overlaps the packed weights");
+    if (!same(Y, residual)) CHECK(check_apart(Y, "Y", {residual}));
+    Linear4Call a{*X, *W, or_none(bias), or_none(residual), *Y, act};
+    Pieces count;
+    linear4(a, count, nullptr);
+    CHECK(check_work(work, work_bytes, count.used));
+    CHECK(check_ordinal(device));
+    if (m == 0) return SVM_OK;
+    OnDevice on(device);
+    Pieces ws{static_cast<unsigned char*>(work), true};
+    linear4(a, ws, (hipStream_t)stream);
     HIP_TRY(hipPeekAtLastError());
     return SVM_OK;
     GUARD_END

@@ -88,6 +88,110 @@ def test_clipped_step_accepted():
     assert clipped(factor=None) == nv.SVM_E_DEVICE
 
 
+# -------------------------------------------------------- weights in 4 bits
+
+
+def arr(rows, cols, at=1 << 20, ld=None, dtype=nv.SVM_F32, dev=1):
+    return nv.svm_array(at, rows, cols, cols if ld is None else ld, dtype,
+                        dev)
+
+
+def packed(rows=40, cols=100, at=1 << 28, nbytes=1 << 20, group=32,
+           dtype=nv.SVM_F32):
+    return nv.svm_packed4(at, nbytes, rows, cols, group, dtype)
+
+
+BAD_PACKED = [packed(rows=0), packed(cols=0), packed(rows=(1 << 21) + 1),
+              packed(cols=(1 << 21) + 1), packed(group=16), packed(group=96),
+              packed(group=0), packed(dtype=3), packed(dtype=-1),
+              packed(at=None), packed(at=(1 << 28) + 8),
+              # 3 tiles of 16 x 128: 3072 bytes of codes, 4 * 48 scales
+              packed(nbytes=3 * 1024 + 4 * 48 * 4 - 1), packed(nbytes=-1)]
+
+
+def test_pack4_bytes():
+    lib, n = nv.load(), ct.c_int64(-1)
+    for args, want in (((40, 100, 32, 0), 3072 + 4 * 48 * 4),
+                       ((40, 100, 128, 1), 3072 + 48 * 2),
+                       ((1, 1, 64, 2), 1024 + 2 * 16 * 2),
+                       ((1 << 21, 1 << 21, 128, 0), (1 << 41) + (1 << 37))):
+        assert lib.svm_pack4_bytes(*args, ct.byref(n)) == 0
+        assert n.value == want
+    for args in ((0, 1, 32, 0), (1, 0, 32, 0), (1, 1, 33, 0), (1, 1, 32, 3),
+                 ((1 << 21) + 1, 1, 32, 0)):
+        assert lib.svm_pack4_bytes(*args, ct.byref(n)) == INV
+        assert n.value == 0
+    assert lib.svm_pack4_bytes(1, 1, 32, 0, None) == INV
+
+
+def pack(W=None, P=None, device=0, fn="svm_pack4"):
+    W, P = W or arr(40, 100), P or packed()
+    if fn == "svm_pack4":
+        return nv.load().svm_pack4(ref(W), ref(P), device, None)
+    return nv.load().svm_unpack4(ref(P), ref(W), device, None)
+
+
+@pytest.mark.parametrize("fn", ["svm_pack4", "svm_unpack4"])
+def test_pack4_refusals(fn):
+    for P in BAD_PACKED:
+        assert pack(P=P, fn=fn) == INV
+        assert nv.svm_last_error()
+    for W in (arr(40, 99), arr(39, 100), arr(40, 100, dtype=1),
+              arr(40, 100, ld=99), arr(40, 100, at=None),
+              arr(40, 100, at=(1 << 20) + 2), arr(40, 100, at=1 << 28),
+              arr(40, 100, at=(1 << 28) + 3072)):
+        assert pack(W=W, fn=fn) == INV
+    assert pack(W=arr(40, 100, dev=0), fn=fn) == UNS
+    assert pack(device=-1, fn=fn) == INV
+    lib = nv.load()
+    assert lib.svm_pack4(None, ref(packed()), 0, None) == INV
+    assert lib.svm_pack4(ref(arr(40, 100)), None, 0, None) == INV
+    assert lib.svm_unpack4(None, ref(arr(40, 100)), 0, None) == INV
+    assert lib.svm_unpack4(ref(packed()), None, 0, None) == INV
+
+
+def linear4(X=None, P=None, b=None, R=None, act=0, Y=None, work=16,
+            nbytes=1 << 40, device=0):
+    X, P = X or arr(6, 100), P or packed()
+    Y = Y or arr(X.rows, 40, at=3 << 20)
+    return nv.load().svm_linear4(ref(X), ref(P), ref(b), ref(R), act, ref(Y),
+                                 work, nbytes, device, None)
+
+
+@pytest.mark.parametrize("kw", [dict(P=P) for P in BAD_PACKED] + [
+    dict(act=6), dict(act=-1), dict(X=arr(6, 99)), dict(X=arr(-1, 100)),
+    dict(X=arr(6, 100, dtype=1)), dict(X=arr(6, 100, at=None)),
+    dict(b=arr(1, 39, at=4 << 20)), dict(b=arr(40, 1, at=4 << 20)),
+    dict(R=arr(6, 39, at=4 << 20)), dict(Y=arr(6, 39, at=3 << 20)),
+    dict(Y=arr(5, 40, at=3 << 20)), dict(Y=arr(6, 40)),
+    dict(Y=arr(6, 40, at=1 << 28)), dict(R=arr(6, 40, at=(3 << 20) + 16)),
+    dict(R=arr(6, 40, at=3 << 20, ld=41)), dict(device=-1), dict(work=17),
+    # many rows need the unpacked weights
+    dict(X=arr(5000, 100, at=5 << 28), Y=arr(5000, 40, at=6 << 28),
+         work=None)])
+def test_linear4_refusals(kw):
+    assert linear4(**kw) == INV
+    assert nv.svm_last_error()
+
+
+@needs_no_gpu
+def test_packed_weights_accepted():
+    assert pack() == nv.SVM_E_DEVICE
+    assert pack(fn="svm_unpack4") == nv.SVM_E_DEVICE
+    assert linear4() == nv.SVM_E_DEVICE
+    assert linear4(R=arr(6, 40, at=3 << 20)) == nv.SVM_E_DEVICE  # in place
+    assert linear4(X=arr(0, 100, at=None), work=None) == nv.SVM_E_DEVICE
+    assert linear4(P=packed(nbytes=3 * 1024 + 4 * 48 * 4)) == nv.SVM_E_DEVICE
+
+
+def test_packed4_layout_matches_header(tmp_path):
+    S = nv.svm_packed4
+    names = [n for n, _ in S._fields_]
+    got = layout(tmp_path, ["sizeof(svm_packed4)"] + [
+        "offsetof(svm_packed4, %s)" % n for n in names])
+    assert got == [ct.sizeof(S)] + [getattr(S, n).offset for n in names]
+
+
 # ------------------------------------------------------------------ structs
 
 
