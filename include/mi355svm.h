@@ -566,16 +566,16 @@ svm_status svm_adamw_step_clipped(const svm_adamw_tensor *tensors,
 /* The weights of a linear layer in 4 bits, rows x cols, with a scale to each
  * `group` (32, 64 or 128) consecutive inputs of an output.  A weight stands
  * for scale times 0, 0.5, 1, 1.5, 2, 3, 4 or 6 with a sign.  data: device
- * memory, 16-byte aligned, of the bytes that svm_pack4_bytes states, in an
- * order of the library's own; it may be copied and kept, and read by any call
- * with the same rows, cols, group and dtype. */
+ * memory, 16-byte aligned, of the bytes that svm_pack_weights_bytes states, in
+ * an order of the library's own; it may be copied and kept, and read by any
+ * call with the same rows, cols, group and dtype. */
 typedef struct {
     void *data;
     int64_t bytes;       /* of data */
     int64_t rows, cols;  /* outputs, inputs: each in [1, 2^21] */
     int32_t group;       /* 32, 64 or 128 */
     int32_t dtype;       /* svm_dtype of the weights and of the scales */
-} svm_packed4;
+} svm_packed;
 
 /* Rounds the weights W to 4 bits.  A group's scale is a sixth of its largest
  * magnitude, cut to six significant bits (SVM_F16: and to whole steps of
@@ -583,14 +583,14 @@ typedef struct {
  * takes the nearest of the magnitudes, in the middle between two the one with
  * the even place (0, 1, 2, 4).  A weight that is not finite makes all of its
  * group NaN.  to: rows, cols and dtype of W. */
-svm_status svm_pack4(const svm_array *W, const svm_packed4 *to,
-                     int32_t device, void *stream);
-svm_status svm_pack4_bytes(int64_t rows, int64_t cols, int32_t group,
-                           int32_t dtype, int64_t *bytes);
+svm_status svm_pack_weights(const svm_array *W, const svm_packed *to,
+                            int32_t device, void *stream);
+svm_status svm_pack_weights_bytes(int64_t rows, int64_t cols, int32_t group,
+                                  int32_t dtype, int64_t *bytes);
 
 /* What packed weights stand for, exactly: W rows x cols, of their type. */
-svm_status svm_unpack4(const svm_packed4 *packed, const svm_array *W,
-                       int32_t device, void *stream);
+svm_status svm_unpack_weights(const svm_packed *packed, const svm_array *W,
+                              int32_t device, void *stream);
 
 /* One layer on packed weights: Y = act(X W^T + bias) + residual, arrays as in
  * svm_linear.  No weight is rounded further: sums of X times codes over 32
@@ -598,12 +598,13 @@ svm_status svm_unpack4(const svm_packed4 *packed, const svm_array *W,
  * |X| up to 1e36 stays in range).  Made for few rows, whose time is that of
  * reading the weights; many go through svm_linear's products on the unpacked
  * weights, in the workspace.  residual may be Y itself. */
-svm_status svm_linear4(const svm_array *X, const svm_packed4 *W,
-                       const svm_array *bias, const svm_array *residual,
-                       int32_t act, const svm_array *Y, void *work,
-                       int64_t work_bytes, int32_t device, void *stream);
-svm_status svm_linear4_workspace(const svm_array *X, const svm_packed4 *W,
-                                 int64_t *bytes);
+svm_status svm_linear_packed(const svm_array *X, const svm_packed *W,
+                             const svm_array *bias, const svm_array *residual,
+                             int32_t act, const svm_array *Y, void *work,
+                             int64_t work_bytes, int32_t device,
+                             void *stream);
+svm_status svm_linear_packed_workspace(const svm_array *X,
+                                       const svm_packed *W, int64_t *bytes);
 
 const char *svm_last_error(void);
 

@@ -81,23 +81,24 @@ void adamw_state(const int8_t* m, const uint8_t* v, const float* ms,
 struct Shape4 {
     int64_t tiles, chunks, groups, code_bytes, bytes;
     int gshift;
-    explicit Shape4(const svm_packed4& w)
+    explicit Shape4(const svm_packed& w)
         : Shape4(w.rows, w.cols, w.group, w.dtype) {}
     Shape4(int64_t rows, int64_t cols, int32_t group, int32_t dtype)
         : tiles((rows + 15) / 16), chunks((cols + 127) / 128),
           groups(chunks * (128 / group)), code_bytes(tiles * chunks * 1024),
-          bytes(code_bytes + tiles * groups * 16 * (int64_t)dtype_bytes(dtype)),
+          bytes(code_bytes +
+                tiles * groups * 16 * (int64_t)dtype_bytes(dtype)),
           gshift(group == 32 ? 5 : group == 64 ? 6 : 7)
     {
     }
 };
 
-void pack4(const svm_array& W, const svm_packed4& to, hipStream_t s);
-void unpack4(const svm_packed4& w, const svm_array& W, hipStream_t s);
+void pack4(const svm_array& W, const svm_packed& to, hipStream_t s);
+void unpack4(const svm_packed& w, const svm_array& W, hipStream_t s);
 
 struct Linear4Call {
     svm_array X;
-    svm_packed4 W;
+    svm_packed W;
     svm_array bias, residual, Y;  // data NULL: not there
     int32_t act = SVM_ACT_NONE;
 };

@@ -366,12 +366,12 @@ unsigned tile_blocks(int64_t waves)
     return (unsigned)(nb < 16384 ? nb : 16384);
 }
 
-const void* scales_of(const svm_packed4& w)
+const void* scales_of(const svm_packed& w)
 {
     return (const char*)w.data + Shape4(w).code_bytes;
 }
 
-void launch_unpack(const svm_packed4& w, int64_t cols, void* to, int64_t ld,
+void launch_unpack(const svm_packed& w, int64_t cols, void* to, int64_t ld,
                    hipStream_t s)
 {
     const Shape4 sh(w);
@@ -388,7 +388,7 @@ constexpr int64_t kMostFewRows = 64;
 
 }  // namespace
 
-void pack4(const svm_array& W, const svm_packed4& to, hipStream_t s)
+void pack4(const svm_array& W, const svm_packed& to, hipStream_t s)
 {
     const Shape4 sh(to);
     const PackArgs a{W.data, W.ld, to.rows, to.cols, sh.chunks, sh.groups,
@@ -405,7 +405,7 @@ void pack4(const svm_array& W, const svm_packed4& to, hipStream_t s)
     });
 }
 
-void unpack4(const svm_packed4& w, const svm_array& W, hipStream_t s)
+void unpack4(const svm_packed& w, const svm_array& W, hipStream_t s)
 {
     launch_unpack(w, w.cols, W.data, W.ld, s);
 }

@@ -53,7 +53,7 @@ svm_status check_shape4(int64_t rows, int64_t cols, int32_t group,
     return SVM_OK;
 }
 
-svm_status check_packed4(const svm_packed4* w)
+svm_status check_packed4(const svm_packed* w)
 {
     if (!w) return fail(SVM_E_INVALID, "packed weights are NULL");
     CHECK(check_shape4(w->rows, w->cols, w->group, w->dtype));
@@ -70,7 +70,7 @@ svm_status check_packed4(const svm_packed4* w)
 }
 
 // Whether the array has bytes in common with packed weights.
-bool overlap4(const svm_array* a, const svm_packed4* w)
+bool overlap4(const svm_array* a, const svm_packed* w)
 {
     if (!a || !a->data || !a->rows) return false;
     const uintptr_t pa = (uintptr_t)a->data, pw = (uintptr_t)w->data;
@@ -79,7 +79,7 @@ bool overlap4(const svm_array* a, const svm_packed4* w)
     return pa < pw + (uintptr_t)Shape4(*w).bytes && pw < pa + na;
 }
 
-svm_status check_linear4_inputs(const svm_array* X, const svm_packed4* W)
+svm_status check_linear4_inputs(const svm_array* X, const svm_packed* W)
 {
     CHECK(check_first(X, "X"));
     CHECK(check_packed4(W));
@@ -150,8 +150,8 @@ svm_status svm_adamw_step_clipped(const svm_adamw_tensor* tensors,
     GUARD_END
 }
 
-svm_status svm_pack4_bytes(int64_t rows, int64_t cols, int32_t group,
-                           int32_t dtype, int64_t* bytes)
+svm_status svm_pack_weights_bytes(int64_t rows, int64_t cols, int32_t group,
+                                  int32_t dtype, int64_t* bytes)
 {
     ENTRY_BEGIN
     if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
@@ -162,8 +162,8 @@ svm_status svm_pack4_bytes(int64_t rows, int64_t cols, int32_t group,
     GUARD_END
 }
 
-svm_status svm_pack4(const svm_array* W, const svm_packed4* to, int32_t device,
-                     void* stream)
+svm_status svm_pack_weights(const svm_array* W, const svm_packed* to,
+                            int32_t device, void* stream)
 {
     ENTRY_BEGIN
     CHECK(check_first(W, "W"));
@@ -179,8 +179,8 @@ svm_status svm_pack4(const svm_array* W, const svm_packed4* to, int32_t device,
     GUARD_END
 }
 
-svm_status svm_unpack4(const svm_packed4* packed, const svm_array* W,
-                       int32_t device, void* stream)
+svm_status svm_unpack_weights(const svm_packed* packed, const svm_array* W,
+                              int32_t device, void* stream)
 {
     ENTRY_BEGIN
     CHECK(check_packed4(packed));
@@ -195,8 +195,8 @@ svm_status svm_unpack4(const svm_packed4* packed, const svm_array* W,
     GUARD_END
 }
 
-svm_status svm_linear4_workspace(const svm_array* X, const svm_packed4* W,
-                                 int64_t* bytes)
+svm_status svm_linear_packed_workspace(const svm_array* X,
+                                       const svm_packed* W, int64_t* bytes)
 {
     ENTRY_BEGIN
     if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
@@ -210,10 +210,10 @@ svm_status svm_linear4_workspace(const svm_array* X, const svm_packed4* W,
     GUARD_END
 }
 
-svm_status svm_linear4(const svm_array* X, const svm_packed4* W,
-                       const svm_array* bias, const svm_array* residual,
-                       int32_t act, const svm_array* Y, void* work,
-                       int64_t work_bytes, int32_t device, void* stream)
+svm_status svm_linear_packed(const svm_array* X, const svm_packed* W,
+                             const svm_array* bias, const svm_array* residual,
+                             int32_t act, const svm_array* Y, void* work,
+                             int64_t work_bytes, int32_t device, void* stream)
 {
     ENTRY_BEGIN
     CHECK(check_act(act));

@@ -51,8 +51,8 @@ EXPORTS = [
     "svm_layer_norm_backward", "svm_layer_norm_backward_workspace",
     "svm_hinge_loss", "svm_hinge_loss_workspace", "svm_adamw_step",
     "svm_adamw_state", "svm_grad_norm", "svm_grad_norm_workspace",
-    "svm_adamw_step_clipped", "svm_pack4", "svm_pack4_bytes", "svm_unpack4",
-    "svm_linear4", "svm_linear4_workspace",
+    "svm_adamw_step_clipped", "svm_pack_weights", "svm_pack_weights_bytes",
+    "svm_unpack_weights", "svm_linear_packed", "svm_linear_packed_workspace",
 ]
 
 
@@ -142,7 +142,7 @@ class svm_grad(ct.Structure):
                 ("dtype", ct.c_int32)]
 
 
-class svm_packed4(ct.Structure):
+class svm_packed(ct.Structure):
     _fields_ = [("data", ct.c_void_p), ("bytes", ct.c_int64),
                 ("rows", ct.c_int64), ("cols", ct.c_int64),
                 ("group", ct.c_int32), ("dtype", ct.c_int32)]
@@ -238,12 +238,13 @@ def load(path: Optional[str] = None):
     lib.svm_grad_norm_workspace.argtypes = [vp, i32, P(i64)]
     lib.svm_adamw_step_clipped.argtypes = [vp, i32, P(svm_adamw_params), vp,
                                            i32, vp]
-    p4 = P(svm_packed4)
-    lib.svm_pack4.argtypes = [pa, p4, i32, vp]
-    lib.svm_pack4_bytes.argtypes = [i64, i64, i32, i32, P(i64)]
-    lib.svm_unpack4.argtypes = [p4, pa, i32, vp]
-    lib.svm_linear4.argtypes = [pa, p4, pa, pa, i32, pa, vp, i64, i32, vp]
-    lib.svm_linear4_workspace.argtypes = [pa, p4, P(i64)]
+    p4 = P(svm_packed)
+    lib.svm_pack_weights.argtypes = [pa, p4, i32, vp]
+    lib.svm_pack_weights_bytes.argtypes = [i64, i64, i32, i32, P(i64)]
+    lib.svm_unpack_weights.argtypes = [p4, pa, i32, vp]
+    lib.svm_linear_packed.argtypes = [pa, p4, pa, pa, i32, pa, vp, i64, i32,
+                                      vp]
+    lib.svm_linear_packed_workspace.argtypes = [pa, p4, P(i64)]
     for name in EXPORTS:  # fail now, not at first use, if one is missing
         getattr(lib, name)
     _lib = lib
@@ -905,12 +906,12 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
                    weight_decay: float = 0.01, step: int = 1,
                    grad_scale: float = 1.0, factor=None, stream=None):
     """One AdamW step over the tensors `params` (contiguous, updated in
-    place, no two of them overlapping) with the gradients `grads`.  The states are flat tensors as
-    svm_adamw_states makes them: m and v in float32, or int8 and uint8 with
-    float32 scales, and optionally the master weights.  `factor`: the clipping
-    factor of svm_grad_norm, a float32 scalar on the device that multiplies
-    the gradients; where it is not finite the step is left out and nothing
-    changes."""
+    place, no two of them overlapping) with the gradients `grads`.  The states
+    are flat tensors as svm_adamw_states makes them: m and v in float32, or
+    int8 and uint8 with float32 scales, and optionally the master weights.
+    `factor`: the clipping factor of svm_grad_norm, a float32 scalar on the
+    device that multiplies the gradients; where it is not finite the step is
+    left out and nothing changes."""
     import torch
     if len(params) != len(grads):
         raise SvmError(SVM_E_INVALID, "params and grads differ in number")
@@ -1050,11 +1051,11 @@ def svm_grad_norm(grads, max_norm: float = float("inf"),
     return norm, factor
 
 
-class Packed4:
-    """Weights in 4 bits, as svm_pack4 makes them: `data` (uint8, on the
+class PackedWeights:
+    """Weights in 4 bits, as svm_pack_weights makes them: `data` (uint8, on the
     device) in the library's own order, and what it stands for: `shape`
     (outputs, inputs), `group` and `dtype`.  data may be saved and loaded;
-    Packed4(data, shape, group, dtype) makes the weights from it again."""
+    PackedWeights(data, shape, group, dtype) makes them from it again."""
 
     def __init__(self, data, shape, group: int, dtype):
         self.data, self.group, self.dtype = data, int(group), dtype
@@ -1065,42 +1066,42 @@ class Packed4:
                            "tensor of bytes with a shape of two")
 
     def __repr__(self):
-        return "Packed4(%d x %d, groups of %d, %s)" % (
+        return "PackedWeights(%d x %d, groups of %d, %s)" % (
             *self.shape, self.group, self.dtype)
 
 
 def _packed(c, P):
-    """svm_packed4 of a Packed4 on the call's device."""
-    if not isinstance(P, Packed4):
-        raise SvmError(SVM_E_INVALID, "packed weights must be a Packed4")
+    """svm_packed of a PackedWeights on the call's device."""
+    if not isinstance(P, PackedWeights):
+        raise SvmError(SVM_E_INVALID, "packed weights must be a PackedWeights")
     if P.data.get_device() != c.index:
         raise SvmError(SVM_E_INVALID, "the packed weights are on another "
                        "device")
     c.keep.append(P.data)
-    return svm_packed4(P.data.data_ptr(), P.data.numel(), *P.shape, P.group,
+    return svm_packed(P.data.data_ptr(), P.data.numel(), *P.shape, P.group,
                        _DTYPES.get(P.dtype, -1))
 
 
-def svm_pack4(W, group: int = 64, stream=None) -> Packed4:
+def svm_pack_weights(W, group: int = 64, stream=None) -> PackedWeights:
     """The weights W (outputs x inputs) rounded to 4 bits, with a scale to
-    each `group` (32, 64 or 128) inputs of an output, for svm_linear4."""
+    each `group` (32, 64 or 128) inputs of an output, for svm_linear_packed."""
     import torch
     lib = load()
     c = _Call(W, stream)
     a = c.arr(W, "W")
     size = ct.c_int64()
-    _check(lib.svm_pack4_bytes(a.rows, a.cols, group, a.dtype,
+    _check(lib.svm_pack_weights_bytes(a.rows, a.cols, group, a.dtype,
                                ct.byref(size)))
-    P = Packed4(c.empty((size.value,), torch.uint8), (a.rows, a.cols), group,
-                W.dtype)
+    P = PackedWeights(c.empty((size.value,), torch.uint8), (a.rows, a.cols),
+                      group, W.dtype)
     p = _packed(c, P)
     c.ready()
-    _check(lib.svm_pack4(ct.byref(a), ct.byref(p), c.index, c.handle))
+    _check(lib.svm_pack_weights(ct.byref(a), ct.byref(p), c.index, c.handle))
     c.done()
     return P
 
 
-def svm_unpack4(P: Packed4, stream=None):
+def svm_unpack_weights(P: PackedWeights, stream=None):
     """The weights that P stands for, exactly, in their own type."""
     import torch
     lib = load()
@@ -1108,14 +1109,14 @@ def svm_unpack4(P: Packed4, stream=None):
     p = _packed(c, P)
     W = c.empty(P.shape, P.dtype)
     c.ready()
-    _check(lib.svm_unpack4(ct.byref(p), ct.byref(c.arr(W, "W", True)),
+    _check(lib.svm_unpack_weights(ct.byref(p), ct.byref(c.arr(W, "W", True)),
                            c.index, c.handle))
     c.done()
     return W
 
 
-def svm_linear4(X, P: Packed4, bias=None, residual=None, act="none", out=None,
-                stream=None):
+def svm_linear_packed(X, P: PackedWeights, bias=None, residual=None,
+                      act="none", out=None, stream=None):
     """act(X W^T + bias) + residual on weights in 4 bits -> Y.  `out`
     receives Y when given (it may be `residual`)."""
     lib = load()
@@ -1123,12 +1124,12 @@ def svm_linear4(X, P: Packed4, bias=None, residual=None, act="none", out=None,
     a, p = c.arr(X, "X"), _packed(c, P)
     Y = out if out is not None else X.new_empty(X.shape[:-1] + (p.rows,))
     need = ct.c_int64()
-    _check(lib.svm_linear4_workspace(ct.byref(a), ct.byref(p),
+    _check(lib.svm_linear_packed_workspace(ct.byref(a), ct.byref(p),
                                      ct.byref(need)))
     ws = c.work(need.value)
     b, r = c.arr(bias, "bias"), c.arr(residual, "residual")
     c.ready()
-    _check(lib.svm_linear4(ct.byref(a), ct.byref(p), _ref(b), _ref(r),
+    _check(lib.svm_linear_packed(ct.byref(a), ct.byref(p), _ref(b), _ref(r),
                            _act(act), ct.byref(c.arr(Y, "out", True)), ws,
                            need.value, c.index, c.handle))
     c.done()

@@ -63,13 +63,13 @@ def same_values(a, b):
 
 @pytest.mark.parametrize("t", list(TYPES))
 @pytest.mark.parametrize("group", [32, 64, 128])
-@pytest.mark.parametrize("n,k", [(1, 1), (1, 31), (3, 33), (15, 127), (16, 128),
-                                 (17, 129), (10, 784), (333, 501), (70, 4097)])
+@pytest.mark.parametrize("n,k", [(1, 1), (1, 31), (3, 33), (15, 127),
+                                 (16, 128), (17, 129), (10, 784), (333, 501), (70, 4097)])
 def test_pack_and_unpack(n, k, group, t):
     W = rnd(gen(n * k + group), n, k, by=k ** -0.5, t=t)
-    P = nv.svm_pack4(W, group)
+    P = nv.svm_pack_weights(W, group)
     assert P.shape == (n, k) and P.dtype == W.dtype
-    got = nv.svm_unpack4(P)
+    got = nv.svm_unpack_weights(P)
     assert got.dtype == W.dtype and got.shape == W.shape
     assert same_values(got.cpu().double(), held(W, group)[0])
     # the largest magnitude of a group is held to within a sixth
@@ -99,7 +99,8 @@ def test_pack_borders_and_ends_of_the_range(t):
     W[12, 5], W[12, 40] = -math.inf, 2.0
     W = W.to(TYPES[t]).to(DEV)
     for group in (32, 64):
-        got = nv.svm_unpack4(nv.svm_pack4(W, group)).cpu().double()
+        P = nv.svm_pack_weights(W, group)
+        got = nv.svm_unpack_weights(P).cpu().double()
         want = held(W, group)[0]
         assert same_values(got, want)
         assert got[10:13, :32].isnan().all()
@@ -113,7 +114,8 @@ def test_pack_strided(t):
     g = gen(5)
     B = rnd(g, 40, 300, t=t)
     for W in (B[:, 3:203], B[::2, :77], B.t(), B[:, ::3]):
-        a, b = nv.svm_pack4(W, 32), nv.svm_pack4(W.contiguous(), 32)
+        a = nv.svm_pack_weights(W, 32)
+        b = nv.svm_pack_weights(W.contiguous(), 32)
         assert torch.equal(a.data, b.data)
 
 
@@ -128,8 +130,8 @@ def act64(name, z):
 
 
 def check(X, P, b, R, act, t, W=None, **kw):
-    Y = nv.svm_linear4(X, P, b, R, act=act, **kw)
-    W = nv.svm_unpack4(P) if W is None else W
+    Y = nv.svm_linear_packed(X, P, b, R, act=act, **kw)
+    W = nv.svm_unpack_weights(P) if W is None else W
     x, w = X.double().reshape(-1, X.shape[-1]), W.double()
     z, mag = x @ w.t(), x.abs() @ w.abs().t()
     if b is not None:
@@ -157,7 +159,7 @@ def test_rows(m, t):
         g = gen(m * 7 + n)
         X, W = rnd(g, m, k, t=t), rnd(g, n, k, by=k ** -0.5, t=t)
         b, R = rnd(g, n, t=t), rnd(g, m, n, t=t)
-        P = nv.svm_pack4(W, group)
+        P = nv.svm_pack_weights(W, group)
         check(X, P, b, R, "gelu", t)
         check(X, P, None, None, "none", t)
 
@@ -170,7 +172,7 @@ def test_inputs(k, t):
     n = 50
     W = rnd(g, n, k, by=k ** -0.5, t=t)
     for group in (32, 128):
-        P = nv.svm_pack4(W, group)
+        P = nv.svm_pack_weights(W, group)
         for m in (1, 3, 20):
             check(rnd(g, m, k, t=t), P, rnd(g, n, t=t), None, "silu", t)
 
@@ -183,7 +185,7 @@ def test_acts(m, act, t):
     g = gen(m)
     X, W = rnd(g, m, 100, t=t), rnd(g, 72, 100, by=0.2, t=t)
     b, R = rnd(g, 72, t=t), rnd(g, m, 72, t=t)
-    P = nv.svm_pack4(W, 32)
+    P = nv.svm_pack_weights(W, 32)
     check(X, P, b, R, act, t)
     check(X, P, b, None, act, t)
     check(X, P, None, R, act, t)
@@ -197,7 +199,7 @@ def test_large(m, k, n, t):
     g = gen(m + k)
     X, W = rnd(g, m, k, t=t), rnd(g, n, k, by=k ** -0.5, t=t)
     b, R = rnd(g, n, t=t), rnd(g, m, n, t=t)
-    check(X, nv.svm_pack4(W, 64), b, R, "gelu", t)
+    check(X, nv.svm_pack_weights(W, 64), b, R, "gelu", t)
 
 
 @pytest.mark.parametrize("t", list(TYPES))
@@ -205,7 +207,7 @@ def test_large(m, k, n, t):
 def test_strides_in_place_and_nothing_beside(m, t):
     g = gen(m + 1)
     k, n = 100, 90
-    P = nv.svm_pack4(rnd(g, n, k, by=0.1, t=t), 32)
+    P = nv.svm_pack_weights(rnd(g, n, k, by=0.1, t=t), 32)
     for shift in (0, 1, 3, 8):
         X = rnd(g, m, k + 29, t=t)[:, shift:shift + k]
         R = rnd(g, m, n + 13, t=t)[:, shift:shift + n]
@@ -218,28 +220,28 @@ def test_strides_in_place_and_nothing_beside(m, t):
         assert bool((out[rest] == 7.0).all())
         want = o.clone()
         o.copy_(R)
-        nv.svm_linear4(X, P, b, o, act="tanh", out=o)
+        nv.svm_linear_packed(X, P, b, o, act="tanh", out=o)
         assert torch.equal(o, want)
     # a transposed input, leading dimensions, one row without any
     X = rnd(g, k, m, t=t).t()
     Y = check(X, P, None, None, "none", t)
-    Y3 = nv.svm_linear4(X.reshape(1, m, 1, k), P)
+    Y3 = nv.svm_linear_packed(X.reshape(1, m, 1, k), P)
     assert Y3.shape == (1, m, 1, n) and torch.equal(Y3.view(m, n), Y)
-    assert nv.svm_linear4(X[0].contiguous(), P).shape == (n,)
+    assert nv.svm_linear_packed(X[0].contiguous(), P).shape == (n,)
 
 
 @pytest.mark.parametrize("t", list(TYPES))
 def test_rows_do_not_depend_on_each_other(t):
     # an infinity or NaN in a row stays there, and shows; no rows are allowed
     g = gen(11)
-    P = nv.svm_pack4(rnd(g, 60, 200, by=0.1, t=t), 32)
-    W = nv.svm_unpack4(P).double()
+    P = nv.svm_pack_weights(rnd(g, 60, 200, by=0.1, t=t), 32)
+    W = nv.svm_unpack_weights(P).double()
     for m in (4, 16, 40, 80):
         X = rnd(g, m, 200, t=t)
-        clean = nv.svm_linear4(X, P)
+        clean = nv.svm_linear_packed(X, P)
         bad = X.clone()
         bad[1, 199], bad[2, 5] = math.nan, math.inf
-        got = nv.svm_linear4(bad, P)
+        got = nv.svm_linear_packed(bad, P)
         keep = [i for i in range(m) if i not in (1, 2)]
         assert torch.equal(got[keep], clean[keep])
         assert bool(got[1].isnan().all())
@@ -247,16 +249,16 @@ def test_rows_do_not_depend_on_each_other(t):
         w = W[:, 5]
         assert bool((got[2].double() == w * math.inf)[w != 0].all())
         assert bool(got[2][w == 0].isnan().all())
-    assert nv.svm_linear4(X[:0], P).shape == (0, 60)
+    assert nv.svm_linear_packed(X[:0], P).shape == (0, 60)
 
 
 def test_a_group_that_is_not_a_number_shows_in_its_output_alone():
     g = gen(12)
     W = rnd(g, 40, 100)
     W[7, 50] = math.nan
-    P = nv.svm_pack4(W, 32)
+    P = nv.svm_pack_weights(W, 32)
     for m in (1, 10, 100):
-        Y = nv.svm_linear4(rnd(g, m, 100), P)
+        Y = nv.svm_linear_packed(rnd(g, m, 100), P)
         assert bool(Y[:, 7].isnan().all())
         assert not bool(Y[:, :7].isnan().any() or Y[:, 8:].isnan().any())
 
@@ -267,13 +269,13 @@ def test_32_bit_inputs_keep_all_their_bits():
     k = 64
     W = torch.zeros(k, 128, device=DEV)
     W[:, :64].fill_diagonal_(6.0)
-    P = nv.svm_pack4(W, 64)
+    P = nv.svm_pack_weights(W, 64)
     g = gen(13)
     for m in (1, 16, 33):
         x = torch.randn(m, 128, generator=g, device=DEV)
         x[:, 64:] = 0.0
         for by in (1.0, 2.0 ** -100, 2.0 ** 115):
-            Y = nv.svm_linear4(x * by, P).double()
+            Y = nv.svm_linear_packed(x * by, P).double()
             want = x[:, :64].double() * by * 6.0
             assert bool(((Y - want).abs() <= 2 * E * want.abs()).all())
 
@@ -281,26 +283,26 @@ def test_32_bit_inputs_keep_all_their_bits():
 def test_streams_and_replays():
     g = gen(14)
     W, R = rnd(g, 300, 260, t="bf16"), rnd(g, 300, 90, t="bf16").t()
-    P = nv.svm_pack4(W, 64)
+    P = nv.svm_pack_weights(W, 64)
     X = {m: rnd(g, 260, m, t="bf16").t() for m in (2, 30, 90)}
     side = torch.cuda.Stream()
     for m, x in X.items():
-        want = nv.svm_linear4(x, P, None, R[:m], act="gelu")
-        Q = nv.svm_pack4(W, 64, stream=side)
-        got = nv.svm_linear4(x, Q, None, R[:m], act="gelu", stream=side)
-        back = nv.svm_unpack4(Q, stream=side)
+        want = nv.svm_linear_packed(x, P, None, R[:m], act="gelu")
+        Q = nv.svm_pack_weights(W, 64, stream=side)
+        got = nv.svm_linear_packed(x, Q, None, R[:m], act="gelu", stream=side)
+        back = nv.svm_unpack_weights(Q, stream=side)
         side.synchronize()
         assert torch.equal(got, want)
         assert torch.equal(Q.data, P.data)
-        assert torch.equal(back, nv.svm_unpack4(P))
+        assert torch.equal(back, nv.svm_unpack_weights(P))
         torch.cuda.synchronize()
         xc = x.contiguous()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
-            out = nv.svm_linear4(xc, P, None, R[:m], act="gelu")
+            out = nv.svm_linear_packed(xc, P, None, R[:m], act="gelu")
         for turn in range(4):
             xc.mul_(0.9)
-            eager = nv.svm_linear4(xc, P, None, R[:m], act="gelu")
+            eager = nv.svm_linear_packed(xc, P, None, R[:m], act="gelu")
             torch.cuda.synchronize()
             graph.replay()
             torch.cuda.synchronize()
@@ -316,46 +318,46 @@ def test_offsets_past_32_bits():
     W = torch.empty(n, k, dtype=torch.bfloat16, device=DEV)
     for i in range(0, n, 500):
         W[i:i + 500] = rows
-    P = nv.svm_pack4(W, 128)
+    P = nv.svm_pack_weights(W, 128)
     assert P.data.numel() > 1 << 31
-    part = nv.svm_pack4(rows, 128)
-    w = nv.svm_unpack4(part)
+    part = nv.svm_pack_weights(rows, 128)
+    w = nv.svm_unpack_weights(part)
     for m in (1, 20):
         X = rnd(g, m, k, t="bf16")
-        Y = nv.svm_linear4(X, P)
-        want = nv.svm_linear4(X, part)
+        Y = nv.svm_linear_packed(X, P)
+        want = nv.svm_linear_packed(X, part)
         assert torch.equal(Y, want.repeat(1, n // 500))
     W.zero_()
-    back = nv.svm_unpack4(P)
+    back = nv.svm_unpack_weights(P)
     for i in (0, 20000, n - 500):
         assert torch.equal(back[i:i + 500], w)
 
 
 def test_packed_weights_are_made_again_from_their_bytes():
     g = gen(16)
-    P = nv.svm_pack4(rnd(g, 50, 70), 32)
-    Q = nv.Packed4(P.data.cpu().to(DEV), [50, 70], 32, torch.float32)
+    P = nv.svm_pack_weights(rnd(g, 50, 70), 32)
+    Q = nv.PackedWeights(P.data.cpu().to(DEV), [50, 70], 32, torch.float32)
     X = rnd(g, 3, 70)
-    assert torch.equal(nv.svm_linear4(X, P), nv.svm_linear4(X, Q))
-    short = nv.Packed4(P.data[:-16], P.shape, 32, torch.float32)
+    assert torch.equal(nv.svm_linear_packed(X, P), nv.svm_linear_packed(X, Q))
+    short = nv.PackedWeights(P.data[:-16], P.shape, 32, torch.float32)
     for call, code in (
-            (lambda: nv.svm_linear4(X, short), nv.SVM_E_INVALID),
-            (lambda: nv.svm_unpack4(short), nv.SVM_E_INVALID),
-            (lambda: nv.svm_linear4(X.half(), P), nv.SVM_E_INVALID),
-            (lambda: nv.svm_linear4(X[:, :69], P), nv.SVM_E_INVALID),
-            (lambda: nv.svm_linear4(X, X), nv.SVM_E_INVALID),
-            (lambda: nv.svm_linear4(X, nv.Packed4(
+            (lambda: nv.svm_linear_packed(X, short), nv.SVM_E_INVALID),
+            (lambda: nv.svm_unpack_weights(short), nv.SVM_E_INVALID),
+            (lambda: nv.svm_linear_packed(X.half(), P), nv.SVM_E_INVALID),
+            (lambda: nv.svm_linear_packed(X[:, :69], P), nv.SVM_E_INVALID),
+            (lambda: nv.svm_linear_packed(X, X), nv.SVM_E_INVALID),
+            (lambda: nv.svm_linear_packed(X, nv.PackedWeights(
                 P.data.cpu(), P.shape, 32, torch.float32)), nv.SVM_E_INVALID),
-            (lambda: nv.svm_linear4(X, nv.Packed4(
+            (lambda: nv.svm_linear_packed(X, nv.PackedWeights(
                 P.data, P.shape, 48, torch.float32)), nv.SVM_E_INVALID),
-            (lambda: nv.svm_linear4(X, nv.Packed4(
+            (lambda: nv.svm_linear_packed(X, nv.PackedWeights(
                 P.data, P.shape, 32, torch.float64)), nv.SVM_E_INVALID),
-            (lambda: nv.Packed4(P.data[::2], P.shape, 32, torch.float32),
+            (lambda: nv.PackedWeights(P.data[::2], P.shape, 32, torch.float32),
              nv.SVM_E_INVALID),
-            (lambda: nv.svm_pack4(X, 48), nv.SVM_E_INVALID),
-            (lambda: nv.svm_pack4(X.cpu()), nv.SVM_E_UNSUPPORTED),
-            (lambda: nv.svm_linear4(X, P, act="swish"), nv.SVM_E_INVALID),
-            (lambda: nv.svm_linear4(X, P, out=torch.empty(
+            (lambda: nv.svm_pack_weights(X, 48), nv.SVM_E_INVALID),
+            (lambda: nv.svm_pack_weights(X.cpu()), nv.SVM_E_UNSUPPORTED),
+            (lambda: nv.svm_linear_packed(X, P, act="swish"), nv.SVM_E_INVALID),
+            (lambda: nv.svm_linear_packed(X, P, out=torch.empty(
                 3, 49, device=DEV)), nv.SVM_E_INVALID)):
         with pytest.raises(nv.SvmError) as e:
             call()

@@ -98,7 +98,7 @@ def arr(rows, cols, at=1 << 20, ld=None, dtype=nv.SVM_F32, dev=1):
 
 def packed(rows=40, cols=100, at=1 << 28, nbytes=1 << 20, group=32,
            dtype=nv.SVM_F32):
-    return nv.svm_packed4(at, nbytes, rows, cols, group, dtype)
+    return nv.svm_packed(at, nbytes, rows, cols, group, dtype)
 
 
 BAD_PACKED = [packed(rows=0), packed(cols=0), packed(rows=(1 << 21) + 1),
@@ -115,23 +115,23 @@ def test_pack4_bytes():
                        ((40, 100, 128, 1), 3072 + 48 * 2),
                        ((1, 1, 64, 2), 1024 + 2 * 16 * 2),
                        ((1 << 21, 1 << 21, 128, 0), (1 << 41) + (1 << 37))):
-        assert lib.svm_pack4_bytes(*args, ct.byref(n)) == 0
+        assert lib.svm_pack_weights_bytes(*args, ct.byref(n)) == 0
         assert n.value == want
     for args in ((0, 1, 32, 0), (1, 0, 32, 0), (1, 1, 33, 0), (1, 1, 32, 3),
                  ((1 << 21) + 1, 1, 32, 0)):
-        assert lib.svm_pack4_bytes(*args, ct.byref(n)) == INV
+        assert lib.svm_pack_weights_bytes(*args, ct.byref(n)) == INV
         assert n.value == 0
-    assert lib.svm_pack4_bytes(1, 1, 32, 0, None) == INV
+    assert lib.svm_pack_weights_bytes(1, 1, 32, 0, None) == INV
 
 
-def pack(W=None, P=None, device=0, fn="svm_pack4"):
+def pack(W=None, P=None, device=0, fn="svm_pack_weights"):
     W, P = W or arr(40, 100), P or packed()
-    if fn == "svm_pack4":
-        return nv.load().svm_pack4(ref(W), ref(P), device, None)
-    return nv.load().svm_unpack4(ref(P), ref(W), device, None)
+    if fn == "svm_pack_weights":
+        return nv.load().svm_pack_weights(ref(W), ref(P), device, None)
+    return nv.load().svm_unpack_weights(ref(P), ref(W), device, None)
 
 
-@pytest.mark.parametrize("fn", ["svm_pack4", "svm_unpack4"])
+@pytest.mark.parametrize("fn", ["svm_pack_weights", "svm_unpack_weights"])
 def test_pack4_refusals(fn):
     for P in BAD_PACKED:
         assert pack(P=P, fn=fn) == INV
@@ -144,18 +144,18 @@ def test_pack4_refusals(fn):
     assert pack(W=arr(40, 100, dev=0), fn=fn) == UNS
     assert pack(device=-1, fn=fn) == INV
     lib = nv.load()
-    assert lib.svm_pack4(None, ref(packed()), 0, None) == INV
-    assert lib.svm_pack4(ref(arr(40, 100)), None, 0, None) == INV
-    assert lib.svm_unpack4(None, ref(arr(40, 100)), 0, None) == INV
-    assert lib.svm_unpack4(ref(packed()), None, 0, None) == INV
+    assert lib.svm_pack_weights(None, ref(packed()), 0, None) == INV
+    assert lib.svm_pack_weights(ref(arr(40, 100)), None, 0, None) == INV
+    assert lib.svm_unpack_weights(None, ref(arr(40, 100)), 0, None) == INV
+    assert lib.svm_unpack_weights(ref(packed()), None, 0, None) == INV
 
 
 def linear4(X=None, P=None, b=None, R=None, act=0, Y=None, work=16,
             nbytes=1 << 40, device=0):
     X, P = X or arr(6, 100), P or packed()
     Y = Y or arr(X.rows, 40, at=3 << 20)
-    return nv.load().svm_linear4(ref(X), ref(P), ref(b), ref(R), act, ref(Y),
-                                 work, nbytes, device, None)
+    return nv.load().svm_linear_packed(ref(X), ref(P), ref(b), ref(R), act,
+                                       ref(Y), work, nbytes, device, None)
 
 
 @pytest.mark.parametrize("kw", [dict(P=P) for P in BAD_PACKED] + [
@@ -177,7 +177,7 @@ def test_linear4_refusals(kw):
 @needs_no_gpu
 def test_packed_weights_accepted():
     assert pack() == nv.SVM_E_DEVICE
-    assert pack(fn="svm_unpack4") == nv.SVM_E_DEVICE
+    assert pack(fn="svm_unpack_weights") == nv.SVM_E_DEVICE
     assert linear4() == nv.SVM_E_DEVICE
     assert linear4(R=arr(6, 40, at=3 << 20)) == nv.SVM_E_DEVICE  # in place
     assert linear4(X=arr(0, 100, at=None), work=None) == nv.SVM_E_DEVICE
@@ -185,10 +185,10 @@ def test_packed_weights_accepted():
 
 
 def test_packed4_layout_matches_header(tmp_path):
-    S = nv.svm_packed4
+    S = nv.svm_packed
     names = [n for n, _ in S._fields_]
-    got = layout(tmp_path, ["sizeof(svm_packed4)"] + [
-        "offsetof(svm_packed4, %s)" % n for n in names])
+    got = layout(tmp_path, ["sizeof(svm_packed)"] + [
+        "offsetof(svm_packed, %s)" % n for n in names])
     assert got == [ct.sizeof(S)] + [getattr(S, n).offset for n in names]
 
 
