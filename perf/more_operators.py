@@ -212,7 +212,7 @@ def prepare(case, seed):
     s["codes"], s["scales"] = _to4(W, c["group"])
     if own:
         from paper_1706_05544_amd import native as nv
-        s["packed"] = nv.svm_pack4(W, c["group"])
+        s["packed"] = nv.svm_pack_weights(W, c["group"])
     return s
 
 
@@ -396,7 +396,8 @@ def _library(s):
         return nv.svm_group_norm_backward(
             s["dY"], s["X"], c["groups"], s["mean"], s["rstd"], s["w"],
             s["b"], act=c["act"], residual=s["res"])
-    return nv.svm_linear4(s["X"], s["packed"], s["b"], s["R"], act=c["act"])
+    return nv.svm_linear_packed(s["X"], s["packed"], s["b"], s["R"],
+                                act=c["act"])
 
 
 def run(state):
