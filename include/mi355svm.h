@@ -532,6 +532,43 @@ svm_status svm_adamw_state(const int8_t *m, const uint8_t *v,
                            int64_t n, float *m_out, float *v_out,
                            int32_t device, void *stream);
 
+/* Group norm with an activation, channels last.  X has `positions` rows to a
+ * sample and cols channels in `groups` groups of consecutive ones; for each
+ * sample and group, over its positions and channels,
+ *   y = act((x - mean) rstd weight + bias),
+ *   rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
+ * rows a multiple of positions (>= 1), cols of groups.  weight and bias
+ * (1 x cols) are nullable (1 and 0).  mean and rstd (samples x groups floats,
+ * nullable) receive the statistics that the gradient needs.  Y may be X
+ * itself (same data and ld). */
+svm_status svm_group_norm(const svm_array *X, int64_t positions,
+                          int64_t groups, const svm_array *weight,
+                          const svm_array *bias, double eps, int32_t act,
+                          const svm_array *Y, float *mean, float *rstd,
+                          void *work, int64_t work_bytes, int32_t device,
+                          void *stream);
+svm_status svm_group_norm_workspace(int64_t rows, int64_t positions,
+                                    int64_t cols, int64_t groups,
+                                    int32_t dtype, int64_t *bytes);
+
+/* Its gradients: with xh = (x - mean) rstd, dZ = dY act'(xh weight + bias)
+ * and a = dZ weight, means over a sample's group,
+ *   dX = rstd (a - mean(a) - xh mean(a xh)) + residual,
+ *   dweight = sum over rows of dZ xh,  dbias = sum over rows of dZ.
+ * residual (rows x cols, nullable): the gradient that reaches X past the
+ * norm.  dX, dweight and dbias are nullable; dX may be dY or the residual
+ * itself.  With no rows dweight and dbias are set to 0. */
+svm_status svm_group_norm_backward(
+    const svm_array *dY, const svm_array *X, int64_t positions,
+    int64_t groups, const float *mean, const float *rstd,
+    const svm_array *weight, const svm_array *bias, int32_t act,
+    const svm_array *residual, const svm_array *dX, const svm_array *dweight,
+    const svm_array *dbias, void *work, int64_t work_bytes, int32_t device,
+    void *stream);
+svm_status svm_group_norm_backward_workspace(int64_t rows, int64_t positions,
+                                             int64_t cols, int64_t groups,
+                                             int32_t dtype, int64_t *bytes);
+
 /* One tensor of svm_grad_norm: n contiguous values.  n = 0 is allowed. */
 typedef struct {
     const void *data;

@@ -20,7 +20,8 @@ ARCH = "gfx950"
 DEVICE_SOURCES = ["kernels.hip", "rows.hip", "lockstep.hip", "select.hip",
                   "predict.hip", "noalloc.hip", "iterate.hip", "factor.hip",
                   "resident.hip", "linear.hip", "matmul.hip", "norm.hip", "hinge.hip",
-                  "adamw.hip", "gradnorm.hip", "linear4.hip"]
+                  "adamw.hip", "gradnorm.hip", "linear4.hip",
+                  "groupnorm.hip"]
 HOST_SOURCES = ["solver.cpp", "api.cpp", "layers.cpp", "network.cpp"]
 
 # Packed fp32 instructions are disabled for every compilation that has a

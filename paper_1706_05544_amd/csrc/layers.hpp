@@ -76,6 +76,25 @@ void adamw_state(const int8_t* m, const uint8_t* v, const float* ms,
                  hipStream_t s);
 
 
+struct GroupCall {
+    svm_array X, weight, bias, Y;  // data NULL: not there
+    int64_t positions = 1, groups = 1;
+    float eps = 0.0f;
+    int32_t act = SVM_ACT_NONE;
+    float *mean = nullptr, *rstd = nullptr;
+};
+// Lays out the workspace in `ws`; with ws.run set it queues the work too.
+void group_norm(const GroupCall& c, Pieces& ws, hipStream_t s);
+
+struct GroupGradCall {
+    svm_array dY, X, weight, bias, residual, dX, dweight, dbias;
+    int64_t positions = 1, groups = 1;
+    int32_t act = SVM_ACT_NONE;
+    const float *mean = nullptr, *rstd = nullptr;
+    bool sums = false;  // dweight or dbias is asked for
+};
+void group_norm_backward(const GroupGradCall& c, Pieces& ws, hipStream_t s);
+
 // Sizes of weights in 4 bits: tiles of 16 outputs, chunks of 128 inputs,
 // groups of a tile row, bytes of the codes and of all.
 struct Shape4 {

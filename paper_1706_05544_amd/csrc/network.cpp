@@ -1,7 +1,7 @@
 // C entry points around a feature network's training step and its serving:
 // argument checks, status codes and dispatch.  Every check comes before any
-// device call; the arithmetic is in gradnorm.hip, adamw.hip and
-// linear4.hip.
+// device call; the arithmetic is in gradnorm.hip, adamw.hip,
+// linear4.hip and groupnorm.hip.
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -84,6 +84,21 @@ svm_status check_linear4_inputs(const svm_array* X, const svm_packed* W)
     CHECK(check_first(X, "X"));
     CHECK(check_packed4(W));
     return check_array(X, "X", X->rows, W->cols, W->dtype);
+}
+
+// rows positions in samples of `positions`, cols channels in groups
+svm_status check_groups(int64_t rows, int64_t positions, int64_t cols,
+                        int64_t groups)
+{
+    if (rows < 0 || rows > ((int64_t)1 << 31) - 1)
+        return fail(SVM_E_INVALID, "rows must be in [0, 2^31)");
+    if (cols < 1 || cols > kMaxWidth)
+        return fail(SVM_E_INVALID, "cols must be in [1, 2^21]");
+    if (positions < 1 || rows % positions)
+        return fail(SVM_E_INVALID, "rows must be whole samples of positions");
+    if (groups < 1 || cols % groups)
+        return fail(SVM_E_INVALID, "cols must be whole groups");
+    return SVM_OK;
 }
 
 }  // namespace
@@ -236,6 +251,144 @@ svm_status svm_linear_packed(const svm_array* X, const svm_packed* W,
     OnDevice on(device);
     Pieces ws{static_cast<unsigned char*>(work), true};
     linear4(a, ws, (hipStream_t)stream);
+    HIP_TRY(hipPeekAtLastError());
+    return SVM_OK;
+    GUARD_END
+}
+
+svm_status svm_group_norm_workspace(int64_t rows, int64_t positions,
+                                    int64_t cols, int64_t groups,
+                                    int32_t dtype, int64_t* bytes)
+{
+    ENTRY_BEGIN
+    if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
+    *bytes = 0;
+    CHECK(check_groups(rows, positions, cols, groups));
+    if (dtype < SVM_F32 || dtype > SVM_F16)
+        return fail(SVM_E_INVALID, "unknown type");
+    GroupCall a;
+    a.X = {nullptr, rows, cols, cols, dtype, 1};
+    a.weight = a.bias = a.Y = kNone;
+    a.positions = positions;
+    a.groups = groups;
+    Pieces count;
+    group_norm(a, count, nullptr);
+    *bytes = count.used;
+    return SVM_OK;
+    GUARD_END
+}
+
+svm_status svm_group_norm(const svm_array* X, int64_t positions,
+                          int64_t groups, const svm_array* weight,
+                          const svm_array* bias, double eps, int32_t act,
+                          const svm_array* Y, float* mean, float* rstd,
+                          void* work, int64_t work_bytes, int32_t device,
+                          void* stream)
+{
+    ENTRY_BEGIN
+    CHECK(check_act(act));
+    CHECK(check_first(X, "X"));
+    const int64_t m = X->rows, n = X->cols;
+    CHECK(check_groups(m, positions, n, groups));
+    if (weight) CHECK(check_array(weight, "weight", 1, n, X->dtype));
+    if (bias) CHECK(check_array(bias, "bias", 1, n, X->dtype));
+    if (!std::isfinite(eps) || eps < 0)
+        return fail(SVM_E_INVALID, "eps must be finite and >= 0");
+    CHECK(check_array(Y, "Y", m, n, X->dtype));
+    CHECK(check_apart(Y, "Y", {weight, bias}));
+    if (!same(Y, X)) CHECK(check_apart(Y, "Y", {X}));
+    CHECK(check_float(mean, "mean"));
+    CHECK(check_float(rstd, "rstd"));
+    GroupCall a{*X,  or_none(weight), or_none(bias), *Y,
+                positions, groups, (float)eps, act, mean, rstd};
+    Pieces count;
+    group_norm(a, count, nullptr);
+    CHECK(check_work(work, work_bytes, count.used));
+    CHECK(check_ordinal(device));
+    if (m == 0) return SVM_OK;
+    OnDevice on(device);
+    Pieces ws{static_cast<unsigned char*>(work), true};
+    group_norm(a, ws, (hipStream_t)stream);
+    HIP_TRY(hipPeekAtLastError());
+    return SVM_OK;
+    GUARD_END
+}
+
+svm_status svm_group_norm_backward_workspace(int64_t rows, int64_t positions,
+                                             int64_t cols, int64_t groups,
+                                             int32_t dtype, int64_t* bytes)
+{
+    ENTRY_BEGIN
+    if (!bytes) return fail(SVM_E_INVALID, "bytes is NULL");
+    *bytes = 0;
+    CHECK(check_groups(rows, positions, cols, groups));
+    if (dtype < SVM_F32 || dtype > SVM_F16)
+        return fail(SVM_E_INVALID, "unknown type");
+    GroupGradCall a;
+    a.X = {nullptr, rows, cols, cols, dtype, 1};
+    a.dY = a.X;
+    a.weight = a.bias = a.residual = a.dX = a.dweight = a.dbias = kNone;
+    a.positions = positions;
+    a.groups = groups;
+    a.sums = true;
+    Pieces count;
+    group_norm_backward(a, count, nullptr);
+    *bytes = count.used;
+    return SVM_OK;
+    GUARD_END
+}
+
+svm_status svm_group_norm_backward(
+    const svm_array* dY, const svm_array* X, int64_t positions,
+    int64_t groups, const float* mean, const float* rstd,
+    const svm_array* weight, const svm_array* bias, int32_t act,
+    const svm_array* residual, const svm_array* dX, const svm_array* dweight,
+    const svm_array* dbias, void* work, int64_t work_bytes, int32_t device,
+    void* stream)
+{
+    ENTRY_BEGIN
+    CHECK(check_act(act));
+    CHECK(check_first(dY, "dY"));
+    const int64_t m = dY->rows, n = dY->cols;
+    const int32_t t = dY->dtype;
+    CHECK(check_groups(m, positions, n, groups));
+    CHECK(check_array(X, "X", m, n, t));
+    if (m > 0 && (!mean || !rstd))
+        return fail(SVM_E_INVALID, "mean or rstd is NULL");
+    CHECK(check_float(mean, "mean"));
+    CHECK(check_float(rstd, "rstd"));
+    if (weight) CHECK(check_array(weight, "weight", 1, n, t));
+    if (bias) CHECK(check_array(bias, "bias", 1, n, t));
+    if (residual) CHECK(check_array(residual, "residual", m, n, t));
+    if (dX) {
+        CHECK(check_array(dX, "dX", m, n, t));
+        CHECK(check_apart(dX, "dX", {X, weight, bias, dweight, dbias}));
+        if (!same(dX, dY)) CHECK(check_apart(dX, "dX", {dY}));
+        if (!same(dX, residual)) CHECK(check_apart(dX, "dX", {residual}));
+    }
+    if (dweight) {
+        CHECK(check_array(dweight, "dweight", 1, n, t));
+        CHECK(check_apart(dweight, "dweight",
+                          {dY, X, weight, bias, residual, dbias}));
+    }
+    if (dbias) {
+        CHECK(check_array(dbias, "dbias", 1, n, t));
+        CHECK(check_apart(dbias, "dbias", {dY, X, weight, bias, residual}));
+    }
+    GroupGradCall a{*dY,          *X,
+                    or_none(weight),   or_none(bias),
+                    or_none(residual), or_none(dX),
+                    or_none(dweight),  or_none(dbias),
+                    positions,    groups,
+                    act,          mean,
+                    rstd,         dweight || dbias};
+    Pieces count;
+    group_norm_backward(a, count, nullptr);
+    CHECK(check_work(work, work_bytes, count.used));
+    CHECK(check_ordinal(device));
+    OnDevice on(device);
+    Pieces ws{static_cast<unsigned char*>(work), true};
+    group_norm_backward(a, ws, (hipStream_t)stream);
     HIP_TRY(hipPeekAtLastError());
     return SVM_OK;
     GUARD_END

@@ -53,6 +53,8 @@ EXPORTS = [
     "svm_adamw_state", "svm_grad_norm", "svm_grad_norm_workspace",
     "svm_adamw_step_clipped", "svm_pack_weights", "svm_pack_weights_bytes",
     "svm_unpack_weights", "svm_linear_packed", "svm_linear_packed_workspace",
+    "svm_group_norm", "svm_group_norm_workspace", "svm_group_norm_backward",
+    "svm_group_norm_backward_workspace",
 ]
 
 
@@ -245,6 +247,14 @@ def load(path: Optional[str] = None):
     lib.svm_linear_packed.argtypes = [pa, p4, pa, pa, i32, pa, vp, i64, i32,
                                       vp]
     lib.svm_linear_packed_workspace.argtypes = [pa, p4, P(i64)]
+    lib.svm_group_norm.argtypes = [pa, i64, i64, pa, pa, f64, i32, pa, vp, vp,
+                                   vp, i64, i32, vp]
+    lib.svm_group_norm_workspace.argtypes = [i64, i64, i64, i64, i32, P(i64)]
+    lib.svm_group_norm_backward.argtypes = [pa, pa, i64, i64, vp, vp, pa, pa,
+                                            i32, pa, pa, pa, pa, vp, i64, i32,
+                                            vp]
+    lib.svm_group_norm_backward_workspace.argtypes = [i64, i64, i64, i64, i32,
+                                                      P(i64)]
     for name in EXPORTS:  # fail now, not at first use, if one is missing
         getattr(lib, name)
     _lib = lib
@@ -1049,6 +1059,84 @@ def svm_grad_norm(grads, max_norm: float = float("inf"),
                              size.value, c.index, c.handle))
     c.done()
     return norm, factor
+
+
+def _positions(X) -> int:
+    """Rows to a sample: the product of the dimensions between the first and
+    the last."""
+    if X.dim() < 2:
+        raise SvmError(SVM_E_INVALID, "group norm takes samples x positions x "
+                       "channels: two dimensions at least")
+    n = 1
+    for s in X.shape[1:-1]:
+        n *= s
+    return max(n, 1)
+
+
+def svm_group_norm(X, groups: int, weight=None, bias=None, eps: float = 1e-5,
+                   act="none", save: bool = False, out=None, stream=None):
+    """Group norm with an activation over X (samples, any positions,
+    channels): act((x - mean) rstd weight + bias), the statistics over a
+    sample's positions and the channels of a group -> Y, or (Y, mean, rstd)
+    when `save` (float32, samples x groups).  `out` receives Y when given (it
+    may be X)."""
+    import torch
+    lib = load()
+    c = _Call(X, stream)
+    a, per = c.arr(X, "X"), _positions(X)
+    Y = out if out is not None else X.new_empty(X.shape)
+    mean = rstd = None
+    if save:
+        mean = c.empty((X.shape[0], groups), torch.float32)
+        rstd = c.empty((X.shape[0], groups), torch.float32)
+        if not a.rows:  # samples without positions, if any
+            mean.zero_(), rstd.zero_()
+    size = ct.c_int64()
+    _check(lib.svm_group_norm_workspace(a.rows, per, a.cols, groups, a.dtype,
+                                        ct.byref(size)))
+    ws = c.work(size.value)
+    w, b = c.arr(weight, "weight"), c.arr(bias, "bias")
+    c.ready()
+    _check(lib.svm_group_norm(ct.byref(a), per, groups, _ref(w), _ref(b), eps,
+                              _act(act), ct.byref(c.arr(Y, "out", True)),
+                              _ptr(mean), _ptr(rstd), ws, size.value, c.index,
+                              c.handle))
+    c.done()
+    if out is not None:
+        _written(out)
+    return (Y, mean, rstd) if save else Y
+
+
+def svm_group_norm_backward(dY, X, groups: int, mean, rstd, weight=None,
+                            bias=None, act="none", residual=None,
+                            need=(True, True, True), stream=None):
+    """Gradients (dX, dweight, dbias) of svm_group_norm; None where `need` is
+    false.  `residual` is added to dX: the gradient that reaches X past the
+    norm."""
+    lib = load()
+    c = _Call(dY, stream)
+    g, a, per = c.arr(dY, "dY"), c.arr(X, "X"), _positions(dY)
+    if X.shape != dY.shape:
+        raise SvmError(SVM_E_INVALID, "X and dY differ in shape")
+    mp = c.floats(mean, dY.shape[0] * groups, "mean")
+    rp = c.floats(rstd, dY.shape[0] * groups, "rstd")
+    dX = dY.new_empty(X.shape) if need[0] else None
+    dw = dY.new_empty(g.cols) if need[1] else None
+    db = dY.new_empty(g.cols) if need[2] else None
+    size = ct.c_int64()
+    _check(lib.svm_group_norm_backward_workspace(
+        g.rows, per, g.cols, groups, g.dtype, ct.byref(size)))
+    ws = c.work(size.value)
+    w, b, r = (c.arr(weight, "weight"), c.arr(bias, "bias"),
+               c.arr(residual, "residual"))
+    c.ready()
+    _check(lib.svm_group_norm_backward(
+        ct.byref(g), ct.byref(a), per, groups, mp, rp, _ref(w), _ref(b),
+        _act(act), _ref(r), _ref(c.arr(dX, "dX", True)),
+        _ref(c.arr(dw, "dweight", True)), _ref(c.arr(db, "dbias", True)), ws,
+        size.value, c.index, c.handle))
+    c.done()
+    return dX, dw, db
 
 
 class PackedWeights:

@@ -192,6 +192,100 @@ def test_packed4_layout_matches_header(tmp_path):
     assert got == [ct.sizeof(S)] + [getattr(S, n).offset for n in names]
 
 
+# --------------------------------------------------------------- group norm
+
+
+def group(X=None, positions=3, groups=2, w=None, b=None, eps=1e-5, act=0,
+          Y=None, mean=None, rstd=None, work=16, nbytes=1 << 40, device=0):
+    X, Y = X or arr(6, 4), Y or arr(6, 4, at=2 << 20)
+    return nv.load().svm_group_norm(
+        ref(X), positions, groups, ref(w), ref(b), eps, act, ref(Y), mean,
+        rstd, work, nbytes, device, None)
+
+
+GROUPS = [dict(positions=0), dict(positions=-3), dict(positions=4),
+          dict(positions=7), dict(groups=0), dict(groups=-1), dict(groups=3),
+          dict(groups=5)]
+
+
+@pytest.mark.parametrize("kw", GROUPS + [
+    dict(X=arr(6, 0)), dict(X=arr(-3, 4)), dict(X=arr(6, 4, ld=3)),
+    dict(X=arr(6, 4, dtype=4)), dict(w=arr(1, 5, at=4 << 20)),
+    dict(b=arr(2, 4, at=4 << 20)), dict(eps=-1.0), dict(eps=float("nan")),
+    dict(act=6), dict(act=-1), dict(Y=arr(5, 4, at=2 << 20)),
+    dict(Y=arr(6, 4, at=(1 << 20) + 4)), dict(Y=arr(6, 4, ld=5)),
+    dict(w=arr(1, 4, at=2 << 20)), dict(b=arr(1, 4, at=2 << 20)),
+    dict(mean=18), dict(rstd=17), dict(device=-1), dict(work=24),
+    # chunks of few large samples need a workspace
+    dict(X=arr(1 << 20, 4, at=1 << 30), positions=1 << 20,
+         Y=arr(1 << 20, 4, at=2 << 30), work=None)])
+def test_group_norm_refusals(kw):
+    assert group(**kw) == INV
+    assert nv.svm_last_error()
+
+
+_SAME = object()
+
+
+def group_back(dY=None, X=_SAME, positions=3, groups=2, mean=16, rstd=16,
+               w=None, b=None, act=0, res=None, dX=_SAME, dw=_SAME, db=_SAME,
+               work=16, nbytes=1 << 40, device=0):
+    d = lambda v, w: w if v is _SAME else v  # noqa: E731
+    dY, X = dY or arr(6, 4), d(X, arr(6, 4, at=2 << 20))
+    dX, dw, db = (d(dX, arr(6, 4, at=3 << 20)), d(dw, arr(1, 4, at=4 << 20)),
+                  d(db, arr(1, 4, at=5 << 20)))
+    return nv.load().svm_group_norm_backward(
+        ref(dY), ref(X), positions, groups, mean, rstd, ref(w), ref(b), act,
+        ref(res), ref(dX), ref(dw), ref(db), work, nbytes, device, None)
+
+
+@pytest.mark.parametrize("kw", GROUPS + [
+    dict(X=None), dict(X=arr(6, 5, at=2 << 20)), dict(mean=None),
+    dict(rstd=None), dict(mean=18), dict(act=9), dict(dY=arr(6, 0)),
+    dict(w=arr(2, 4, at=9 << 20)), dict(b=arr(1, 3, at=9 << 20)),
+    dict(res=arr(6, 5, at=9 << 20)), dict(dX=arr(6, 4, at=2 << 20)),
+    dict(dX=arr(6, 4, at=4 << 20)), dict(dX=arr(6, 4, ld=5)),
+    dict(dX=arr(6, 4, at=3 << 20, dtype=1)), dict(dw=arr(1, 4)),
+    dict(dw=arr(1, 3, at=4 << 20)), dict(dw=arr(1, 4, at=5 << 20)),
+    dict(db=arr(1, 4, at=2 << 20)), dict(w=arr(1, 4, at=4 << 20)),
+    dict(b=arr(1, 4, at=5 << 20)), dict(work=None), dict(nbytes=16),
+    dict(device=-1)])
+def test_group_norm_backward_refusals(kw):
+    assert group_back(**kw) == INV
+    assert nv.svm_last_error()
+
+
+@needs_no_gpu
+def test_group_norm_accepted():
+    none = nv.SVM_E_DEVICE
+    assert group() == none
+    assert group(Y=arr(6, 4)) == none                        # in place
+    assert group(positions=1, groups=4, work=None) == none
+    assert group(X=arr(0, 4, at=None), Y=arr(0, 4, at=None)) == none
+    assert group_back() == none
+    assert group_back(dX=arr(6, 4)) == none                  # on dY
+    assert group_back(res=arr(6, 4, at=3 << 20)) == none     # on dX
+    assert group_back(dw=None, db=None, work=None) == none
+
+
+def test_group_norm_workspace():
+    lib, n = nv.load(), ct.c_int64(-1)
+    for f in (lib.svm_group_norm_workspace,
+              lib.svm_group_norm_backward_workspace):
+        assert f(6, 3, 4, 2, 0, None) == INV
+        for bad in ((6, 4, 4, 2, 0), (6, 0, 4, 2, 0), (-3, 3, 4, 2, 0),
+                    (6, 3, 4, 3, 0), (6, 3, 0, 1, 0), (6, 3, 4, 2, 3)):
+            assert f(*bad, ct.byref(n)) == INV and n.value == 0
+        # every cut of the largest and the smallest
+        for rows, per, cols, groups in (
+                (0, 1, 1, 1), (1, 1, 1, 1), ((1 << 31) - 1, (1 << 31) - 1, 8,
+                                             1), ((1 << 31) - 1, 1, 8, 8),
+                (1, 1, 1 << 21, 1), (1, 1, 1 << 21, 1 << 21)):
+            for t in range(3):
+                assert f(rows, per, cols, groups, t, ct.byref(n)) == 0
+                assert 0 <= n.value <= 1 << 36
+
+
 # ------------------------------------------------------------------ structs
 
 
