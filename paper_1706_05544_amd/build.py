@@ -21,7 +21,7 @@ DEVICE_SOURCES = ["kernels.hip", "rows.hip", "lockstep.hip", "select.hip",
                   "predict.hip", "noalloc.hip", "iterate.hip", "factor.hip",
                   "resident.hip", "linear.hip", "matmul.hip", "norm.hip", "hinge.hip",
                   "adamw.hip", "gradnorm.hip", "linear4.hip",
-                  "groupnorm.hip"]
+                  "groupnorm.hip", "groupgrad.hip"]
 HOST_SOURCES = ["solver.cpp", "api.cpp", "layers.cpp", "network.cpp"]
 
 # Packed fp32 instructions are disabled for every compilation that has a

@@ -1,0 +1,319 @@
+// Gradients of group norm with an activation (groupnorm.hpp says how they are
+// cut up).  One sweep over a slab for the sums by groups and by columns; the
+// slab and what the activation's slope made of dY stay in registers for dX.
+// Bound by memory.
+#include "groupnorm.hpp"
+
+namespace msvm {
+
+namespace {
+
+constexpr int kGradBlocks = 2048;  // that keep sums for weight and bias
+
+// The slope of the activation at z = xh w + b, xh = (x - mu) rs.  For relu it
+// is a matter of z's sign: where 32 bits' rounding may have turned that, 64
+// bits settle it (the slope would be off by all of itself).
+template <int DT, bool EVEN>
+__device__ __forceinline__ void slopes(
+    int act, const RawEight<DT>& x, const float (&mu)[Place<EVEN>::kK],
+    const float (&rs)[Place<EVEN>::kK], const float (&xh)[8],
+    const float (&w)[8], const float (&b)[8], float (&s)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = fmaf(xh[e], w[e], b[e]);
+    if (act == SVM_ACT_RELU) {
+        bool near = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            near |= fabsf(s[e]) <=
+                    1e-6f * (fabsf(xh[e] * w[e]) + fabsf(b[e]));
+        if (near) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                // (none of this is to be made ahead of the branch)
+                float m = mu[EVEN ? 0 : e], r = rs[EVEN ? 0 : e];
+                float wv = w[e], bv = b[e];
+                asm volatile("" : "+v"(m), "+v"(r), "+v"(wv), "+v"(bv));
+                const double z = fma(((double)x.at(e) - (double)m) * (double)r,
+                                     (double)wv, (double)bv);
+                s[e] = z > 0.0 ? 1.0f : z < 0.0 ? -1.0f : (float)z;
+            }
+        }
+    }
+    if (act == SVM_ACT_NONE) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = 1.0f;
+    } else {
+        act_slopes(act, s);
+    }
+}
+
+template <bool EVEN>
+__device__ __forceinline__ void load_stats(const GroupArgs& a,
+                                           const Place<EVEN>& at, int64_t n,
+                                           float (&mu)[Place<EVEN>::kK],
+                                           float (&rs)[Place<EVEN>::kK])
+{
+#pragma unroll
+    for (int k = 0; k < Place<EVEN>::kK; ++k) {
+        const int64_t g = n * a.groups + at.g0 + at.group[k];
+        mu[k] = a.mean[g];
+        rs[k] = a.rstd[g];
+    }
+}
+
+// PARTS: only the sums, by chunks and for weight and bias.  A block keeps to
+// one slice and adds up in registers what its columns get over its units.
+template <int DT, int T, int IT, bool EVEN, bool PARTS>
+__global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
+{
+    constexpr int kK = Place<EVEN>::kK;
+    __shared__ float bufs[kSlabs<T>][2 * 8 * T];
+    __shared__ float stats[kSlabs<T>][2 * kStat<T>];
+    const Plan& p = a.p;
+    const int slab = threadIdx.x / T, t = threadIdx.x % T;
+    float *buf = bufs[slab], *stat = stats[slab];
+    const int64_t slice = blockIdx.x % p.slices;
+    const int64_t nb = gridDim.x / p.slices;
+    const Place<EVEN> at(a, slice, t);
+    const int64_t units = a.samples * p.chunks;
+    float w[8], b[8];
+    load_eight<DT>(a.w, at.first(), at.count, 1.0f, w);
+    load_eight<DT>(a.b, at.first(), at.count, 0.0f, b);
+    float sb[8] = {}, sw[8] = {};  // over the block's units
+    const float over = 1.0f / (float)(a.positions * p.each);
+    for (int64_t j0 = blockIdx.x / p.slices * kSlabs<T>; j0 < units;
+         j0 += nb * kSlabs<T>) {
+        const Unit u(a, j0 + slab);
+        float mu[kK], rs[kK];
+#pragma unroll
+        for (int k = 0; k < kK; ++k) mu[k] = rs[k] = 0.0f;
+        if (u.rows > 0) load_stats<EVEN>(a, at, u.n, mu, rs);
+        RawEight<DT> x[IT], g[IT];
+        load_slab<DT, IT>(x, a.X, a.ldx, u.row * a.ldx + at.first(), at.row,
+                          p.rows, u.rows, at.count);
+        load_slab<DT, IT>(g, a.dY, a.ldg, u.row * a.ldg + at.first(), at.row,
+                          p.rows, u.rows, at.count);
+        // by group: the sums of a = dZ w and of a xh
+        float dz[IT][8], v[2][kK] = {};
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            const int count = at.row + i * p.rows < u.rows ? at.count : 0;
+            float xh[8], s[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                xh[e] = (x[i].at(e) - mu[EVEN ? 0 : e]) * rs[EVEN ? 0 : e];
+            slopes<DT, EVEN>(a.act, x[i], mu, rs, xh, w, b, s);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                // (past the ends neither the sums nor a NaN get in)
+                const float d = e < count ? g[i].at(e) * s[e] : 0.0f;
+                const float h = e < count ? xh[e] : 0.0f;
+                const float q = d * w[e];
+                dz[i][e] = d;
+                sb[e] += d;
+                sw[e] = fmaf(d, h, sw[e]);
+                v[0][EVEN ? 0 : e] += q;
+                v[1][EVEN ? 0 : e] = fmaf(q, h, v[1][EVEN ? 0 : e]);
+            }
+        }
+        if (!PARTS && !a.out) continue;
+        forget<DT, IT>(x);
+        group_sums<T, 2, EVEN>(p, at, t, v, buf, stat);
+        if (PARTS) {
+            if (u.rows > 0)
+                for (int q = t; q < at.ng; q += T) {
+                    const int64_t ng = u.n * a.groups + at.g0 + q;
+                    const int64_t cp =
+                        p.parts_across > 1 ? slice % p.parts_across : 0;
+                    a.part[ng * p.parts() + cp * p.chunks + u.ch] =
+                        make_float2(stat[q], stat[kStat<T> + q]);
+                }
+            continue;
+        }
+        float s1[kK], s2[kK];
+#pragma unroll
+        for (int k = 0; k < kK; ++k) {
+            s1[k] = stat[at.group[k]] * over;
+            s2[k] = stat[kStat<T> + at.group[k]] * over;
+        }
+        RawEight<DT> res[IT];
+        if (a.res)
+            load_slab<DT, IT>(res, a.res, a.ldr, u.row * a.ldr + at.first(),
+                              at.row, p.rows, u.rows, at.count);
+        const int64_t to = u.row * a.ldo + at.first();
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            const int r = at.row + i * p.rows;
+            if (r >= u.rows || at.count == 0) continue;
+            Eight<DT> d;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int k = EVEN ? 0 : e;
+                const float xh = (x[i].at(e) - mu[k]) * rs[k];
+                d.v[e] = rs[k] * (dz[i][e] * w[e] - fmaf(xh, s2[k], s1[k]));
+            }
+            if (a.res) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) d.v[e] += res[i].at(e);
+            }
+            d.store(a.out, to + r * a.ldo, at.count);
+        }
+    }
+    if (!a.pw) return;
+    // the block's row of the partial sums: over positions and slabs
+    const int wide = p.lanes * 8;
+    __syncthreads();
+    if (at.row < p.rows) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            buf[at.row * wide + at.lane * 8 + e] = sb[e];
+            buf[8 * T + at.row * wide + at.lane * 8 + e] = sw[e];
+        }
+    }
+    __syncthreads();
+    const int64_t to = blockIdx.x / p.slices * (a.groups * p.each) + at.col;
+    for (int c = threadIdx.x; c < 2 * at.cols; c += kSlabThreads<T>) {
+        const int q = c >= at.cols, d = c - q * at.cols;
+        float sum = 0.0f;
+        for (int i = 0; i < kSlabs<T>; ++i)
+#pragma unroll 4
+            for (int r = 0; r < p.rows; ++r)
+                sum += bufs[i][q * 8 * T + r * wide + d];
+        (q ? a.pw : a.pb)[to + d] = sum;
+    }
+}
+
+// dX from joined sums.  A thread to 8 columns, positions in turn.
+template <int DT, bool EVEN>
+__global__ __launch_bounds__(256) void k_group_dx(GroupArgs a)
+{
+    constexpr int kK = Place<EVEN>::kK;
+    const Plan& p = a.p;
+    const int64_t slice = blockIdx.x % p.slices;
+    const int64_t nb = gridDim.x / p.slices;
+    const int64_t units = a.samples * p.chunks;
+    const float over = 1.0f / (float)(a.positions * p.each);
+    for_lanes<EVEN>(a, slice, [&](const Place<EVEN>& at, int row, int step,
+                                  int count) {
+        const int64_t c = at.first();
+        float w[8], b[8];
+        load_eight<DT>(a.w, c, count, 1.0f, w);
+        load_eight<DT>(a.b, c, count, 0.0f, b);
+        for (int64_t j = blockIdx.x / p.slices; j < units; j += nb) {
+            const Unit u(a, j);
+            float mu[kK], rs[kK], s1[kK], s2[kK];
+            load_stats<EVEN>(a, at, u.n, mu, rs);
+#pragma unroll
+            for (int k = 0; k < kK; ++k) {
+                const float2 s =
+                    a.sums[u.n * a.groups + at.g0 + at.group[k]];
+                s1[k] = s.x * over;
+                s2[k] = s.y * over;
+            }
+            constexpr int kAhead = 2;
+            for (int r0 = row; r0 < u.rows; r0 += step * kAhead) {
+                RawEight<DT> x[kAhead], g[kAhead], res[kAhead];
+                load_slab<DT, kAhead>(x, a.X, a.ldx, u.row * a.ldx + c, r0,
+                                      step, u.rows, count);
+                load_slab<DT, kAhead>(g, a.dY, a.ldg, u.row * a.ldg + c, r0,
+                                      step, u.rows, count);
+                if (a.res)
+                    load_slab<DT, kAhead>(res, a.res, a.ldr,
+                                          u.row * a.ldr + c, r0, step, u.rows,
+                                          count);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const int r = r0 + i * step;
+                    if (r >= u.rows) continue;
+                    Eight<DT> d;
+                    float xh[8], s[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        xh[e] = (x[i].at(e) - mu[EVEN ? 0 : e]) *
+                                rs[EVEN ? 0 : e];
+                    slopes<DT, EVEN>(a.act, x[i], mu, rs, xh, w, b, s);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int k = EVEN ? 0 : e;
+                        d.v[e] = rs[k] * (g[i].at(e) * s[e] * w[e] -
+                                          fmaf(xh[e], s2[k], s1[k]));
+                    }
+                    if (a.res) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) d.v[e] += res[i].at(e);
+                    }
+                    d.store(a.out, (u.row + r) * a.ldo + c, count);
+                }
+            }
+        }
+    });
+}
+
+}  // namespace
+
+void group_norm_backward(const GroupGradCall& c, Pieces& ws, hipStream_t s)
+{
+    const int64_t samples = c.X.rows / c.positions, n = c.X.cols;
+    GroupArgs a{};
+    a.X = c.X.data;
+    a.dY = c.dY.data;
+    a.res = c.residual.data;
+    a.w = c.weight.data;
+    a.b = c.bias.data;
+    a.out = c.dX.data;
+    a.ldx = c.X.ld;
+    a.ldg = c.dY.ld;
+    a.ldr = c.residual.ld;
+    a.ldo = c.dX.ld;
+    a.samples = samples;
+    a.positions = c.positions;
+    a.groups = c.groups;
+    a.act = c.act;
+    a.mean = const_cast<float*>(c.mean);
+    a.rstd = const_cast<float*>(c.rstd);
+    a.p = plan_of(samples, c.positions, n, c.groups, c.X.dtype, true);
+    const Plan& p = a.p;
+    const int64_t rows = samples ? blocks_across(a, kGradBlocks) : 0;
+    const int64_t all = samples * c.groups;
+    if (c.sums) {
+        a.pw = ws.take<float>(rows * n);
+        a.pb = ws.take<float>(rows * n);
+    }
+    float2* joined = nullptr;
+    if (p.split()) {
+        a.part = ws.take<float2>(all * p.parts());
+        joined = ws.take<float2>(all);
+        a.sums = joined;
+    }
+    if (!ws.run) return;
+    if (samples > 0 && (c.sums || a.out))
+        for_dtype(c.X.dtype, [&]<int DT>() {
+            const dim3 grid((unsigned)(rows * p.slices));
+            for_plan<DT, true>(p, [&]<int T, int IT, bool EVEN>() {
+                if (!p.split()) {
+                    hipLaunchKernelGGL((k_group_grad<DT, T, IT, EVEN, false>),
+                                       grid, dim3(kSlabThreads<T>), 0, s, a);
+                    return;
+                }
+                if constexpr (T >= 256)
+                    hipLaunchKernelGGL((k_group_grad<DT, T, IT, EVEN, true>),
+                                       grid, dim3(kSlabThreads<T>), 0, s, a);
+            });
+            if (!p.split() || !a.out) return;
+            launch_join<true>(a, joined, s);
+            const dim3 all_blocks(
+                (unsigned)(blocks_across(a, 1 << 20) * p.slices));
+            if (p.even)
+                hipLaunchKernelGGL((k_group_dx<DT, true>), all_blocks,
+                                   dim3(256), 0, s, a);
+            else
+                hipLaunchKernelGGL((k_group_dx<DT, false>), all_blocks,
+                                   dim3(256), 0, s, a);
+        });
+    if (c.sums)
+        launch_column_sums(a.pw, a.pb, rows, n, c.X.dtype, c.dweight.data,
+                           c.dbias.data, s);
+}
+
+}  // namespace msvm

@@ -1,0 +1,455 @@
+// Group norm with an activation over samples x positions x channels, channels
+// last: how a call is cut up, and what its kernels (groupnorm.hip) and those
+// of its gradients (groupgrad.hip) share.
+//
+// A unit of work is a slab: the positions of one sample (or a chunk of them)
+// by a slice of columns, whole groups side by side, wide enough to fill the
+// memory's lines (groups of more than kWideCols channels are cut into slices
+// of their own).  T threads hold a slab in registers, each 8 columns of every
+// R-th position, from its read to its write.  Where the 8 columns of a thread
+// lie in one group, its sum is one number, and the threads' numbers are joined
+// through LDS; for groups of other widths the sums are joined by columns
+// first.  Where a sample's slab is too large, or slabs are too few to fill the
+// card, the positions are cut into chunks: one launch for the chunks' sums,
+// one that joins them, and one that applies them and reads the values again.
+#pragma once
+
+#include "elem.hpp"
+#include "layers.hpp"
+
+namespace msvm {
+namespace {
+
+constexpr int64_t kWideCols = 4096;
+
+// How a call is cut up.  All by the sizes and the type.
+struct Plan {
+    int threads, pieces;   // of a slab: T, and IT pieces of 8 for each
+    int lanes, rows;       // lanes across the slice; positions at a time
+    int64_t each;          // channels of a group
+    int64_t groups;        // of a slice (1 where a group has several slices)
+    int64_t cols;          // of a slice
+    int64_t slices, parts_across;  // of a row; of a group
+    int64_t chunk, chunks; // positions of a chunk; chunks of a sample
+    bool even;             // the 8 columns of a thread lie in one group
+    __host__ __device__ bool split() const
+    {
+        return chunks > 1 || parts_across > 1;
+    }
+    __host__ __device__ int64_t parts() const { return chunks * parts_across; }
+};
+
+struct GroupArgs {
+    const void *X, *dY, *res, *w, *b;
+    void* out;
+    int64_t ldx, ldg, ldr, ldo;
+    int64_t samples, positions, groups;
+    float eps;
+    int act;
+    float *mean, *rstd;     // written by the forward pass, else read
+    float2* part;           // sums of the chunks
+    const float2* sums;     // joined sums of a gradient
+    float *pw, *pb;         // rows of partial sums for weight and bias
+    Plan p;
+};
+
+// Threads of a block, slabs of it; groups and columns of a slice at most.
+template <int T>
+constexpr int kSlabThreads = T > 256 ? T : 256;
+template <int T>
+constexpr int kSlabs = kSlabThreads<T> / T;
+template <int T>
+constexpr int kStat = T < 256 ? 2 * T : 512;
+
+// What a thread has of the slab of its slice.
+template <bool EVEN>
+struct Place {
+    static constexpr int kK = EVEN ? 1 : 8;  // groups that it may meet
+    int64_t col, g0;  // first column and group
+    int lane, row;    // of the 8-column pieces; first position
+    int count;        // columns that there are, of 8
+    int cols, ng;     // of this slice
+    int group[kK];    // of the thread's columns, in the slice
+
+    __device__ __forceinline__ Place(const GroupArgs& a, int64_t slice, int t)
+    {
+        const Plan& p = a.p;
+        lane = t % p.lanes;
+        row = t / p.lanes;
+        if (p.parts_across > 1) {
+            g0 = slice / p.parts_across;
+            const int64_t c = (slice - g0 * p.parts_across) * p.cols;
+            col = g0 * p.each + c;
+            cols = (int)(p.each - c < p.cols ? p.each - c : p.cols);
+            ng = 1;
+        } else {
+            g0 = slice * p.groups;
+            col = g0 * p.each;
+            const int64_t left = a.groups - g0;
+            ng = (int)(left < p.groups ? left : p.groups);
+            cols = ng * (int)p.each;
+        }
+        count = row < p.rows ? eight_of(cols, lane * 8) : 0;
+#pragma unroll
+        for (int e = 0; e < kK; ++e) {
+            const int g =
+                p.parts_across > 1 ? 0 : (lane * 8 + e) / (int)p.each;
+            group[e] = g < ng ? g : ng - 1;
+        }
+    }
+    __device__ __forceinline__ int64_t first() const { return col + lane * 8; }
+    // channels of a group that are in this slice
+    __device__ __forceinline__ int each(const Plan& p) const
+    {
+        return p.parts_across > 1 ? cols : (int)p.each;
+    }
+};
+
+// Where unit j of a slice begins, and how many positions it has (none past
+// the last unit).
+struct Unit {
+    int64_t n, ch, row;
+    int rows;
+    __device__ __forceinline__ Unit(const GroupArgs& a, int64_t j)
+    {
+        n = a.p.chunks > 1 ? j / a.p.chunks : j;
+        ch = a.p.chunks > 1 ? j - n * a.p.chunks : 0;
+        const int64_t r0 = ch * a.p.chunk;
+        row = n * a.positions + r0;
+        const int64_t left = a.positions - r0;
+        rows = j < a.samples * a.p.chunks
+                   ? (int)(left < a.p.chunk ? left : a.p.chunk)
+                   : 0;
+    }
+};
+
+// Waits for the threads of a slab (one wave's LDS accesses are in order).
+template <int T>
+__device__ __forceinline__ void slab_sync()
+{
+    if constexpr (T <= 64) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
+        __syncthreads();
+    }
+}
+
+// Adds up Q quantities of a slab's threads by groups: stat[q kStat + g].  v is
+// a thread's one number (EVEN) or its 8 columns' sums.  buf: T or 8 T floats
+// for each quantity; its earlier contents have been read by all threads
+// before the last slab_sync.
+template <int T, int Q, bool EVEN>
+__device__ __forceinline__ void group_sums(
+    const Plan& p, const Place<EVEN>& at, int t,
+    const float (&v)[Q][Place<EVEN>::kK], float* buf, float* stat)
+{
+    int team = T < 64 ? T : 64;
+    while (team > 1 && team * at.ng > T) team >>= 1;
+    const int l = t % team, first = t / team, step = T / team;
+    const int each = at.each(p);
+    const int wide = EVEN ? p.lanes : p.lanes * 8;
+    constexpr int kOne = EVEN ? T : 8 * T;
+    int rows = p.rows, width = each;
+    if constexpr (EVEN) {
+        if (at.row < p.rows) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+                buf[q * kOne + at.row * wide + at.lane] = v[q][0];
+        }
+        slab_sync<T>();
+        width = (each + 7) / 8;
+    } else {
+        if (at.row < p.rows) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    buf[q * kOne + at.row * wide + at.lane * 8 + e] = v[q][e];
+        }
+        slab_sync<T>();
+        // columns first: as many rows are left as the threads have turns
+        rows = T / wide < 1 ? 1 : T / wide < p.rows ? T / wide : p.rows;
+        for (int i = t; i < rows * wide; i += T) {
+            const int r0 = i / wide;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                float* s = buf + q * kOne + (i - r0 * wide);
+                float sum = s[r0 * wide];
+#pragma unroll 4
+                for (int r = r0 + rows; r < p.rows; r += rows)
+                    sum += s[r * wide];
+                s[r0 * wide] = sum;
+            }
+        }
+        slab_sync<T>();
+    }
+    const int items = rows * width;
+    for (int g = first; g < at.ng; g += step) {
+        float sum[Q] = {};
+        for (int i = l; i < items; i += team) {
+            const int r = (int)((unsigned)i / (unsigned)width);
+            const int c = r * wide + g * width + (i - r * width);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) sum[q] += buf[q * kOne + c];
+        }
+        for (int off = team >> 1; off > 0; off >>= 1)
+#pragma unroll
+            for (int q = 0; q < Q; ++q) sum[q] += __shfl_xor(sum[q], off);
+        if (l == 0) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) stat[q * kStat<T> + g] = sum[q];
+        }
+    }
+    slab_sync<T>();
+}
+
+// Values of a vector at a thread's columns; `fill` where it has none.
+template <int DT>
+__device__ __forceinline__ void load_eight(const void* p, int64_t at,
+                                           int count, float fill,
+                                           float (&v)[8])
+{
+    Eight<DT> x;
+    if (p) x.load(p, at, count);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = p ? x.v[e] : fill;
+}
+
+// The pieces of a slab: all loads before the first use.  Past the last
+// position a whole piece is its last one again (a branch around a load would
+// have the next wait for it); `there` tells them apart.
+template <int DT, int IT>
+__device__ __forceinline__ void load_slab(RawEight<DT> (&x)[IT], const void* X,
+                                          int64_t ld, int64_t first, int row,
+                                          int step, int rows, int count)
+{
+    if (count == 8 && rows > 0) {
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            const int r = row + i * step < rows ? row + i * step : rows - 1;
+            x[i].load(X, first + r * ld, 8);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            const int r = row + i * step;
+            x[i].load(X, first + r * ld, r < rows ? count : 0);
+        }
+    }
+}
+
+// The compiler is not to keep what it made of these registers (their values
+// in 32 bits, twice the room).
+template <int DT, int IT>
+__device__ __forceinline__ void forget(RawEight<DT> (&x)[IT])
+{
+    if constexpr (DT != SVM_F32) {
+#pragma unroll
+        for (int i = 0; i < IT; ++i) asm volatile("" : "+v"(x[i].v[0]));
+    }
+}
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Pieces of a thread at most: 64 registers for the forward pass' raw values;
+// the gradient holds the values and 32 bits of each gradient.
+int most_pieces(int32_t dtype, bool grad)
+{
+    if (grad) return dtype == SVM_F32 ? 4 : 8;
+    return dtype == SVM_F32 ? 8 : 16;
+}
+
+// The pieces that the kernels are made for, from `need` on.
+int pieces_of(int threads, int64_t need)
+{
+    if (need <= 1) return 1;
+    if (threads == 16) return 2;
+    if (need <= 2 && threads == 256) return 2;
+    return need <= 4 ? 4 : need <= 8 ? 8 : 16;
+}
+
+// The cut of a call.  Slices begin as narrow as fills a line of memory (more
+// slabs), and grow while a slab has too little to do.
+Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
+             int64_t groups, int32_t dtype, bool grad)
+{
+    Plan p{};
+    p.each = channels / groups;
+    p.parts_across = p.each > kWideCols ? up(p.each, kWideCols) : 1;
+    p.even = p.parts_across > 1 || p.each % 8 == 0;
+    if (p.parts_across > 1) {
+        p.groups = 1;
+        p.cols = kWideCols;
+        p.slices = groups * p.parts_across;
+    } else {
+        const int64_t line = dtype == SVM_F32 ? 32 : 64;
+        p.groups = up(line, p.each);
+        while (p.groups < groups && positions * p.groups * p.each < 1024 &&
+               p.groups * 2 * p.each <= 512)
+            p.groups *= 2;
+        if (p.groups > groups) p.groups = groups;
+        p.cols = p.groups * p.each;
+        p.slices = up(groups, p.groups);
+    }
+    p.lanes = (int)up(p.cols, 8);
+    const int most = most_pieces(dtype, grad);
+    const int64_t units = samples * p.slices;
+    constexpr int kThreads[4] = {16, 64, 256, 512};
+    constexpr int kPieces[4] = {2, 4, 8, 16};
+    auto fits = [&](int i, int64_t pieces) {
+        const int t = kThreads[i];
+        if (pieces > kPieces[i]) pieces = kPieces[i];
+        if (pieces > most) pieces = most;
+        return p.lanes <= t && p.groups <= 2 * t &&
+               up(positions, t / p.lanes) <= pieces;
+    };
+    int i = 0;
+    // few slabs: more threads to each, so that they are done sooner
+    while (i < 3 && !fits(i, units * kThreads[i] < 131072 ? 1 : 16)) ++i;
+    bool whole = p.parts_across == 1 && fits(i, 16);
+    // a slab for each sample leaves most of the card idle
+    if (units * kThreads[i] < 65536 &&
+        samples * positions * channels > 1 << 18 && positions > 1)
+        whole = false;
+    p.chunk = positions;
+    p.chunks = 1;
+    if (!whole) {
+        i = p.lanes > 256 ? 3 : 2;
+        const int64_t rows = kThreads[i] / p.lanes;
+        const int64_t deep = most < 8 ? most : 8;
+        // chunks that fill the card's blocks, but no longer than fits
+        int64_t chunk = up(positions * units, 2048);
+        if (chunk < rows) chunk = rows;
+        if (chunk > rows * deep) chunk = rows * deep;
+        p.chunk = chunk < positions ? chunk : positions;
+        p.chunks = up(positions, p.chunk);
+    }
+    p.threads = kThreads[i];
+    p.rows = p.threads / p.lanes;
+    p.pieces = pieces_of(p.threads, up(p.chunk, p.rows));
+    if (p.pieces > most) p.pieces = most;
+    return p;
+}
+
+// Calls f with the threads and pieces of a plan and whether it is even.
+template <int DT, bool GRAD, class F>
+void for_plan(const Plan& p, F&& f)
+{
+    constexpr int kMost = GRAD ? (DT == SVM_F32 ? 4 : 8)
+                               : (DT == SVM_F32 ? 8 : 16);
+    auto go = [&]<int T, int IT>() {
+        if (p.even) f.template operator()<T, IT, true>();
+        else f.template operator()<T, IT, false>();
+    };
+    if (p.threads == 16) {
+        if (p.pieces == 1) go.template operator()<16, 1>();
+        else go.template operator()<16, 2>();
+    } else if (p.threads == 64) {
+        if (p.pieces == 1) go.template operator()<64, 1>();
+        else go.template operator()<64, 4>();
+    } else if (p.threads == 256) {
+        if (p.pieces == 1) go.template operator()<256, 1>();
+        else if (p.pieces == 2) go.template operator()<256, 2>();
+        else if (p.pieces == 4) go.template operator()<256, 4>();
+        else if constexpr (kMost >= 8) go.template operator()<256, 8>();
+    } else {
+        if (p.pieces == 1) go.template operator()<512, 1>();
+        else if (p.pieces == 4) go.template operator()<512, 4>();
+        else if (p.pieces == 8) {
+            if constexpr (kMost >= 8) go.template operator()<512, 8>();
+        } else if constexpr (kMost >= 16) {
+            go.template operator()<512, 16>();
+        }
+    }
+}
+
+// Blocks to a slice: each has a unit or more for each of its slabs.
+int64_t blocks_across(const GroupArgs& a, int64_t most)
+{
+    const int64_t slabs = a.p.threads < 256 ? 256 / a.p.threads : 1;
+    const int64_t nb = up(a.samples * a.p.chunks, slabs);
+    const int64_t cap = most / a.p.slices > 1 ? most / a.p.slices : 1;
+    return nb < cap ? nb : cap;
+}
+
+// Joins the chunks' sums of a group, a wave to a group: the mean of the
+// parts' means by their sizes, and the squares about it.  SUMS: adds the
+// parts of a gradient's two sums instead.
+template <bool SUMS>
+__global__ __launch_bounds__(256) void k_group_join(GroupArgs a, float2* sums)
+{
+    const Plan& p = a.p;
+    const int lane = threadIdx.x & 63;
+    const int64_t all = a.samples * a.groups;
+    const int64_t parts = p.parts();
+    const float size = (float)(a.positions * p.each);
+    for (int64_t g = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); g < all;
+         g += (int64_t)gridDim.x * 4) {
+        const float2* q = a.part + g * parts;
+        float s0 = 0.0f, s1 = 0.0f;
+        auto count = [&](int64_t i) {
+            const int64_t cp = p.parts_across > 1 ? i / p.chunks : 0;
+            const int64_t ch = i - cp * p.chunks;
+            const int64_t r = a.positions - ch * p.chunk;
+            const int64_t c = p.parts_across > 1 ? p.each - cp * p.cols
+                                                 : p.each;
+            const int64_t wide = p.parts_across > 1 ? p.cols : p.each;
+            return (float)((r < p.chunk ? r : p.chunk) *
+                           (c < wide ? c : wide));
+        };
+        for (int64_t i = lane; i < parts; i += 64) {
+            const float2 v = q[i];
+            s0 += SUMS ? v.x : v.x * count(i);
+            s1 += v.y;
+        }
+        s0 = SUMS ? wave_sum(s0) : wave_sum(s0) / size;
+        s1 = wave_sum(s1);
+        if (SUMS) {
+            if (lane == 0) sums[g] = make_float2(s0, s1);
+            continue;
+        }
+        float far = 0.0f;
+        for (int64_t i = lane; i < parts; i += 64) {
+            const float d = q[i].x - s0;
+            far = fmaf(d * d, count(i), far);
+        }
+        s1 += wave_sum(far);
+        if (lane == 0) {
+            a.mean[g] = s0;
+            a.rstd[g] = 1.0f / sqrtf(s1 / size + a.eps);
+        }
+    }
+}
+
+template <bool SUMS>
+void launch_join(const GroupArgs& a, float2* sums, hipStream_t s)
+{
+    const int64_t nb = up(a.samples * a.groups, 4);
+    hipLaunchKernelGGL((k_group_join<SUMS>),
+                       dim3((unsigned)(nb < 65536 ? nb : 65536)), dim3(256), 0,
+                       s, a, sums);
+}
+
+// A thread's columns and rows of an applying kernel: 256 threads, the plan's
+// lanes across (more than 256 in turns).  f(at, row, step, count).
+template <bool EVEN, class F>
+__device__ __forceinline__ void for_lanes(const GroupArgs& a, int64_t slice,
+                                          F&& f)
+{
+    const int lanes = a.p.lanes;
+    const int step = lanes < 256 ? 256 / lanes : 1;
+    for (int t0 = 0; t0 < lanes; t0 += 256) {
+        const int t = t0 + (int)threadIdx.x;
+        const Place<EVEN> at(a, slice, t);
+        const int row = lanes < 256 ? at.row : 0;
+        const int count = row < step && (lanes < 256 || t < lanes)
+                              ? eight_of(at.cols, at.lane * 8)
+                              : 0;
+        if (count > 0) f(at, row, step, count);
+        if (lanes < 256) break;
+    }
+}
+
+}  // namespace
+}  // namespace msvm
