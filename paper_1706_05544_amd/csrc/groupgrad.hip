@@ -77,28 +77,38 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
     const int64_t nb = gridDim.x / p.slices;
     const Place<EVEN> at(a, slice, t);
     const int64_t units = a.samples * p.chunks;
-    float w[8], b[8];
-    load_eight<DT>(a.w, at.first(), at.count, 1.0f, w);
-    load_eight<DT>(a.b, at.first(), at.count, 0.0f, b);
+    Eights<DT> w8, b8;
+    w8.load(a.w, at.first(), at.count, 1.0f);
+    b8.load(a.b, at.first(), at.count, 0.0f);
     float sb[8] = {}, sw[8] = {};  // over the block's units
     const float over = 1.0f / (float)(a.positions * p.each);
     for (int64_t j0 = blockIdx.x / p.slices * kSlabs<T>; j0 < units;
          j0 += nb * kSlabs<T>) {
         const Unit u(a, j0 + slab);
-        float mu[kK], rs[kK];
-#pragma unroll
-        for (int k = 0; k < kK; ++k) mu[k] = rs[k] = 0.0f;
-        if (u.rows > 0) load_stats<EVEN>(a, at, u.n, mu, rs);
         RawEight<DT> x[IT], g[IT];
-        load_slab<DT, IT>(x, a.X, a.ldx, u.row * a.ldx + at.first(), at.row,
-                          p.rows, u.rows, at.count);
-        load_slab<DT, IT>(g, a.dY, a.ldg, u.row * a.ldg + at.first(), at.row,
-                          p.rows, u.rows, at.count);
+        const bool any = u.rows > 0 && at.count > 0;
+        const int64_t last = u.row + u.rows - 1;
+        load_slab<DT, IT>(x, a.X, (u.row + at.row) * a.ldx + at.first(),
+                          p.rows * a.ldx, last * a.ldx + at.first(), any,
+                          at.count, a.endx);
+        load_slab<DT, IT>(g, a.dY, (u.row + at.row) * a.ldg + at.first(),
+                          p.rows * a.ldg, last * a.ldg + at.first(), any,
+                          at.count, a.endg);
+        // (a slab without a unit takes the last sample's; it adds nothing)
+        float mu[kK], rs[kK];
+        load_stats<EVEN>(a, at, u.n < a.samples ? u.n : a.samples - 1, mu, rs);
+        float w[8], b[8];
+        w8.values(w);
+        b8.values(b);
         // by group: the sums of a = dZ w and of a xh
         float dz[IT][8], v[2][kK] = {};
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
-            const int count = at.row + i * p.rows < u.rows ? at.count : 0;
+            if (i > 0 && i * p.rows >= u.rows) break;
+            // (a piece past the end is another's again, and adds nothing)
+            const bool there = at.row + i * p.rows < u.rows;
+            forget(x[i]);
+            forget(g[i]);
             float xh[8], s[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -106,19 +116,20 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
             slopes<DT, EVEN>(a.act, x[i], mu, rs, xh, w, b, s);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                // (past the ends neither the sums nor a NaN get in)
-                const float d = e < count ? g[i].at(e) * s[e] : 0.0f;
-                const float h = e < count ? xh[e] : 0.0f;
+                const float d = there ? g[i].at(e) * s[e] : 0.0f;
                 const float q = d * w[e];
                 dz[i][e] = d;
                 sb[e] += d;
-                sw[e] = fmaf(d, h, sw[e]);
+                sw[e] = fmaf(d, xh[e], sw[e]);
                 v[0][EVEN ? 0 : e] += q;
-                v[1][EVEN ? 0 : e] = fmaf(q, h, v[1][EVEN ? 0 : e]);
+                v[1][EVEN ? 0 : e] = fmaf(q, xh[e], v[1][EVEN ? 0 : e]);
             }
+            settle(sb);
+            settle(sw);
+            settle(v[0]);
+            settle(v[1]);
         }
         if (!PARTS && !a.out) continue;
-        forget<DT, IT>(x);
         group_sums<T, 2, EVEN>(p, at, t, v, buf, stat);
         if (PARTS) {
             if (u.rows > 0)
@@ -137,15 +148,19 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
             s1[k] = stat[at.group[k]] * over;
             s2[k] = stat[kStat<T> + at.group[k]] * over;
         }
-        RawEight<DT> res[IT];
-        if (a.res)
-            load_slab<DT, IT>(res, a.res, a.ldr, u.row * a.ldr + at.first(),
-                              at.row, p.rows, u.rows, at.count);
-        const int64_t to = u.row * a.ldo + at.first();
+        int64_t to = here((u.row + at.row) * a.ldo + at.first());
+        constexpr int kAhead = IT < 4 ? IT : 4;
+        RawEight<DT> res[kAhead];
 #pragma unroll
-        for (int i = 0; i < IT; ++i) {
+        for (int i = 0; i < IT; ++i, to += p.rows * a.ldo) {
             const int r = at.row + i * p.rows;
+            if (a.res && i % kAhead == 0)
+                load_slab<DT, kAhead>(
+                    res, a.res, (u.row + r) * a.ldr + at.first(),
+                    p.rows * a.ldr, last * a.ldr + at.first(), any, at.count,
+                    a.endr);
             if (r >= u.rows || at.count == 0) continue;
+            forget(x[i]);
             Eight<DT> d;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -155,9 +170,9 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
             }
             if (a.res) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) d.v[e] += res[i].at(e);
+                for (int e = 0; e < 8; ++e) d.v[e] += res[i % kAhead].at(e);
             }
-            d.store(a.out, to + r * a.ldo, at.count);
+            store_some<DT, EVEN>(d, a.out, to, at.count);
         }
     }
     if (!a.pw) return;
@@ -184,6 +199,8 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
     }
 }
 
+constexpr int kAhead = 4;
+
 // dX from joined sums.  A thread to 8 columns, positions in turn.
 template <int DT, bool EVEN>
 __global__ __launch_bounds__(256) void k_group_dx(GroupArgs a)
@@ -197,9 +214,9 @@ __global__ __launch_bounds__(256) void k_group_dx(GroupArgs a)
     for_lanes<EVEN>(a, slice, [&](const Place<EVEN>& at, int row, int step,
                                   int count) {
         const int64_t c = at.first();
-        float w[8], b[8];
-        load_eight<DT>(a.w, c, count, 1.0f, w);
-        load_eight<DT>(a.b, c, count, 0.0f, b);
+        Eights<DT> w8, b8;
+        w8.load(a.w, c, count, 1.0f);
+        b8.load(a.b, c, count, 0.0f);
         for (int64_t j = blockIdx.x / p.slices; j < units; j += nb) {
             const Unit u(a, j);
             float mu[kK], rs[kK], s1[kK], s2[kK];
@@ -211,21 +228,26 @@ __global__ __launch_bounds__(256) void k_group_dx(GroupArgs a)
                 s1[k] = s.x * over;
                 s2[k] = s.y * over;
             }
-            constexpr int kAhead = 2;
             for (int r0 = row; r0 < u.rows; r0 += step * kAhead) {
                 RawEight<DT> x[kAhead], g[kAhead], res[kAhead];
-                load_slab<DT, kAhead>(x, a.X, a.ldx, u.row * a.ldx + c, r0,
-                                      step, u.rows, count);
-                load_slab<DT, kAhead>(g, a.dY, a.ldg, u.row * a.ldg + c, r0,
-                                      step, u.rows, count);
+                const int64_t at0 = u.row + r0, last = u.row + u.rows - 1;
+                load_slab<DT, kAhead>(x, a.X, at0 * a.ldx + c, step * a.ldx,
+                                      last * a.ldx + c, true, count, a.endx);
+                load_slab<DT, kAhead>(g, a.dY, at0 * a.ldg + c, step * a.ldg,
+                                      last * a.ldg + c, true, count, a.endg);
                 if (a.res)
-                    load_slab<DT, kAhead>(res, a.res, a.ldr,
-                                          u.row * a.ldr + c, r0, step, u.rows,
-                                          count);
+                    load_slab<DT, kAhead>(res, a.res, at0 * a.ldr + c,
+                                          step * a.ldr, last * a.ldr + c,
+                                          true, count, a.endr);
+                float w[8], b[8];
+                w8.values(w);
+                b8.values(b);
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
                     const int r = r0 + i * step;
                     if (r >= u.rows) continue;
+                    forget(x[i]);
+                    forget(g[i]);
                     Eight<DT> d;
                     float xh[8], s[8];
 #pragma unroll
@@ -243,7 +265,8 @@ __global__ __launch_bounds__(256) void k_group_dx(GroupArgs a)
 #pragma unroll
                         for (int e = 0; e < 8; ++e) d.v[e] += res[i].at(e);
                     }
-                    d.store(a.out, (u.row + r) * a.ldo + c, count);
+                    store_some<DT, EVEN>(d, a.out,
+                                         (u.row + r) * a.ldo + c, count);
                 }
             }
         }
@@ -266,6 +289,9 @@ void group_norm_backward(const GroupGradCall& c, Pieces& ws, hipStream_t s)
     a.ldg = c.dY.ld;
     a.ldr = c.residual.ld;
     a.ldo = c.dX.ld;
+    a.endx = end_of(c.X);
+    a.endg = end_of(c.dY);
+    a.endr = end_of(c.residual);
     a.samples = samples;
     a.positions = c.positions;
     a.groups = c.groups;
@@ -302,14 +328,15 @@ void group_norm_backward(const GroupGradCall& c, Pieces& ws, hipStream_t s)
             });
             if (!p.split() || !a.out) return;
             launch_join<true>(a, joined, s);
-            const dim3 all_blocks(
-                (unsigned)(blocks_across(a, 1 << 20) * p.slices));
+            GroupArgs b = a;
+            b.p = apply_plan(a, kAhead);
+            const dim3 turns((unsigned)(blocks_across(b, 1 << 20) * p.slices));
             if (p.even)
-                hipLaunchKernelGGL((k_group_dx<DT, true>), all_blocks,
-                                   dim3(256), 0, s, a);
+                hipLaunchKernelGGL((k_group_dx<DT, true>), turns, dim3(256), 0,
+                                   s, b);
             else
-                hipLaunchKernelGGL((k_group_dx<DT, false>), all_blocks,
-                                   dim3(256), 0, s, a);
+                hipLaunchKernelGGL((k_group_dx<DT, false>), turns, dim3(256),
+                                   0, s, b);
         });
     if (c.sums)
         launch_column_sums(a.pw, a.pb, rows, n, c.X.dtype, c.dweight.data,

@@ -22,17 +22,19 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
     const int64_t nb = gridDim.x / p.slices;
     const Place<EVEN> at(a, slice, t);
     const int64_t units = a.samples * p.chunks;
-    float w[8], b[8];
+    Eights<DT> w8, b8;
     if (!PARTS) {
-        load_eight<DT>(a.w, at.first(), at.count, 1.0f, w);
-        load_eight<DT>(a.b, at.first(), at.count, 0.0f, b);
+        w8.load(a.w, at.first(), at.count, 1.0f);
+        b8.load(a.b, at.first(), at.count, 0.0f);
     }
     for (int64_t j0 = blockIdx.x / p.slices * kSlabs<T>; j0 < units;
          j0 += nb * kSlabs<T>) {
         const Unit u(a, j0 + slab);
         RawEight<DT> x[IT];
-        load_slab<DT, IT>(x, a.X, a.ldx, u.row * a.ldx + at.first(), at.row,
-                          p.rows, u.rows, at.count);
+        load_slab<DT, IT>(x, a.X, (u.row + at.row) * a.ldx + at.first(),
+                          p.rows * a.ldx,
+                          (u.row + u.rows - 1) * a.ldx + at.first(),
+                          u.rows > 0 && at.count > 0, at.count, a.endx);
         float v[1][kK] = {};
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
@@ -40,8 +42,8 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 v[0][EVEN ? 0 : e] += there ? x[i].at(e) : 0.0f;
+            settle(v[0]);
         }
-        forget<DT, IT>(x);
         group_sums<T, 1, EVEN>(p, at, t, v, buf, stat);
         const float size = (float)((int64_t)u.rows * at.each(p));
         float mu[kK];
@@ -52,15 +54,16 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
         }
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
+            forget(x[i]);
             const bool there = at.row + i * p.rows < u.rows;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = x[i].at(e) - mu[EVEN ? 0 : e];
-                float& s = v[0][EVEN ? 0 : e];
-                if (there && e < at.count) s = fmaf(d, d, s);
+                const float d =
+                    there ? x[i].at(e) - mu[EVEN ? 0 : e] : 0.0f;
+                v[0][EVEN ? 0 : e] = fmaf(d, d, v[0][EVEN ? 0 : e]);
             }
+            settle(v[0]);
         }
-        forget<DT, IT>(x);
         group_sums<T, 1, EVEN>(p, at, t, v, buf + kBuf, stat + kStat<T>);
         if (u.rows > 0)
             for (int g = t; g < at.ng; g += T) {
@@ -82,11 +85,14 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
         for (int k = 0; k < kK; ++k)
             rs[k] = 1.0f /
                     sqrtf(stat[kStat<T> + at.group[k]] / size + a.eps);
-        const int64_t to = u.row * a.ldo + at.first();
+        float w[8], b[8];
+        w8.values(w);
+        b8.values(b);
+        int64_t to = here((u.row + at.row) * a.ldo + at.first());
 #pragma unroll
-        for (int i = 0; i < IT; ++i) {
-            const int r = at.row + i * p.rows;
-            if (r >= u.rows || at.count == 0) continue;
+        for (int i = 0; i < IT; ++i, to += p.rows * a.ldo) {
+            if (at.row + i * p.rows >= u.rows || at.count == 0) continue;
+            forget(x[i]);
             Eight<DT> y;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -94,10 +100,12 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
                 y.v[e] = fmaf((x[i].at(e) - mu[k]) * rs[k], w[e], b[e]);
             }
             act_values(a.act, y.v);
-            y.store(a.out, to + r * a.ldo, at.count);
+            store_some<DT, EVEN>(y, a.out, to, at.count);
         }
     }
 }
+
+constexpr int kAhead = 4;
 
 // Applies joined statistics.  A thread to 8 columns, positions in turn.
 template <int DT, bool EVEN>
@@ -111,9 +119,9 @@ __global__ __launch_bounds__(256) void k_group_apply(GroupArgs a)
     for_lanes<EVEN>(a, slice, [&](const Place<EVEN>& at, int row, int step,
                                   int count) {
         const int64_t c = at.first();
-        float w[8], b[8];
-        load_eight<DT>(a.w, c, count, 1.0f, w);
-        load_eight<DT>(a.b, c, count, 0.0f, b);
+        Eights<DT> w8, b8;
+        w8.load(a.w, c, count, 1.0f);
+        b8.load(a.b, c, count, 0.0f);
         for (int64_t j = blockIdx.x / p.slices; j < units; j += nb) {
             const Unit u(a, j);
             float mu[kK], rs[kK];
@@ -123,15 +131,20 @@ __global__ __launch_bounds__(256) void k_group_apply(GroupArgs a)
                 mu[k] = a.mean[g];
                 rs[k] = a.rstd[g];
             }
-            constexpr int kAhead = 4;
             for (int r0 = row; r0 < u.rows; r0 += step * kAhead) {
                 RawEight<DT> x[kAhead];
-                load_slab<DT, kAhead>(x, a.X, a.ldx, u.row * a.ldx + c, r0,
-                                      step, u.rows, count);
+                load_slab<DT, kAhead>(x, a.X, (u.row + r0) * a.ldx + c,
+                                      step * a.ldx,
+                                      (u.row + u.rows - 1) * a.ldx + c, true,
+                                      count, a.endx);
+                float w[8], b[8];
+                w8.values(w);
+                b8.values(b);
 #pragma unroll
                 for (int i = 0; i < kAhead; ++i) {
                     const int r = r0 + i * step;
                     if (r >= u.rows) continue;
+                    forget(x[i]);
                     Eight<DT> y;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
@@ -140,7 +153,8 @@ __global__ __launch_bounds__(256) void k_group_apply(GroupArgs a)
                                       b[e]);
                     }
                     act_values(a.act, y.v);
-                    y.store(a.out, (u.row + r) * a.ldo + c, count);
+                    store_some<DT, EVEN>(y, a.out,
+                                         (u.row + r) * a.ldo + c, count);
                 }
             }
         }
@@ -158,6 +172,7 @@ void group_norm(const GroupCall& c, Pieces& ws, hipStream_t s)
     a.b = c.bias.data;
     a.out = c.Y.data;
     a.ldx = c.X.ld;
+    a.endx = end_of(c.X);
     a.ldo = c.Y.ld;
     a.samples = samples;
     a.positions = c.positions;
@@ -192,12 +207,15 @@ void group_norm(const GroupCall& c, Pieces& ws, hipStream_t s)
         });
         if (!p.split()) return;
         launch_join<false>(a, nullptr, s);
+        GroupArgs b = a;
+        b.p = apply_plan(a, kAhead);
+        const dim3 turns((unsigned)(blocks_across(b, 1 << 20) * p.slices));
         if (p.even)
-            hipLaunchKernelGGL((k_group_apply<DT, true>), grid, dim3(256), 0,
-                               s, a);
+            hipLaunchKernelGGL((k_group_apply<DT, true>), turns, dim3(256), 0,
+                               s, b);
         else
-            hipLaunchKernelGGL((k_group_apply<DT, false>), grid, dim3(256), 0,
-                               s, a);
+            hipLaunchKernelGGL((k_group_apply<DT, false>), turns, dim3(256), 0,
+                               s, b);
     });
 }
 

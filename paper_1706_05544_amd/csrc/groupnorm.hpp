@@ -44,6 +44,7 @@ struct GroupArgs {
     void* out;
     int64_t ldx, ldg, ldr, ldo;
     int64_t samples, positions, groups;
+    int64_t endx, endg, endr;  // of the inputs, in values
     float eps;
     int act;
     float *mean, *rstd;     // written by the forward pass, else read
@@ -158,7 +159,7 @@ __device__ __forceinline__ void group_sums(
                 buf[q * kOne + at.row * wide + at.lane] = v[q][0];
         }
         slab_sync<T>();
-        width = (each + 7) / 8;
+        width = each / 8;
     } else {
         if (at.row < p.rows) {
 #pragma unroll
@@ -204,49 +205,159 @@ __device__ __forceinline__ void group_sums(
     slab_sync<T>();
 }
 
-// Values of a vector at a thread's columns; `fill` where it has none.
+// A vector's values at a thread's columns, or `fill`: loaded raw, so that
+// other loads can follow, and turned into 32 bits later.
 template <int DT>
-__device__ __forceinline__ void load_eight(const void* p, int64_t at,
-                                           int count, float fill,
-                                           float (&v)[8])
-{
-    Eight<DT> x;
-    if (p) x.load(p, at, count);
+struct Eights {
+    RawEight<DT> raw;
+    __device__ __forceinline__ void load(const void* p, int64_t at, int count,
+                                         float fill)
+    {
+        raw.ones();
+        if (fill == 0.0f) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = p ? x.v[e] : fill;
+            for (int k = 0; k < RawEight<DT>::kN; ++k)
+                raw.v[k] = (Elem<DT>)0.0f;
+        }
+        if (p) raw.load(p, at, count);
+    }
+    __device__ __forceinline__ void values(float (&v)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = raw.at(e);
+    }
+};
+
+// The first `count` of eight values to at, in as few stores as there are
+// powers of two in it.
+template <int DT, bool EVEN>
+__device__ __forceinline__ void store_some(const Eight<DT>& y, void* p,
+                                           int64_t at, int count)
+{
+    using T = Elem<DT>;
+    if (EVEN || count == 8) {
+        y.store(p, at, 8);
+        return;
+    }
+    typedef T Four __attribute__((ext_vector_type(4)));
+    typedef T Two __attribute__((ext_vector_type(2)));
+    typedef Four LooseFour __attribute__((aligned(sizeof(T))));
+    typedef Two LooseTwo __attribute__((aligned(sizeof(T))));
+    T* q = (T*)p + at;
+    const Four lo = {(T)y.v[0], (T)y.v[1], (T)y.v[2], (T)y.v[3]};
+    const Four hi = {(T)y.v[4], (T)y.v[5], (T)y.v[6], (T)y.v[7]};
+    if (count & 4) {
+        *(LooseFour*)q = lo;
+        q += 4;
+    }
+    const Four left = count & 4 ? hi : lo;
+    if (count & 2) {
+        *(LooseTwo*)q = Two{left[0], left[1]};
+        q += 2;
+    }
+    if (count & 1) *q = count & 2 ? left[2] : left[0];
 }
 
-// The pieces of a slab: all loads before the first use.  Past the last
-// position a whole piece is its last one again (a branch around a load would
-// have the next wait for it); `there` tells them apart.
+// The compiler is neither to keep what it made of these registers before (the
+// values in 32 bits, twice the room) nor to make it ahead of its turn.
+template <int DT>
+__device__ __forceinline__ void forget(RawEight<DT>& x)
+{
+#pragma unroll
+    for (int k = 0; k < RawEight<DT>::kN; ++k) asm volatile("" : "+v"(x.v[k]));
+}
+
+// These are to be made here (left to the end of a loop, what they are made of
+// stays in registers until then).
+template <int N>
+__device__ __forceinline__ void settle(float (&v)[N])
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) asm volatile("" : "+v"(v[k]));
+}
+
+// The values from `by` on take the first places (by < 8; the last are left).
+template <int DT>
+__device__ __forceinline__ void shift(RawEight<DT>& x, int by)
+{
+    typedef uint32_t U4 __attribute__((ext_vector_type(4)));
+    uint32_t d[4 * RawEight<DT>::kN];
+#pragma unroll
+    for (int k = 0; k < RawEight<DT>::kN; ++k) {
+        const U4 u = __builtin_bit_cast(U4, x.v[k]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[4 * k + e] = u[e];
+    }
+    constexpr int kWords = 4 * RawEight<DT>::kN;
+    if constexpr (DT != SVM_F32) {
+        if (by & 1)
+#pragma unroll
+            for (int e = 0; e < kWords; ++e)
+                d[e] = __builtin_amdgcn_alignbit(
+                    e + 1 < kWords ? d[e + 1] : 0u, d[e], 16);
+        by >>= 1;
+    }
+#pragma unroll
+    for (int step = 1; step < kWords; step *= 2)
+        if (by & step)
+#pragma unroll
+            for (int e = 0; e + step < kWords; ++e) d[e] = d[e + step];
+#pragma unroll
+    for (int k = 0; k < RawEight<DT>::kN; ++k)
+        x.v[k] = __builtin_bit_cast(
+            decltype(x.v[k] + x.v[k]),
+            U4{d[4 * k], d[4 * k + 1], d[4 * k + 2], d[4 * k + 3]});
+}
+
+// A value that the compiler knows nothing about: what is made of it is made
+// where it is used (offsets of all pieces, made ahead of a loop over slabs,
+// would take two registers for each piece and array).
+__device__ __forceinline__ int64_t here(int64_t v)
+{
+    int lo = (int)v, hi = (int)(v >> 32);
+    asm volatile("" : "+v"(lo), "+v"(hi));
+    return (int64_t)((uint64_t)(uint32_t)hi << 32 | (uint32_t)lo);
+}
+
+// The pieces of a slab: all loads before the first use.  `at` is the thread's
+// first value, `last` its value in the slab's last position: past that a piece
+// is the last one again (a branch around a load would have the next wait for
+// it).  Past the slice's columns a piece has what follows in memory, whose
+// sums nobody reads; where that would be past the array's end, the eight
+// values before the end are loaded and shifted into place.  (Arrays of fewer
+// than eight values: plans of one piece, values loaded one by one.)
 template <int DT, int IT>
 __device__ __forceinline__ void load_slab(RawEight<DT> (&x)[IT], const void* X,
-                                          int64_t ld, int64_t first, int row,
-                                          int step, int rows, int count)
+                                          int64_t at, int64_t step,
+                                          int64_t last, bool any, int count,
+                                          int64_t end)
 {
-    if (count == 8 && rows > 0) {
+    if (!any) {
 #pragma unroll
-        for (int i = 0; i < IT; ++i) {
-            const int r = row + i * step < rows ? row + i * step : rows - 1;
-            x[i].load(X, first + r * ld, 8);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < IT; ++i) {
-            const int r = row + i * step;
-            x[i].load(X, first + r * ld, r < rows ? count : 0);
-        }
+        for (int i = 0; i < IT; ++i) x[i].ones();
+        return;
     }
-}
-
-// The compiler is not to keep what it made of these registers (their values
-// in 32 bits, twice the room).
-template <int DT, int IT>
-__device__ __forceinline__ void forget(RawEight<DT> (&x)[IT])
-{
-    if constexpr (DT != SVM_F32) {
+    if constexpr (IT == 1) {
+        const int64_t a = at < last ? at : last;
+        x[0].load(X, a, a + 8 <= end ? 8 : count);
+    } else {
+        int64_t a = here(at);
 #pragma unroll
-        for (int i = 0; i < IT; ++i) asm volatile("" : "+v"(x[i].v[0]));
+        for (int i = 0; i < IT; ++i) {
+            int64_t b = a < last ? a : last;
+            b = b < end - 8 ? b : end - 8;
+            x[i].load(X, b, 8);
+            a += step;
+        }
+        if (last > end - 8) {
+            a = here(at);
+#pragma unroll
+            for (int i = 0; i < IT; ++i) {
+                const int64_t by = (a < last ? a : last) - (end - 8);
+                if (by > 0) shift(x[i], (int)by);
+                a += step;
+            }
+        }
     }
 }
 
@@ -277,7 +388,7 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
     Plan p{};
     p.each = channels / groups;
     p.parts_across = p.each > kWideCols ? up(p.each, kWideCols) : 1;
-    p.even = p.parts_across > 1 || p.each % 8 == 0;
+    p.even = p.each % 8 == 0;
     if (p.parts_across > 1) {
         p.groups = 1;
         p.cols = kWideCols;
@@ -315,11 +426,20 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
     p.chunk = positions;
     p.chunks = 1;
     if (!whole) {
+        if (p.parts_across == 1) {
+            // the rows whole, up to 512 columns: chunks make enough units
+            p.slices = up(channels, 512);
+            if (p.slices > groups) p.slices = groups;
+            p.groups = up(groups, p.slices);
+            p.slices = up(groups, p.groups);
+            p.cols = p.groups * p.each;
+            p.lanes = (int)up(p.cols, 8);
+        }
         i = p.lanes > 256 ? 3 : 2;
         const int64_t rows = kThreads[i] / p.lanes;
         const int64_t deep = most < 8 ? most : 8;
-        // chunks that fill the card's blocks, but no longer than fits
-        int64_t chunk = up(positions * units, 2048);
+        // chunks enough for two blocks to a CU, but no longer than fits
+        int64_t chunk = up(positions * samples * p.slices, 512);
         if (chunk < rows) chunk = rows;
         if (chunk > rows * deep) chunk = rows * deep;
         p.chunk = chunk < positions ? chunk : positions;
@@ -362,6 +482,19 @@ void for_plan(const Plan& p, F&& f)
             go.template operator()<512, 16>();
         }
     }
+}
+
+// The same for the kernel that applies joined sums: its chunks are as long as
+// its threads load ahead, or longer where there are enough of them.
+Plan apply_plan(const GroupArgs& a, int ahead)
+{
+    Plan p = a.p;
+    const int64_t turn = (p.lanes < 256 ? 256 / p.lanes : 1) * ahead;
+    const int64_t turns =
+        up(up(a.positions * a.samples * p.slices, turn), 8192);
+    p.chunk = turn * turns < a.positions ? turn * turns : a.positions;
+    p.chunks = up(a.positions, p.chunk);
+    return p;
 }
 
 // Blocks to a slice: each has a unit or more for each of its slabs.
@@ -420,6 +553,11 @@ __global__ __launch_bounds__(256) void k_group_join(GroupArgs a, float2* sums)
             a.rstd[g] = 1.0f / sqrtf(s1 / size + a.eps);
         }
     }
+}
+
+int64_t end_of(const svm_array& x)
+{
+    return x.rows > 0 ? (x.rows - 1) * x.ld + x.cols : 0;
 }
 
 template <bool SUMS>

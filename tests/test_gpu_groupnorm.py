@@ -173,7 +173,8 @@ SIZES = [(1, 1, 1, 1), (1, 1, 8, 8), (3, 1, 7, 7), (5, 1, 64, 8),
          (1, 70000, 8, 1), (1, 3000, 320, 1), (6, 1024, 130, 2),
          (2, 100, 4096, 1), (3, 7, 9000, 2), (1, 1, 50000, 1),
          (2, 33, 16384, 4), (1, 1, 131072, 64), (17, 64, 40, 1),
-         (40, 300, 65, 13)]
+         (40, 300, 65, 13), (1, 300, 1, 1), (3, 900, 3, 1), (2, 90, 5, 5),
+         (1, 40000, 7, 7)]
 
 
 @pytest.mark.parametrize("t", list(TYPES))
