@@ -11,8 +11,8 @@
 // tiles of 16 outputs one after another along the inputs.  Lane l of the
 // matrix instruction holds 8 consecutive inputs (l / 16) of output l % 16 in
 // each of the tile's four steps of 32 inputs: its four steps lie side by side,
-// 16 bytes.  Behind the codes the scales, 16 outputs side by side, group
-// after group.
+// 16 bytes.  Behind the codes the scales, in the same order of tiles: for each
+// of 16 outputs those of its groups in the tile (4, 2 or 1) side by side.
 #include "elem.hpp"
 #include "matmul.hpp"
 
@@ -104,8 +104,7 @@ __global__ __launch_bounds__(256) void k_pack4(PackArgs p)
             const bool bad = !(t <= kMost);
             const float sc = bad ? __builtin_nanf("") : scale_of<DT>(t);
             if (g == 0)
-                ((T*)p.scales)[(tile * p.groups + c * kGroups + q) * 16 + r] =
-                    (T)sc;
+                ((T*)p.scales)[(w * 16 + r) * kGroups + q] = (T)sc;
 #pragma unroll
             for (int s = 0; s < kSteps; ++s) {
                 uint32_t d = 0;
@@ -169,7 +168,7 @@ __global__ __launch_bounds__(256) void k_unpack4(UnpackArgs p)
         for (int s = 0; s < 4; ++s) {
             const int64_t at = c * 128 + s * 32 + g * 8;
             const float sc = (float)((const T*)p.scales)[
-                (tile * p.groups + ((c * 128 + s * 32) >> p.gshift)) * 16 + r];
+                ((w * 16 + r) << (7 - p.gshift)) + ((s * 32) >> p.gshift)];
             const floatx2 v0 = two32<0>(d[s]), v1 = two32<1>(d[s]),
                           v2 = two32<2>(d[s]), v3 = two32<3>(d[s]);
             Eight<DT> x;
@@ -227,137 +226,157 @@ struct Factor8 {
     }
 };
 
+constexpr int kWaves = 8;  // of a block
+
 struct Linear4Args {
     const void* X;
     const unsigned char* codes;
     const void* scales;
-    int64_t ldx, m, n, k, chunks, groups;
-    int gshift;
+    int64_t ldx, m, n, k, chunks;
     Epilogue e;
 };
 
-// Few rows: 16 NT outputs to a block and 16 MT rows, the inputs in chunks of
-// 128 taken in turn by its W waves, whose sums are joined at the end in a
-// fixed order.  The codes come straight from memory to the lane that
-// multiplies them, the next chunk's while this one's are used.
-// FEW: up to 4 rows, every fourth of the 16 that the matrix instruction takes,
-// so that a lane has one sum to scale and not four.
-template <int DT, int MT, int NT, int W, bool FEW>
-__global__ __launch_bounds__(64 * W) void k_linear4(Linear4Args p)
-{
+// What a lane has of a chunk of 128 inputs: codes and scales of NT tiles of
+// outputs, and its row's inputs.
+template <int DT, int NT, int GPC>
+struct Stage {
     using T = Elem<DT>;
-    constexpr int kCols = NT * 16, kPad = kCols + 4;
-    constexpr int kRegs = FEW ? 1 : 4;
-    __shared__ float red[W][MT * 16][kPad];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int i = lane & 15, g = lane >> 4;
-    const int64_t t0 = (int64_t)blockIdx.x * NT;
-    const int64_t r0 = (int64_t)blockIdx.y * (MT * 16);
-    const int64_t tiles = (p.n + 15) / 16;
-    float acc[MT][NT][kRegs];
-#pragma unroll
-    for (int a = 0; a < MT; ++a)
-#pragma unroll
-        for (int b = 0; b < NT; ++b)
-#pragma unroll
-            for (int v = 0; v < kRegs; ++v) acc[a][b][v] = 0.0f;
-    int64_t xrow[MT];  // -1: no row of X here
-#pragma unroll
-    for (int a = 0; a < MT; ++a) {
-        const int64_t row = FEW ? ((i & 3) == 0 ? i >> 2 : p.m)
-                                : r0 + a * 16 + i;
-        xrow[a] = row < p.m ? row * p.ldx : -1;
-    }
+    typedef T Scales __attribute__((ext_vector_type(GPC)));
     uint4v code[NT];
-    T scale[NT][4];
-    RawEight<DT> x[MT][4];
-    auto fetch = [&](int64_t c) {
+    Scales scale[NT];
+    RawEight<DT> x[4];
+
+    // t, row: the lane's tiles and where its row begins (beyond the last tile
+    // and row the last again, whose sums are not used)
+    __device__ __forceinline__ void load(const Linear4Args& p,
+                                         const int64_t (&t)[NT], int64_t row,
+                                         int64_t c, int lane)
+    {
+        const int i = lane & 15, g = lane >> 4;
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
-            // (past the last tile the last one again: its sums are not used)
-            const int64_t t = t0 + b < tiles ? t0 + b : tiles - 1;
-            code[b] = *(const uint4v*)(p.codes + (t * p.chunks + c) * 1024 +
-                                       lane * 16);
+            const int64_t w = t[b] * p.chunks + c;
+            code[b] = *(const uint4v*)(p.codes + w * 1024 + lane * 16);
+            scale[b] = ((const Scales*)p.scales)[w * 16 + i];
+        }
+        if (c * 128 + 128 <= p.k) {
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                scale[b][s] = ((const T*)p.scales)[
-                    (t * p.groups + ((c * 128 + s * 32) >> p.gshift)) * 16 + i];
-        }
-#pragma unroll
-        for (int a = 0; a < MT; ++a)
+                x[s].load(p.X, row + c * 128 + s * 32 + g * 8, 8);
+        } else {
 #pragma unroll
             for (int s = 0; s < 4; ++s) {
                 const int64_t at = c * 128 + s * 32 + g * 8;
-                x[a][s].load(p.X, xrow[a] + at,
-                             xrow[a] < 0 ? 0 : eight_of(p.k, at));
+                x[s].load(p.X, row + at, eight_of(p.k, at));
             }
-    };
-    if (wave < p.chunks) fetch(wave);
-    for (int64_t c = wave; c < p.chunks; c += W) {
-        uint4v d[NT];
-        float sc[NT][4];
-        Factor8<DT> f[MT][4];
-#pragma unroll
-        for (int b = 0; b < NT; ++b) {
-            d[b] = code[b];
-#pragma unroll
-            for (int s = 0; s < 4; ++s) sc[b][s] = (float)scale[b][s];
         }
+    }
+
+    // acc += this chunk's products.  A group's are added up by the matrix
+    // instruction and multiplied by its scale once.
+    template <int REGS>
+    __device__ __forceinline__ void add(float (&acc)[NT][REGS]) const
+    {
+        constexpr int kSteps = 4 / GPC;
 #pragma unroll
-        for (int a = 0; a < MT; ++a)
+        for (int q = 0; q < GPC; ++q) {
+            floatx4 part[NT];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) f[a][s].from(x[a][s]);
-        if (c + W < p.chunks) fetch(c + W);
+            for (int b = 0; b < NT; ++b) part[b] = floatx4{0, 0, 0, 0};
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+            for (int s = q * kSteps; s < (q + 1) * kSteps; ++s) {
+                short8v w[NT];
 #pragma unroll
-            for (int b = 0; b < NT; ++b) {
-                const short8v w = eight16<DT>(d[b][s]);
+                for (int b = 0; b < NT; ++b) w[b] = eight16<DT>(code[b][s]);
+                Factor8<DT> f;
+                f.from(x[s]);
 #pragma unroll
-                for (int a = 0; a < MT; ++a) {
-                    floatx4 part = {0, 0, 0, 0};
+                for (int r = Factor8<DT>::kParts - 1; r >= 0; --r)
 #pragma unroll
-                    for (int q = Factor8<DT>::kParts - 1; q >= 0; --q)
-                        part = mfma32<DT>(f[a][s].v[q], w, part);
-#pragma unroll
-                    for (int v = 0; v < kRegs; ++v)
-                        acc[a][b][v] = fmaf(part[v], sc[b][s], acc[a][b][v]);
-                }
+                    for (int b = 0; b < NT; ++b)
+                        part[b] = mfma32<DT>(f.v[r], w[b], part[b]);
             }
+#pragma unroll
+            for (int b = 0; b < NT; ++b)
+#pragma unroll
+                for (int v = 0; v < REGS; ++v)
+                    acc[b][v] =
+                        fmaf(part[b][v], (float)scale[b][q], acc[b][v]);
+        }
+    }
+};
+
+// Few rows: 16 NT outputs to a block and 16 rows, the inputs in chunks of 128
+// taken in turn by its waves, whose sums are joined at the end in a fixed
+// order.  The codes come straight from memory to the lane that multiplies
+// them, the next chunk's while this one's are used (two chunks ahead, and 4 or
+// 16 waves, were slower).
+// FEW: up to 4 rows, every fourth of the 16 that the matrix instruction takes,
+// so that a lane has one sum to scale and not four.
+// Bound by the read of the codes where they are many: 1 x 4096 over 16384 in
+// f16 8.4 us in a row of calls, 4.3 TB/s; by latency where they are few: 1 x
+// 784 over 1024 4.0 us, of which an empty launch is 2; and for more rows by
+// what is read of X from the caches, again for every 16 NT outputs: 32 x 4096
+// over 4096 in bf16 7.6 us, 128 rows 13.4.
+template <int DT, int NT, int GPC, bool FEW>
+__global__ __launch_bounds__(64 * kWaves) void k_linear4(Linear4Args p)
+{
+    constexpr int kCols = NT * 16, kPad = kCols + 4;
+    constexpr int kRegs = FEW ? 1 : 4;
+    constexpr int kRows = FEW ? 4 : 16;
+    __shared__ float red[kWaves][kRows][kPad];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int i = lane & 15, g = lane >> 4;
+    const int64_t t0 = (int64_t)blockIdx.x * NT;
+    const int64_t r0 = (int64_t)blockIdx.y * 16;
+    const int64_t tiles = (p.n + 15) / 16;
+    int64_t t[NT];
+#pragma unroll
+    for (int b = 0; b < NT; ++b) t[b] = t0 + b < tiles ? t0 + b : tiles - 1;
+    const int64_t at = FEW ? i >> 2 : r0 + i;
+    const int64_t row = (at < p.m ? at : p.m - 1) * p.ldx;
+    float acc[NT][kRegs] = {};
+    Stage<DT, NT, GPC> next;
+    if (wave < p.chunks) next.load(p, t, row, wave, lane);
+    for (int64_t c = wave; c < p.chunks; c += kWaves) {
+        const Stage<DT, NT, GPC> now = next;
+        if (c + kWaves < p.chunks) next.load(p, t, row, c + kWaves, lane);
+        now.template add<kRegs>(acc);
     }
 #pragma unroll
-    for (int a = 0; a < MT; ++a)
+    for (int b = 0; b < NT; ++b)
 #pragma unroll
-        for (int b = 0; b < NT; ++b)
-#pragma unroll
-            for (int v = 0; v < kRegs; ++v)
-                red[wave][a * 16 + (FEW ? g : g * 4 + v)][b * 16 + i] =
-                    acc[a][b][v];
+        for (int v = 0; v < kRegs; ++v)
+            red[wave][FEW ? g : g * 4 + v][b * 16 + i] = acc[b][v];
     __syncthreads();
-    for (int it = threadIdx.x; it < MT * 16 * NT * 2; it += 64 * W) {
-        const int row = it / (NT * 2), c0 = it % (NT * 2) * 8;
-        const int64_t r = r0 + row, j = t0 * 16 + c0;
-        const int count = eight_of(p.n, j);
-        if (r >= p.m || count == 0) continue;
-        Eight<DT> v, bias;
-        RawEight<DT> res;
+    // a thread to eight outputs
+    static_assert(kRows * NT * 2 <= 64 * kWaves, "one turn");
+    const int mine = (int)threadIdx.x / (NT * 2);
+    const int c0 = (int)threadIdx.x % (NT * 2) * 8;
+    const int64_t r = r0 + mine, j = t0 * 16 + c0;
+    const int count = mine < kRows && r < p.m ? eight_of(p.n, j) : 0;
+    if (count == 0) return;
+    Eight<DT> v;
+    RawEight<DT> bias, res;
+    if (p.e.bias) bias.load(p.e.bias, j, count);
+    if (p.e.residual) res.load(p.e.residual, r * p.e.ldr + j, count);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v.v[e] = bias.v[e] = 0.0f;
-        if (p.e.bias) bias.load(p.e.bias, j, count);
-        if (p.e.residual) res.load(p.e.residual, r * p.e.ldr + j, count);
+    for (int e = 0; e < 8; ++e) v.v[e] = 0.0f;
 #pragma unroll
-        for (int w = 0; w < W; ++w)
+    for (int w = 0; w < kWaves; ++w)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v.v[e] += red[w][row][c0 + e];
+        for (int e = 0; e < 8; ++e) v.v[e] += red[w][mine][c0 + e];
+    if (p.e.bias) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v.v[e] += bias.v[e];
-        act_values(p.e.act, v.v);
-        if (p.e.residual) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v.v[e] += res.at(e);
-        }
-        v.store(p.e.Y, r * p.e.ldy + j, count);
+        for (int e = 0; e < 8; ++e) v.v[e] += bias.at(e);
     }
+    act_values(p.e.act, v.v);
+    if (p.e.residual) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.v[e] += res.at(e);
+    }
+    v.store(p.e.Y, r * p.e.ldy + j, count);
 }
 
 unsigned tile_blocks(int64_t waves)
@@ -384,7 +403,16 @@ void launch_unpack(const svm_packed& w, int64_t cols, void* to, int64_t ld,
     });
 }
 
-constexpr int64_t kMostFewRows = 64;
+// Whether rows are few enough for k_linear4, whose time grows with them (and
+// a block's waves, with few inputs to each, are done sooner): 384 x 4096 over
+// 4096 in bf16 takes 33.0 us, unpacked and multiplied 38.2, 512 rows 41.8 and
+// 39.1; 1024 x 784 over 1024 takes 10.0 and 12.2, 2048 rows 20 and 16.1; in
+// 32 bits 256 x 4096 over 4096 51.7 and 59.0, 384 rows 72.3 and 71.7; 1024 x
+// 784 over 1024 21.2 and 23.7, 2048 rows 42 and 29.1.
+bool few_rows4(int64_t m, int64_t n, int64_t k)
+{
+    return m <= (n * k <= 1 << 20 ? 1024 : 384);
+}
 
 }  // namespace
 
@@ -417,7 +445,7 @@ void linear4(const Linear4Call& a, Pieces& ws, hipStream_t s)
     const Epilogue e{a.bias.data, a.residual.data, a.Y.data, nullptr,
                      a.residual.ld, a.Y.ld, 0, a.act};
     const Shape4 sh(a.W);
-    if (m > kMostFewRows) {
+    if (!few_rows4(m, a.W.rows, a.W.cols)) {
         // many rows: the weights once, as the product kernels take them
         const int64_t ld = (a.W.cols + 7) / 8 * 8;
         void* W = ws.take<char>(a.W.rows * ld * dtype_bytes(a.W.dtype));
@@ -431,25 +459,42 @@ void linear4(const Linear4Call& a, Pieces& ws, hipStream_t s)
         p.e = e;
         p.A = factor_of(a.X, true, ws, s);
         p.B = factor_of(w, true, ws, s);
+        p.narrow = p.dtype == SVM_F32;
         product(p, ws, s);
         return;
     }
     if (!ws.run) return;
     const Linear4Args k{a.X.data, (const unsigned char*)a.W.data,
                         scales_of(a.W), a.X.ld, m, a.W.rows, a.W.cols,
-                        sh.chunks, sh.groups, sh.gshift, e};
+                        sh.chunks, e};
     for_dtype(a.W.dtype, [&]<int DT>() {
-        auto go = [&]<int MT, int NT, int W, bool FEW>() {
-            hipLaunchKernelGGL(
-                (k_linear4<DT, MT, NT, W, FEW>),
-                dim3((unsigned)((sh.tiles + NT - 1) / NT),
-                     (unsigned)((m + MT * 16 - 1) / (MT * 16))),
-                dim3(64 * W), 0, s, k);
+        auto run = [&]<int NT, int GPC, bool FEW>() {
+            hipLaunchKernelGGL((k_linear4<DT, NT, GPC, FEW>),
+                               dim3((unsigned)((sh.tiles + NT - 1) / NT),
+                                    (unsigned)((m + 15) / 16)),
+                               dim3(64 * kWaves), 0, s, k);
         };
-        if (m <= 4) go.template operator()<1, 1, 8, true>();
-        else if (m <= 16) go.template operator()<1, 1, 8, false>();
-        else if (m <= 32) go.template operator()<2, 1, 8, false>();
-        else go.template operator()<4, 1, 8, false>();
+        auto go = [&]<int NT, bool FEW>() {
+            if (a.W.group == 32) run.template operator()<NT, 4, FEW>();
+            else if (a.W.group == 64) run.template operator()<NT, 2, FEW>();
+            else run.template operator()<NT, 1, FEW>();
+        };
+        // As many tiles of outputs to a block as leave a block for each CU:
+        // they share what is read of X, and in 32 bits its splitting (32 x
+        // 4096 over 4096, bf16: 11.2 us with one, 7.6 with two, 8.2 with
+        // four; 64 x 4096: 18.8, 11.6 and 8.4; 1 x 4096 over 16384: 9.5 with
+        // one, 8.5 with two, 8.6 with four).
+        const int64_t all = (m + 15) / 16 * sh.tiles;
+        if (m <= 4) {
+            if (all >= 512) go.template operator()<2, true>();
+            else go.template operator()<1, true>();
+        } else if (all >= 1024) {
+            go.template operator()<4, false>();
+        } else if (all >= 512) {
+            go.template operator()<2, false>();
+        } else {
+            go.template operator()<1, false>();
+        }
     });
 }
 

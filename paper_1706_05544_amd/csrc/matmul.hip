@@ -704,18 +704,20 @@ struct Split {
         }
     }
 
+    template <int PARTS>
     __device__ __forceinline__ void write(const Bf16x8 (&part)[kN][3],
                                           short* buf) const
     {
 #pragma unroll
         for (int q = 0; q < kN; ++q)
 #pragma unroll
-            for (int s = 0; s < 3; ++s)
+            for (int s = 0; s < PARTS; ++s)
                 *(Bf16x8*)(buf + s * R * kStep32 + lds[q]) = part[q][s];
     }
 
     // The last, partial step: `summed` summed values from k0 on, the others
     // zeros, straight to LDS.
+    template <int PARTS>
     __device__ __forceinline__ void tail(const Factor& f, int64_t x0, int64_t n,
                                          int64_t k0, int summed, short* buf)
     {
@@ -734,7 +736,7 @@ struct Split {
                        row < summed ? eight_of(n, x0 + piece * 8) : 0);
             three_parts(x.v, part);
 #pragma unroll
-            for (int s = 0; s < 3; ++s)
+            for (int s = 0; s < PARTS; ++s)
                 *(Bf16x8*)(buf + s * R * kStep32 + lds[q]) = part[s];
         }
     }
@@ -755,14 +757,21 @@ struct Split {
 // TFLOP/s of the 32-bit product), a library's 32-bit product 1043 with no cosine.
 // The matrix cores are at work in 43 % of the cycles; the splitting (vector
 // instructions) and the LDS traffic of three parts take the rest.
-template <int BM, int BN, int WGM, int WGN, bool AALONG, bool BALONG>
+// NARROW: B's values are those of bf16, so that h' is all of them: three
+// products, of which each reads a part of A's.  Unpacked 4-bit weights: 5000 x
+// 2048 over 784 97 us, with the six 138; 16384 x 2048 over 2048 397 and 645.
+template <int BM, int BN, int WGM, int WGN, bool AALONG, bool BALONG,
+          bool NARROW>
 __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
 {
     constexpr int NW = WGM * WGN, T = 64 * NW;
     constexpr int FM = BM / WGM / 16, FN = BN / WGN / 16;
     constexpr int kBK = kStep32, kSlab = slab_rows(FM) * FN * 16;
     constexpr int kB = 3 * BM * kBK;            // where B's planes begin
-    constexpr int kLds = 3 * (BM + BN) * kBK;   // values of a buffer
+    constexpr int kParts = NARROW ? 1 : 3;      // of B
+    constexpr int kPlanes = (3 * BM + kParts * BN) * kBK;
+    constexpr int kOut = NW / 2 * kSlab * 2;
+    constexpr int kLds = kPlanes > kOut ? kPlanes : kOut;  // of a buffer
     __shared__ __align__(1024) short lds0[kLds];
     __shared__ __align__(1024) short lds1[kLds];
 
@@ -801,8 +810,8 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
         SB::split(rb, pb);
     };
     auto write = [&](short* lds) {
-        sa.write(pa, lds);
-        sb.write(pb, lds + kB);
+        sa.template write<3>(pa, lds);
+        sb.template write<kParts>(pb, lds + kB);
     };
 
     floatx4 acc[FM][FN];
@@ -813,9 +822,11 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
 
     short8v ah[FM], bh[FN], am[FM], bm[FN], al[FM], bl[FN], an[FM], bn[FN];
     auto frags = [&](const short* lds, int plane, short8v* a, short8v* b) {
+        if (plane < kParts) {
 #pragma unroll
-        for (int g = 0; g < FN; ++g)
-            b[g] = fb.read(lds + kB + plane * BN * kBK, wj, g, 0, lane);
+            for (int g = 0; g < FN; ++g)
+                b[g] = fb.read(lds + kB + plane * BN * kBK, wj, g, 0, lane);
+        }
 #pragma unroll
         for (int f = 0; f < FM; ++f)
             a[f] = fa.read(lds + plane * BM * kBK, wi, f, 0, lane);
@@ -848,18 +859,23 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
         __builtin_amdgcn_sched_barrier(0);
         frags(cur, 2, al, bl);
         split();
-        multiply(ah, bm);
-        multiply(am, bh);
-        multiply(am, bm);
-        spread(3 * kMul, 1);
+        if constexpr (!NARROW) {
+            multiply(ah, bm);
+            multiply(am, bh);
+            multiply(am, bm);
+            spread(3 * kMul, 1);
+        } else {
+            multiply(am, bh);
+            spread(kMul, 1);
+        }
         meet<63>();
         write(cur);
         load();
         __builtin_amdgcn_sched_barrier(0);
         frags(oth, 0, an, bn);
-        multiply(ah, bl);
+        if constexpr (!NARROW) multiply(ah, bl);
         multiply(al, bh);
-        spread(2 * kMul, 0);
+        spread((NARROW ? 1 : 2) * kMul, 0);
         __builtin_amdgcn_sched_barrier(0);
     };
 
@@ -880,16 +896,18 @@ __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
         const int64_t k0 = (int64_t)whole * kBK;
         const int summed = (int)(p.k - k0);
         meet<63>();
-        sa.tail(p.A, i0, p.m, k0, summed, lds0);
-        sb.tail(p.B, j0, p.n, k0, summed, lds0 + kB);
+        sa.template tail<3>(p.A, i0, p.m, k0, summed, lds0);
+        sb.template tail<kParts>(p.B, j0, p.n, k0, summed, lds0 + kB);
         meet<63>();
         frags(lds0, 0, ah, bh);
         frags(lds0, 1, am, bm);
         frags(lds0, 2, al, bl);
-        multiply(ah, bl);
+        if constexpr (!NARROW) multiply(ah, bl);
         multiply(al, bh);
-        multiply(am, bm);
-        multiply(ah, bm);
+        if constexpr (!NARROW) {
+            multiply(am, bm);
+            multiply(ah, bm);
+        }
         multiply(am, bh);
         multiply(ah, bh);
     }
@@ -1107,22 +1125,29 @@ void launch16(const Args& a, hipStream_t s)
 }
 
 template <int BM, int BN, int WGM, int WGN>
-void launch32(const Args& a, hipStream_t s)
+void launch32(const Args& a, bool narrow, hipStream_t s)
 {
+    if (narrow) {
+        hipLaunchKernelGGL((k_product32<BM, BN, WGM, WGN, true, true, true>),
+                           dim3(a.tm * a.tn, (unsigned)a.splits),
+                           dim3(64 * WGM * WGN), 0, s, a);
+        return;
+    }
     for_factors(a, [&]<bool AALONG, bool BALONG>() {
-        hipLaunchKernelGGL((k_product32<BM, BN, WGM, WGN, AALONG, BALONG>),
+        hipLaunchKernelGGL((k_product32<BM, BN, WGM, WGN, AALONG, BALONG,
+                                        false>),
                            dim3(a.tm * a.tn, (unsigned)a.splits),
                            dim3(64 * WGM * WGN), 0, s, a);
     });
 }
 
 template <int OT>
-void launch_product(const Args& a, int tile, hipStream_t s)
+void launch_product(const Args& a, int tile, bool narrow, hipStream_t s)
 {
     if constexpr (OT == SVM_F32) {
-        if (tile == 256) launch32<128, 256, 2, 4>(a, s);
-        else if (tile == 128) launch32<128, 128, 2, 4>(a, s);
-        else launch32<64, 64, 2, 2>(a, s);
+        if (tile == 256) launch32<128, 256, 2, 4>(a, narrow, s);
+        else if (tile == 128) launch32<128, 128, 2, 4>(a, narrow, s);
+        else launch32<64, 64, 2, 2>(a, narrow, s);
     } else {
         // Tiles of 128: eight waves, two to a SIMD, each of which waits while
         // the other multiplies (4096 x 1024 over 1024: 15.0 us, with four
@@ -1273,9 +1298,10 @@ void product(const Product& p, Pieces& ws, hipStream_t s)
         q.e.Y = (void*)on(a.e.Y, a.e.ldy);
         q.e.Z = (void*)on(a.e.Z, a.e.ldz);
         q.e.residual = on(a.e.residual, a.e.ldr);
-        if (f32) launch_product<SVM_F32>(q, tile, s);
-        else if (p.dtype == SVM_BF16) launch_product<SVM_BF16>(q, tile, s);
-        else launch_product<SVM_F16>(q, tile, s);
+        if (f32) launch_product<SVM_F32>(q, tile, p.narrow, s);
+        else if (p.dtype == SVM_BF16)
+            launch_product<SVM_BF16>(q, tile, false, s);
+        else launch_product<SVM_F16>(q, tile, false, s);
     }
     if (a.splits > 1) {
         const int64_t nb = (p.m * ((p.n + 7) / 8) + 255) / 256;

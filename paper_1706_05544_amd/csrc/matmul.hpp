@@ -28,6 +28,8 @@ struct Product {
     int64_t m, n, k;
     int32_t dtype;
     Epilogue e;
+    // SVM_F32, both factors along: the values of B are those of bf16 too
+    bool narrow = false;
 };
 
 // Whether the product reads these values as they are: with ld at most

@@ -202,8 +202,24 @@ def test_large(m, k, n, t):
     check(X, nv.svm_pack_weights(W, 64), b, R, "gelu", t)
 
 
+# both sides of where rows count as many, odd sizes, every number of tiles to
+# a block; many rows in 32 bits take three products for six
 @pytest.mark.parametrize("t", list(TYPES))
-@pytest.mark.parametrize("m", [3, 24, 50, 90])
+@pytest.mark.parametrize("m,k,n", [(1024, 100, 90), (1025, 100, 90),
+                                   (1100, 33, 17), (384, 1030, 1040),
+                                   (385, 1030, 1040), (500, 2052, 700),
+                                   (2, 130, 8200), (16, 130, 8200),
+                                   (16, 130, 16500), (33, 130, 2800)])
+def test_many_rows_and_many_tiles(m, k, n, t):
+    g = gen(m + n)
+    X, W = rnd(g, m, k, t=t), rnd(g, n, k, by=k ** -0.5, t=t)
+    b, R = rnd(g, n, t=t), rnd(g, m, n, t=t)
+    for group in (32, 128):
+        check(X, nv.svm_pack_weights(W, group), b, R, "gelu", t)
+
+
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("m", [3, 24, 50, 90, 1030])
 def test_strides_in_place_and_nothing_beside(m, t):
     g = gen(m + 1)
     k, n = 100, 90
@@ -236,7 +252,7 @@ def test_rows_do_not_depend_on_each_other(t):
     g = gen(11)
     P = nv.svm_pack_weights(rnd(g, 60, 200, by=0.1, t=t), 32)
     W = nv.svm_unpack_weights(P).double()
-    for m in (4, 16, 40, 80):
+    for m in (4, 16, 40, 1040):
         X = rnd(g, m, 200, t=t)
         clean = nv.svm_linear_packed(X, P)
         bad = X.clone()
@@ -265,26 +281,30 @@ def test_a_group_that_is_not_a_number_shows_in_its_output_alone():
 
 def test_32_bit_inputs_keep_all_their_bits():
     # weights of 6 and 0 (scale 1): six times the input, whose three parts of
-    # eight bits hold it exactly; two additions in 32 bits, each off by 2^-23
+    # eight bits hold it exactly from 2^-109 on; two additions in 32 bits, each
+    # off by 2^-23
     k = 64
     W = torch.zeros(k, 128, device=DEV)
     W[:, :64].fill_diagonal_(6.0)
     P = nv.svm_pack_weights(W, 64)
     g = gen(13)
-    for m in (1, 16, 33):
+    for m in (1, 16, 33, 1030):
         x = torch.randn(m, 128, generator=g, device=DEV)
         x[:, 64:] = 0.0
         for by in (1.0, 2.0 ** -100, 2.0 ** 115):
             Y = nv.svm_linear_packed(x * by, P).double()
             want = x[:, :64].double() * by * 6.0
-            assert bool(((Y - want).abs() <= 2 * E * want.abs()).all())
+            # (the third part of x below 2^-109 falls under bf16's smallest
+            # step, 2^-133, and is cut by less than that: six times it here)
+            lim = 2 * E * want.abs() + 6 * 2.0 ** -133
+            assert bool(((Y - want).abs() <= lim).all())
 
 
 def test_streams_and_replays():
     g = gen(14)
-    W, R = rnd(g, 300, 260, t="bf16"), rnd(g, 300, 90, t="bf16").t()
+    W, R = rnd(g, 300, 260, t="bf16"), rnd(g, 300, 1090, t="bf16").t()
     P = nv.svm_pack_weights(W, 64)
-    X = {m: rnd(g, 260, m, t="bf16").t() for m in (2, 30, 90)}
+    X = {m: rnd(g, 260, m, t="bf16").t() for m in (2, 30, 1090)}
     side = torch.cuda.Stream()
     for m, x in X.items():
         want = nv.svm_linear_packed(x, P, None, R[:m], act="gelu")
