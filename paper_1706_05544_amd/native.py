@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as ct
 import os
+import struct
 from typing import Optional
 
 import numpy as np
@@ -273,11 +274,6 @@ def _check(rc: int) -> int:
 
 def _is_torch(x) -> bool:
     return type(x).__module__.startswith("torch")
-
-
-def _is_tensor(x) -> bool:
-    import torch
-    return isinstance(x, torch.Tensor)
 
 
 def _torch_sparse_csr():
@@ -1017,10 +1013,6 @@ def svm_adamw_state(m, v, m_scale, v_scale, stream=None):
     return mo, vo
 
 
-_GRAD_ROW = np.dtype([("data", "u8"), ("n", "i8"), ("dtype", "i4"),
-                      ("pad", "i4")])
-
-
 def svm_grad_norm(grads, max_norm: float = float("inf"),
                   grad_scale: float = 1.0, stream=None):
     """The norm of the tensors `grads` taken as one vector, times
@@ -1033,30 +1025,35 @@ def svm_grad_norm(grads, max_norm: float = float("inf"),
     lib = load()
     c = _Call(grads[0], stream)
     T = torch.Tensor
-    if not all(map(_is_tensor, grads)) or \
-            set(map(T.get_device, grads)) != {c.index}:
+    try:
+        devices = set(map(T.get_device, grads))
+    except TypeError:
+        devices = ()
+    if devices != {c.index}:
         raise SvmError(SVM_E_INVALID, "the gradients must be tensors on one "
                        "device")
     if not all(map(T.is_contiguous, grads)):
         grads = [g.contiguous() for g in grads]
-    types = [_DTYPES.get(g.dtype) for g in grads]
-    if None in types:
-        raise SvmError(SVM_E_UNSUPPORTED, "gradients must be float32, bfloat16 "
-                       "or float16")
     c.keep += grads
-    tab = np.zeros(len(grads), dtype=_GRAD_ROW)
-    tab["data"] = list(map(T.data_ptr, grads))
-    tab["n"] = list(map(T.numel, grads))
-    tab["dtype"] = types
+    # svm_grad of each: an address, a length, a type
+    n = len(grads)
+    tab = [0] * (3 * n)
+    try:
+        tab[2::3] = [_DTYPES[g.dtype] for g in grads]
+    except KeyError:
+        raise SvmError(SVM_E_UNSUPPORTED, "gradients must be float32, bfloat16 "
+                       "or float16") from None
+    tab[0::3] = map(T.data_ptr, grads)
+    tab[1::3] = map(T.numel, grads)
+    tab = struct.pack("=" + "Qqq" * n, *tab)
     norm, factor = c.empty((), torch.float32), c.empty((), torch.float32)
     size = ct.c_int64()
-    _check(lib.svm_grad_norm_workspace(_np_ptr(tab), len(tab),
-                                       ct.byref(size)))
+    _check(lib.svm_grad_norm_workspace(tab, n, ct.byref(size)))
     ws = c.work(size.value)
     c.ready()
-    _check(lib.svm_grad_norm(_np_ptr(tab), len(tab), grad_scale, max_norm,
-                             norm.data_ptr(), factor.data_ptr(), ws,
-                             size.value, c.index, c.handle))
+    _check(lib.svm_grad_norm(tab, n, grad_scale, max_norm, norm.data_ptr(),
+                             factor.data_ptr(), ws, size.value, c.index,
+                             c.handle))
     c.done()
     return norm, factor
 
@@ -1140,34 +1137,46 @@ def svm_group_norm_backward(dY, X, groups: int, mean, rstd, weight=None,
 
 
 class PackedWeights:
-    """Weights in 4 bits, as svm_pack_weights makes them: `data` (uint8, on the
-    device) in the library's own order, and what it stands for: `shape`
+    """Weights in 4 bits, as svm_pack_weights makes them: `data` (uint8, on
+    the device) in the library's own order, and what it stands for: `shape`
     (outputs, inputs), `group` and `dtype`.  data may be saved and loaded;
     PackedWeights(data, shape, group, dtype) makes them from it again."""
 
     def __init__(self, data, shape, group: int, dtype):
-        self.data, self.group, self.dtype = data, int(group), dtype
-        self.shape = tuple(int(x) for x in shape)
-        if not _is_tensor(data) or not data.is_contiguous() or \
-                data.element_size() != 1 or len(self.shape) != 2:
+        if not _is_torch(data) or not data.is_contiguous() or \
+                data.element_size() != 1 or len(shape) != 2:
             raise SvmError(SVM_E_INVALID, "packed weights are a contiguous "
                            "tensor of bytes with a shape of two")
+        self._data, self.group, self.dtype = data, int(group), dtype
+        self.shape = tuple(int(x) for x in shape)
+        self._no_work = set()  # numbers of rows that need no workspace
+        self._arr = None
+
+    @property
+    def data(self):
+        return self._data
 
     def __repr__(self):
         return "PackedWeights(%d x %d, groups of %d, %s)" % (
             *self.shape, self.group, self.dtype)
 
+    def _on(self, c: _Call) -> svm_packed:
+        """The C structure, for a call."""
+        if self._data.get_device() != c.index:
+            raise SvmError(SVM_E_INVALID, "the packed weights are on another "
+                           "device")
+        c.keep.append(self._data)
+        if self._arr is None:
+            self._arr = svm_packed(
+                self._data.data_ptr(), self._data.numel(), *self.shape,
+                self.group, _DTYPES.get(self.dtype, -1))
+        return self._arr
 
-def _packed(c, P):
-    """svm_packed of a PackedWeights on the call's device."""
+
+def _packed(P) -> PackedWeights:
     if not isinstance(P, PackedWeights):
         raise SvmError(SVM_E_INVALID, "packed weights must be a PackedWeights")
-    if P.data.get_device() != c.index:
-        raise SvmError(SVM_E_INVALID, "the packed weights are on another "
-                       "device")
-    c.keep.append(P.data)
-    return svm_packed(P.data.data_ptr(), P.data.numel(), *P.shape, P.group,
-                       _DTYPES.get(P.dtype, -1))
+    return P
 
 
 def svm_pack_weights(W, group: int = 64, stream=None) -> PackedWeights:
@@ -1182,7 +1191,7 @@ def svm_pack_weights(W, group: int = 64, stream=None) -> PackedWeights:
                                ct.byref(size)))
     P = PackedWeights(c.empty((size.value,), torch.uint8), (a.rows, a.cols),
                       group, W.dtype)
-    p = _packed(c, P)
+    p = P._on(c)
     c.ready()
     _check(lib.svm_pack_weights(ct.byref(a), ct.byref(p), c.index, c.handle))
     c.done()
@@ -1193,8 +1202,8 @@ def svm_unpack_weights(P: PackedWeights, stream=None):
     """The weights that P stands for, exactly, in their own type."""
     import torch
     lib = load()
-    c = _Call(P.data, stream)
-    p = _packed(c, P)
+    c = _Call(_packed(P).data, stream)
+    p = P._on(c)
     W = c.empty(P.shape, P.dtype)
     c.ready()
     _check(lib.svm_unpack_weights(ct.byref(p), ct.byref(c.arr(W, "W", True)),
@@ -1209,17 +1218,22 @@ def svm_linear_packed(X, P: PackedWeights, bias=None, residual=None,
     receives Y when given (it may be `residual`)."""
     lib = load()
     c = _Call(X, stream)
-    a, p = c.arr(X, "X"), _packed(c, P)
+    a, p = c.arr(X, "X"), _packed(P)._on(c)
     Y = out if out is not None else X.new_empty(X.shape[:-1] + (p.rows,))
-    need = ct.c_int64()
-    _check(lib.svm_linear_packed_workspace(ct.byref(a), ct.byref(p),
-                                     ct.byref(need)))
-    ws = c.work(need.value)
+    need, ws = 0, None
+    if a.rows not in P._no_work:
+        size = ct.c_int64()
+        _check(lib.svm_linear_packed_workspace(ct.byref(a), ct.byref(p),
+                                               ct.byref(size)))
+        need = size.value
+        ws = c.work(need)
+        if not need:
+            P._no_work.add(a.rows)
     b, r = c.arr(bias, "bias"), c.arr(residual, "residual")
     c.ready()
     _check(lib.svm_linear_packed(ct.byref(a), ct.byref(p), _ref(b), _ref(r),
-                           _act(act), ct.byref(c.arr(Y, "out", True)), ws,
-                           need.value, c.index, c.handle))
+                                 _act(act), ct.byref(c.arr(Y, "out", True)),
+                                 ws, need, c.index, c.handle))
     c.done()
     if out is not None:
         _written(out)
