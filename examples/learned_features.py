@@ -6,7 +6,12 @@
 2. A residual feature network on the ten-class images, trained under the
    squared hinge loss in bfloat16 with 8-bit AdamW states, and a one-vs-rest
    SVM with a linear kernel on its features, against the same SVM on the
-   images.
+   images; then the network in 4-bit weights, its head's classes against
+   those of the weights as trained.
+3. The same on patches of the images, with group norm over all of an image's
+   patches.
+
+Every step's gradient norm is clipped.
 
 Synthetic data from paper_1706_05544_amd/workloads.py.  Needs the GPU.
 """
@@ -23,7 +28,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_1706_05544_amd import native as nv  # noqa: E402
 from paper_1706_05544_amd import workloads  # noqa: E402
 from paper_1706_05544_amd.features import (CosineFeatures,  # noqa: E402
-                                           FeatureNet)
+                                           FeatureNet, patches)
 
 
 def timed(what, f):
@@ -51,28 +56,30 @@ def cosine(n, features):
     return acc
 
 
-def network(n, width, blocks, epochs, batch=512):
+def network(n, width, blocks, epochs, batch=512, groups=0):
     w = workloads.make("C4", n=n, n_test=n // 5)
     X, Xt = (torch.from_numpy(a).cuda() for a in (w.X, w.Xt))
     labels = torch.from_numpy(w.y).cuda()
     print("ten classes of images, %d x %d" % X.shape)
-    net = FeatureNet(w.d, width, blocks, w.n_classes, dtype=torch.bfloat16,
-                     bits=8)
-    Xb = X.bfloat16()
+    cut = lambda A: patches(A, 28, 4) if groups else A  # noqa: E731
+    Xb, Xtb = cut(X.bfloat16()), cut(Xt.bfloat16())
+    net = FeatureNet(Xb.shape[-1], width, blocks, w.n_classes,
+                     dtype=torch.bfloat16, bits=8, groups=groups,
+                     positions=Xb.shape[1] if groups else 1)
     order = torch.Generator(device="cuda").manual_seed(0)
 
     def epoch():
         losses = []
         for rows in torch.randperm(n, generator=order,
                                    device="cuda").split(batch):
-            losses.append(net.step(Xb[rows], labels[rows], lr=1e-3))
+            losses.append(net.step(Xb[rows], labels[rows], lr=1e-3, clip=1.0))
         return torch.stack(losses).mean()
 
     for e in range(epochs):
         loss = timed("epoch %d" % (e + 1), epoch)
         print("    loss %.4f" % float(loss))
     F, Ft = timed("features", lambda: (net.features(Xb).float(),
-                                       net.features(Xt.bfloat16()).float()))
+                                       net.features(Xtb).float()))
     acc = []
     for what, A, At in (("images", X, Xt), ("features", F, Ft)):
         m = timed("one-vs-rest linear SVM on the " + what,
@@ -81,6 +88,13 @@ def network(n, width, blocks, epochs, batch=512):
         acc.append(float(np.mean(nv.svm_predict_labels(m, At).cpu().numpy()
                                  == w.yt)))
     print("  accuracy: images %.4f, features %.4f" % tuple(acc))
+    served = net.packed()
+    timed("one image's scores, 4-bit weights", lambda: served.scores(Xtb[:1]))
+    top = [m.scores(Xtb).float().argmax(1).cpu().numpy()
+           for m in (net, served)]
+    acc += [float(np.mean(t == w.yt)) for t in top]
+    print("  accuracy of the head: %.4f, in 4-bit weights %.4f"
+          % tuple(acc[2:]))
     return acc
 
 
@@ -94,3 +108,4 @@ if __name__ == "__main__":
     a = ap.parse_args()
     cosine(a.n, a.features)
     network(a.n, a.width, a.blocks, a.epochs)
+    network(a.n, a.width // 32, a.blocks, a.epochs, groups=4)
