@@ -557,7 +557,8 @@ __global__ __launch_bounds__(256) void k_group_join(GroupArgs a, float2* sums)
 
 int64_t end_of(const svm_array& x)
 {
-    return x.rows > 0 ? (x.rows - 1) * x.ld + x.cols : 0;
+    if (x.rows <= 0) return 0;
+    return (int64_t)((uint64_t)(x.rows - 1) * (uint64_t)x.ld + x.cols);
 }
 
 template <bool SUMS>
