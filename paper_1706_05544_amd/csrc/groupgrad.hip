@@ -73,8 +73,8 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
     const Plan& p = a.p;
     const int slab = threadIdx.x / T, t = threadIdx.x % T;
     float *buf = bufs[slab], *stat = stats[slab];
-    const int64_t slice = blockIdx.x % p.slices;
-    const int64_t nb = gridDim.x / p.slices;
+    const int64_t slice = blockIdx.x % (unsigned)p.slices;
+    const int64_t nb = gridDim.x / (unsigned)p.slices;
     const Place<EVEN> at(a, slice, t);
     const int64_t units = a.samples * p.chunks;
     Eights<DT> w8, b8;
@@ -82,7 +82,7 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
     b8.load(a.b, at.first(), at.count, 0.0f);
     float sb[8] = {}, sw[8] = {};  // over the block's units
     const float over = 1.0f / (float)(a.positions * p.each);
-    for (int64_t j0 = blockIdx.x / p.slices * kSlabs<T>; j0 < units;
+    for (int64_t j0 = blockIdx.x / (unsigned)p.slices * kSlabs<T>; j0 < units;
          j0 += nb * kSlabs<T>) {
         const Unit u(a, j0 + slab);
         RawEight<DT> x[IT], g[IT];
@@ -130,7 +130,9 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
             settle(v[1]);
         }
         if (!PARTS && !a.out) continue;
-        group_sums<T, 2, EVEN>(p, at, t, v, buf, stat);
+        group_sums<T, 2, EVEN>(
+            p, at, t, v, buf, stat,
+            [&](int, float s) { return PARTS ? s : s * over; });
         if (PARTS) {
             if (u.rows > 0)
                 for (int q = t; q < at.ng; q += T) {
@@ -145,8 +147,8 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
         float s1[kK], s2[kK];
 #pragma unroll
         for (int k = 0; k < kK; ++k) {
-            s1[k] = stat[at.group[k]] * over;
-            s2[k] = stat[kStat<T> + at.group[k]] * over;
+            s1[k] = stat[at.group[k]];
+            s2[k] = stat[kStat<T> + at.group[k]];
         }
         int64_t to = here((u.row + at.row) * a.ldo + at.first());
         constexpr int kAhead = IT < 4 ? IT : 4;
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
         }
     }
     __syncthreads();
-    const int64_t to = blockIdx.x / p.slices * (a.groups * p.each) + at.col;
+    const int64_t to = blockIdx.x / (unsigned)p.slices * (a.groups * p.each) + at.col;
     for (int c = threadIdx.x; c < 2 * at.cols; c += kSlabThreads<T>) {
         const int q = c >= at.cols, d = c - q * at.cols;
         float sum = 0.0f;
@@ -207,8 +209,8 @@ __global__ __launch_bounds__(256) void k_group_dx(GroupArgs a)
 {
     constexpr int kK = Place<EVEN>::kK;
     const Plan& p = a.p;
-    const int64_t slice = blockIdx.x % p.slices;
-    const int64_t nb = gridDim.x / p.slices;
+    const int64_t slice = blockIdx.x % (unsigned)p.slices;
+    const int64_t nb = gridDim.x / (unsigned)p.slices;
     const int64_t units = a.samples * p.chunks;
     const float over = 1.0f / (float)(a.positions * p.each);
     for_lanes<EVEN>(a, slice, [&](const Place<EVEN>& at, int row, int step,
@@ -217,7 +219,7 @@ __global__ __launch_bounds__(256) void k_group_dx(GroupArgs a)
         Eights<DT> w8, b8;
         w8.load(a.w, c, count, 1.0f);
         b8.load(a.b, c, count, 0.0f);
-        for (int64_t j = blockIdx.x / p.slices; j < units; j += nb) {
+        for (int64_t j = blockIdx.x / (unsigned)p.slices; j < units; j += nb) {
             const Unit u(a, j);
             float mu[kK], rs[kK], s1[kK], s2[kK];
             load_stats<EVEN>(a, at, u.n, mu, rs);

@@ -18,8 +18,8 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
     const Plan& p = a.p;
     const int slab = threadIdx.x / T, t = threadIdx.x % T;
     float *buf = bufs[slab], *stat = stats[slab];
-    const int64_t slice = blockIdx.x % p.slices;
-    const int64_t nb = gridDim.x / p.slices;
+    const int64_t slice = blockIdx.x % (unsigned)p.slices;
+    const int64_t nb = gridDim.x / (unsigned)p.slices;
     const Place<EVEN> at(a, slice, t);
     const int64_t units = a.samples * p.chunks;
     Eights<DT> w8, b8;
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
         w8.load(a.w, at.first(), at.count, 1.0f);
         b8.load(a.b, at.first(), at.count, 0.0f);
     }
-    for (int64_t j0 = blockIdx.x / p.slices * kSlabs<T>; j0 < units;
+    for (int64_t j0 = blockIdx.x / (unsigned)p.slices * kSlabs<T>; j0 < units;
          j0 += nb * kSlabs<T>) {
         const Unit u(a, j0 + slab);
         RawEight<DT> x[IT];
@@ -44,12 +44,13 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
                 v[0][EVEN ? 0 : e] += there ? x[i].at(e) : 0.0f;
             settle(v[0]);
         }
-        group_sums<T, 1, EVEN>(p, at, t, v, buf, stat);
         const float size = (float)((int64_t)u.rows * at.each(p));
+        group_sums<T, 1, EVEN>(p, at, t, v, buf, stat,
+                               [&](int, float s) { return s / size; });
         float mu[kK];
 #pragma unroll
         for (int k = 0; k < kK; ++k) {
-            mu[k] = stat[at.group[k]] / size;
+            mu[k] = stat[at.group[k]];
             v[0][k] = 0.0f;
         }
 #pragma unroll
@@ -64,11 +65,14 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
             }
             settle(v[0]);
         }
-        group_sums<T, 1, EVEN>(p, at, t, v, buf + kBuf, stat + kStat<T>);
+        group_sums<T, 1, EVEN>(
+            p, at, t, v, buf + kBuf, stat + kStat<T>, [&](int, float s) {
+                return PARTS ? s : 1.0f / sqrtf(s / size + a.eps);
+            });
         if (u.rows > 0)
             for (int g = t; g < at.ng; g += T) {
                 const int64_t ng = u.n * a.groups + at.g0 + g;
-                const float m = stat[g] / size, q = stat[kStat<T> + g];
+                const float m = stat[g], q = stat[kStat<T> + g];
                 if (PARTS) {
                     const int64_t cp =
                         p.parts_across > 1 ? slice % p.parts_across : 0;
@@ -76,15 +80,13 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
                         make_float2(m, q);
                 } else {
                     if (a.mean) a.mean[ng] = m;
-                    if (a.rstd) a.rstd[ng] = 1.0f / sqrtf(q / size + a.eps);
+                    if (a.rstd) a.rstd[ng] = q;
                 }
             }
         if (PARTS) continue;
         float rs[kK];
 #pragma unroll
-        for (int k = 0; k < kK; ++k)
-            rs[k] = 1.0f /
-                    sqrtf(stat[kStat<T> + at.group[k]] / size + a.eps);
+        for (int k = 0; k < kK; ++k) rs[k] = stat[kStat<T> + at.group[k]];
         float w[8], b[8];
         w8.values(w);
         b8.values(b);
@@ -113,8 +115,8 @@ __global__ __launch_bounds__(256) void k_group_apply(GroupArgs a)
 {
     constexpr int kK = Place<EVEN>::kK;
     const Plan& p = a.p;
-    const int64_t slice = blockIdx.x % p.slices;
-    const int64_t nb = gridDim.x / p.slices;
+    const int64_t slice = blockIdx.x % (unsigned)p.slices;
+    const int64_t nb = gridDim.x / (unsigned)p.slices;
     const int64_t units = a.samples * p.chunks;
     for_lanes<EVEN>(a, slice, [&](const Place<EVEN>& at, int row, int step,
                                   int count) {
@@ -122,7 +124,7 @@ __global__ __launch_bounds__(256) void k_group_apply(GroupArgs a)
         Eights<DT> w8, b8;
         w8.load(a.w, c, count, 1.0f);
         b8.load(a.b, c, count, 0.0f);
-        for (int64_t j = blockIdx.x / p.slices; j < units; j += nb) {
+        for (int64_t j = blockIdx.x / (unsigned)p.slices; j < units; j += nb) {
             const Unit u(a, j);
             float mu[kK], rs[kK];
 #pragma unroll

@@ -22,6 +22,21 @@ namespace {
 
 constexpr int64_t kWideCols = 4096;
 
+// Division by d of numbers n with n d < 2^32: one multiplication (by 2^32 / d
+// rounded up: too much by n / 2^32, less than the 1 / d to the next quotient).
+// Blocks are short, and a handful of divisions would be most of their work.
+struct Divisor {
+    uint32_t d, m;
+    __host__ __device__ Divisor(uint32_t d = 1)
+        : d(d), m((uint32_t)((((uint64_t)1 << 32) + d - 1) / d))
+    {
+    }
+    __device__ __forceinline__ int operator()(int n) const
+    {
+        return d == 1 ? n : (int)__umulhi((uint32_t)n, m);
+    }
+};
+
 // How a call is cut up.  All by the sizes and the type.
 struct Plan {
     int threads, pieces;   // of a slab: T, and IT pieces of 8 for each
@@ -32,6 +47,7 @@ struct Plan {
     int64_t slices, parts_across;  // of a row; of a group
     int64_t chunk, chunks; // positions of a chunk; chunks of a sample
     bool even;             // the 8 columns of a thread lie in one group
+    Divisor by_lanes, by_each, by_wide;  // lanes; each; 8 lanes
     __host__ __device__ bool split() const
     {
         return chunks > 1 || parts_across > 1;
@@ -75,8 +91,8 @@ struct Place {
     __device__ __forceinline__ Place(const GroupArgs& a, int64_t slice, int t)
     {
         const Plan& p = a.p;
-        lane = t % p.lanes;
-        row = t / p.lanes;
+        row = p.by_lanes(t);
+        lane = t - row * p.lanes;
         if (p.parts_across > 1) {
             g0 = slice / p.parts_across;
             const int64_t c = (slice - g0 * p.parts_across) * p.cols;
@@ -91,10 +107,16 @@ struct Place {
             cols = ng * (int)p.each;
         }
         count = row < p.rows ? eight_of(cols, lane * 8) : 0;
+        // the first column's group, and where the next one begins
+        int g = p.parts_across > 1 ? 0 : p.by_each(lane * 8);
+        int next = p.parts_across > 1 ? 1 << 30
+                                      : (g + 1) * (int)p.each - lane * 8;
 #pragma unroll
         for (int e = 0; e < kK; ++e) {
-            const int g =
-                p.parts_across > 1 ? 0 : (lane * 8 + e) / (int)p.each;
+            if (e == next) {
+                ++g;
+                next += (int)p.each;
+            }
             group[e] = g < ng ? g : ng - 1;
         }
     }
@@ -136,18 +158,20 @@ __device__ __forceinline__ void slab_sync()
     }
 }
 
-// Adds up Q quantities of a slab's threads by groups: stat[q kStat + g].  v is
+// Adds up Q quantities of a slab's threads by groups: stat[q kStat + g] gets
+// done(q, the sum).  v is
 // a thread's one number (EVEN) or its 8 columns' sums.  buf: T or 8 T floats
 // for each quantity; its earlier contents have been read by all threads
 // before the last slab_sync.
-template <int T, int Q, bool EVEN>
+template <int T, int Q, bool EVEN, class F>
 __device__ __forceinline__ void group_sums(
     const Plan& p, const Place<EVEN>& at, int t,
-    const float (&v)[Q][Place<EVEN>::kK], float* buf, float* stat)
+    const float (&v)[Q][Place<EVEN>::kK], float* buf, float* stat, F&& done)
 {
     int team = T < 64 ? T : 64;
     while (team > 1 && team * at.ng > T) team >>= 1;
-    const int l = t % team, first = t / team, step = T / team;
+    const int shift = __builtin_ctz(team);
+    const int l = t & (team - 1), first = t >> shift, step = T >> shift;
     const int each = at.each(p);
     const int wide = EVEN ? p.lanes : p.lanes * 8;
     constexpr int kOne = EVEN ? T : 8 * T;
@@ -170,9 +194,10 @@ __device__ __forceinline__ void group_sums(
         }
         slab_sync<T>();
         // columns first: as many rows are left as the threads have turns
-        rows = T / wide < 1 ? 1 : T / wide < p.rows ? T / wide : p.rows;
+        const int turns = p.by_wide(T);
+        rows = turns < 1 ? 1 : turns < p.rows ? turns : p.rows;
         for (int i = t; i < rows * wide; i += T) {
-            const int r0 = i / wide;
+            const int r0 = p.by_wide(i);
 #pragma unroll
             for (int q = 0; q < Q; ++q) {
                 float* s = buf + q * kOne + (i - r0 * wide);
@@ -188,8 +213,11 @@ __device__ __forceinline__ void group_sums(
     const int items = rows * width;
     for (int g = first; g < at.ng; g += step) {
         float sum[Q] = {};
+        // (EVEN: i / (each / 8) = 8 i / each)
         for (int i = l; i < items; i += team) {
-            const int r = (int)((unsigned)i / (unsigned)width);
+            const int r = p.parts_across > 1
+                              ? (int)((unsigned)i / (unsigned)width)
+                              : p.by_each(EVEN ? 8 * i : i);
             const int c = r * wide + g * width + (i - r * width);
 #pragma unroll
             for (int q = 0; q < Q; ++q) sum[q] += buf[q * kOne + c];
@@ -199,7 +227,8 @@ __device__ __forceinline__ void group_sums(
             for (int q = 0; q < Q; ++q) sum[q] += __shfl_xor(sum[q], off);
         if (l == 0) {
 #pragma unroll
-            for (int q = 0; q < Q; ++q) stat[q * kStat<T> + g] = sum[q];
+            for (int q = 0; q < Q; ++q)
+                stat[q * kStat<T> + g] = done(q, sum[q]);
         }
     }
     slab_sync<T>();
@@ -396,6 +425,11 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
     } else {
         const int64_t line = dtype == SVM_F32 ? 32 : 64;
         p.groups = up(line, p.each);
+        // rows of whole eights: slices of whole eights too, so that they begin
+        // where 16 bytes do
+        int64_t k = 1;
+        while (channels % 8 == 0 && k * p.each % 8) k *= 2;
+        if (k * p.each <= 512) p.groups = up(p.groups, k) * k;
         while (p.groups < groups && positions * p.groups * p.each < 1024 &&
                p.groups * 2 * p.each <= 512)
             p.groups *= 2;
@@ -447,6 +481,9 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
     }
     p.threads = kThreads[i];
     p.rows = p.threads / p.lanes;
+    p.by_lanes = Divisor((uint32_t)p.lanes);
+    p.by_each = Divisor((uint32_t)p.each);
+    p.by_wide = Divisor((uint32_t)p.lanes * 8);
     p.pieces = pieces_of(p.threads, up(p.chunk, p.rows));
     if (p.pieces > most) p.pieces = most;
     return p;
