@@ -64,8 +64,14 @@ __device__ __forceinline__ void load_stats(const GroupArgs& a,
 
 // PARTS: only the sums, by chunks and for weight and bias.  A block keeps to
 // one slice and adds up in registers what its columns get over its units.
+// (Waves to a SIMD at the least: some are a register or two past the next.)
+template <int IT, bool EVEN>
+constexpr int kWavesAtLeast = IT > 2 ? 2 : IT > 1 ? (EVEN ? 3 : 2)
+                                                  : (EVEN ? 4 : 3);
+
 template <int DT, int T, int IT, bool EVEN, bool PARTS>
-__global__ __launch_bounds__(kSlabThreads<T>) void k_group_grad(GroupArgs a)
+__global__ __launch_bounds__(kSlabThreads<T>, (kWavesAtLeast<IT, EVEN>))
+void k_group_grad(GroupArgs a)
 {
     constexpr int kK = Place<EVEN>::kK;
     __shared__ float bufs[kSlabs<T>][2 * 8 * T];

@@ -193,6 +193,8 @@ __device__ __forceinline__ void group_sums(
                     buf[q * kOne + at.row * wide + at.lane * 8 + e] = v[q][e];
         }
         slab_sync<T>();
+    }
+    if (!EVEN && p.rows > 1) {
         // columns first: as many rows are left as the threads have turns
         const int turns = p.by_wide(T);
         rows = turns < 1 ? 1 : turns < p.rows ? turns : p.rows;
@@ -211,9 +213,11 @@ __device__ __forceinline__ void group_sums(
         slab_sync<T>();
     }
     const int items = rows * width;
+    constexpr int kAtOnce = T <= 16 ? 4 : 1;  // (large teams have few each)
     for (int g = first; g < at.ng; g += step) {
         float sum[Q] = {};
         // (EVEN: i / (each / 8) = 8 i / each)
+#pragma unroll kAtOnce
         for (int i = l; i < items; i += team) {
             const int r = p.parts_across > 1
                               ? (int)((unsigned)i / (unsigned)width)
@@ -403,7 +407,7 @@ int most_pieces(int32_t dtype, bool grad)
 // The pieces that the kernels are made for, from `need` on.
 int pieces_of(int threads, int64_t need)
 {
-    if (need <= 1) return 1;
+    if (need <= 1) return 1;  // (8 threads: never more)
     if (threads == 16) return 2;
     if (need <= 2 && threads == 256) return 2;
     return need <= 4 ? 4 : need <= 8 ? 8 : 16;
@@ -440,8 +444,8 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
     p.lanes = (int)up(p.cols, 8);
     const int most = most_pieces(dtype, grad);
     const int64_t units = samples * p.slices;
-    constexpr int kThreads[4] = {16, 64, 256, 512};
-    constexpr int kPieces[4] = {2, 4, 8, 16};
+    constexpr int kThreads[5] = {8, 16, 64, 256, 512};
+    constexpr int kPieces[5] = {1, 2, 4, 8, 16};
     auto fits = [&](int i, int64_t pieces) {
         const int t = kThreads[i];
         if (pieces > kPieces[i]) pieces = kPieces[i];
@@ -451,7 +455,7 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
     };
     int i = 0;
     // few slabs: more threads to each, so that they are done sooner
-    while (i < 3 && !fits(i, units * kThreads[i] < 131072 ? 1 : 16)) ++i;
+    while (i < 4 && !fits(i, units * kThreads[i] < 131072 ? 1 : 16)) ++i;
     bool whole = p.parts_across == 1 && fits(i, 16);
     // a slab for each sample leaves most of the card idle
     if (units * kThreads[i] < 65536 &&
@@ -469,7 +473,7 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
             p.cols = p.groups * p.each;
             p.lanes = (int)up(p.cols, 8);
         }
-        i = p.lanes > 256 ? 3 : 2;
+        i = p.lanes > 256 ? 4 : 3;
         const int64_t rows = kThreads[i] / p.lanes;
         const int64_t deep = most < 8 ? most : 8;
         // chunks enough for two blocks to a CU, but no longer than fits
@@ -499,7 +503,9 @@ void for_plan(const Plan& p, F&& f)
         if (p.even) f.template operator()<T, IT, true>();
         else f.template operator()<T, IT, false>();
     };
-    if (p.threads == 16) {
+    if (p.threads == 8) {
+        go.template operator()<8, 1>();
+    } else if (p.threads == 16) {
         if (p.pieces == 1) go.template operator()<16, 1>();
         else go.template operator()<16, 2>();
     } else if (p.threads == 64) {
