@@ -38,10 +38,10 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
         float v[1][kK] = {};
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
-            const bool there = at.row + i * p.rows < u.rows;
+            // (a piece past the end is another's again, and adds nothing)
+            if (at.row + i * p.rows >= u.rows) continue;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                v[0][EVEN ? 0 : e] += there ? x[i].at(e) : 0.0f;
+            for (int e = 0; e < 8; ++e) v[0][EVEN ? 0 : e] += x[i].at(e);
             settle(v[0]);
         }
         const float size = (float)((int64_t)u.rows * at.each(p));
@@ -55,12 +55,11 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
         }
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
+            if (at.row + i * p.rows >= u.rows) continue;
             forget(x[i]);
-            const bool there = at.row + i * p.rows < u.rows;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d =
-                    there ? x[i].at(e) - mu[EVEN ? 0 : e] : 0.0f;
+                const float d = x[i].at(e) - mu[EVEN ? 0 : e];
                 v[0][EVEN ? 0 : e] = fmaf(d, d, v[0][EVEN ? 0 : e]);
             }
             settle(v[0]);

@@ -443,6 +443,18 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
     }
     p.lanes = (int)up(p.cols, 8);
     const int most = most_pieces(dtype, grad);
+    // large samples: half a line, where that spares reading them again (64 x
+    // 1024 x 256 in groups of 8, bf16: gradients 51.7 us, in chunks 60.7)
+    const int64_t room = (int64_t)512 * most * 8;
+    const int64_t half = p.groups / 2;
+    if (p.parts_across == 1 && p.groups % 2 == 0 && half * p.each % 8 == 0 &&
+        half * p.each * (dtype == SVM_F32 ? 4 : 2) >= 64 &&
+        positions * p.cols > room && positions * half * p.each <= room) {
+        p.groups = half;
+        p.cols = p.groups * p.each;
+        p.slices = up(groups, p.groups);
+        p.lanes = (int)up(p.cols, 8);
+    }
     const int64_t units = samples * p.slices;
     constexpr int kThreads[5] = {8, 16, 64, 256, 512};
     constexpr int kPieces[5] = {1, 2, 4, 8, 16};
