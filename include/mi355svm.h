@@ -538,8 +538,8 @@ svm_status svm_adamw_state(const int8_t *m, const uint8_t *v,
  *   y = act((x - mean) rstd weight + bias),
  *   rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
  * rows a multiple of positions (>= 1), cols of groups.  weight and bias
- * (1 x cols) are nullable (1 and 0).  mean and rstd (samples x groups floats,
- * nullable) receive the statistics that the gradient needs.  Y may be X
+ * (1 x cols) are nullable (1 and 0).  mean and rstd (samples x groups floats
+ * each, nullable) receive the statistics that the gradient needs.  Y may be X
  * itself (same data and ld). */
 svm_status svm_group_norm(const svm_array *X, int64_t positions,
                           int64_t groups, const svm_array *weight,
@@ -615,8 +615,8 @@ typedef struct {
 } svm_packed;
 
 /* Rounds the weights W to 4 bits.  A group's scale is a sixth of its largest
- * magnitude, cut to six significant bits (SVM_F16: and to whole steps of
- * 2^-23), so that what a weight stands for is a value of its type; each weight
+ * magnitude (times 1/6 in 32 bits), cut to six significant bits (SVM_F16: and
+ * to whole steps of 2^-23), so that what a weight stands for is a value of its type; each weight
  * takes the nearest of the magnitudes, in the middle between two the one with
  * the even place (0, 1, 2, 4).  A weight that is not finite makes all of its
  * group NaN.  to: rows, cols and dtype of W. */
@@ -630,11 +630,11 @@ svm_status svm_unpack_weights(const svm_packed *packed, const svm_array *W,
                               int32_t device, void *stream);
 
 /* One layer on packed weights: Y = act(X W^T + bias) + residual, arrays as in
- * svm_linear.  No weight is rounded further: sums of X times codes over 32
- * inputs are held in 32 bits and multiplied by the group's scale there (so
- * |X| up to 1e36 stays in range).  Made for few rows, whose time is that of
- * reading the weights; many go through svm_linear's products on the unpacked
- * weights, in the workspace.  residual may be Y itself. */
+ * svm_linear.  No weight is rounded further: sums of X times codes over a
+ * group's inputs are held in 32 bits and multiplied by the group's scale there
+ * (so that |X| up to 4e35 stays in range).  Made for few rows, whose time is
+ * that of reading the weights; many go through svm_linear's products on the
+ * unpacked weights, in the workspace.  residual may be Y itself. */
 svm_status svm_linear_packed(const svm_array *X, const svm_packed *W,
                              const svm_array *bias, const svm_array *residual,
                              int32_t act, const svm_array *Y, void *work,

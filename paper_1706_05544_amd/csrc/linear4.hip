@@ -29,14 +29,15 @@ typedef float floatx2 __attribute__((ext_vector_type(2)));
 
 constexpr float kMost = 3.402823466e38f;
 
-// The scale of a group whose largest magnitude is `top`: a sixth of it with
-// six significant bits kept, so that a scale times a code (two significant
-// bits) is a value of any of the types.  In f16 it is a whole number of steps
-// of 2^-23 besides: half of it is a value too.
+// The scale of a group whose largest magnitude is `top`: a sixth of it (the
+// product with the 32-bit number nearest to 1/6) with six significant bits
+// kept, so that a scale times a code (two significant bits) is a value of any
+// of the types.  In f16 it is a whole number of steps of 2^-23 besides: half
+// of it is a value too.
 template <int DT>
 __device__ __forceinline__ float scale_of(float top)
 {
-    const uint32_t b = __builtin_bit_cast(uint32_t, top / 6.0f);
+    const uint32_t b = __builtin_bit_cast(uint32_t, top * (1.0f / 6.0f));
     const float s = __builtin_bit_cast(float, b & ~((1u << 18) - 1));
     if constexpr (DT == SVM_F16)
         return floorf(s * 8388608.0f) * (1.0f / 8388608.0f);

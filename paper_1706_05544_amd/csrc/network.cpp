@@ -299,6 +299,8 @@ svm_status svm_group_norm(const svm_array* X, int64_t positions,
     if (!same(Y, X)) CHECK(check_apart(Y, "Y", {X}));
     CHECK(check_float(mean, "mean"));
     CHECK(check_float(rstd, "rstd"));
+    if (mean && mean == rstd)
+        return fail(SVM_E_INVALID, "mean and rstd are the same");
     GroupCall a{*X,  or_none(weight), or_none(bias), *Y,
                 positions, groups, (float)eps, act, mean, rstd};
     Pieces count;

@@ -1083,15 +1083,15 @@ def svm_group_norm(X, groups: int, weight=None, bias=None, eps: float = 1e-5,
     a, per = c.arr(X, "X"), _positions(X)
     Y = out if out is not None else X.new_empty(X.shape)
     mean = rstd = None
+    size = ct.c_int64()
+    _check(lib.svm_group_norm_workspace(a.rows, per, a.cols, groups, a.dtype,
+                                        ct.byref(size)))
+    ws = c.work(size.value)
     if save:
         mean = c.empty((X.shape[0], groups), torch.float32)
         rstd = c.empty((X.shape[0], groups), torch.float32)
         if not a.rows:  # samples without positions, if any
             mean.zero_(), rstd.zero_()
-    size = ct.c_int64()
-    _check(lib.svm_group_norm_workspace(a.rows, per, a.cols, groups, a.dtype,
-                                        ct.byref(size)))
-    ws = c.work(size.value)
     w, b = c.arr(weight, "weight"), c.arr(bias, "bias")
     c.ready()
     _check(lib.svm_group_norm(ct.byref(a), per, groups, _ref(w), _ref(b), eps,
@@ -1115,6 +1115,10 @@ def svm_group_norm_backward(dY, X, groups: int, mean, rstd, weight=None,
     g, a, per = c.arr(dY, "dY"), c.arr(X, "X"), _positions(dY)
     if X.shape != dY.shape:
         raise SvmError(SVM_E_INVALID, "X and dY differ in shape")
+    for t in (mean, rstd):
+        if _is_torch(t) and t.numel() != dY.shape[0] * groups:
+            raise SvmError(SVM_E_INVALID, "mean and rstd must have a value for "
+                           "each sample and group")
     mp = c.floats(mean, dY.shape[0] * groups, "mean")
     rp = c.floats(rstd, dY.shape[0] * groups, "rstd")
     dX = dY.new_empty(X.shape) if need[0] else None

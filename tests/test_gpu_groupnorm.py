@@ -436,6 +436,7 @@ def test_refusals():
     for call, code in (
             (lambda: nv.svm_group_norm(X, 5), nv.SVM_E_INVALID),
             (lambda: nv.svm_group_norm(X, 0), nv.SVM_E_INVALID),
+            (lambda: nv.svm_group_norm(X, -2, save=True), nv.SVM_E_INVALID),
             (lambda: nv.svm_group_norm(X[0, 0], 2), nv.SVM_E_INVALID),
             (lambda: nv.svm_group_norm(X, 6, X[0, 0, :23]), nv.SVM_E_INVALID),
             (lambda: nv.svm_group_norm(X, 6, X[0, 0].half()),

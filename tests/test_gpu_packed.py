@@ -41,7 +41,8 @@ def held(W, group):
     pad = pad.view(n, -1, group)
     top = pad.abs().amax(2)
     bad = ~torch.isfinite(pad).all(2)
-    s = (torch.where(bad, 0, top) / 6.0).view(torch.int32) >> 18 << 18
+    sixth = torch.tensor(1.0) / torch.tensor(6.0)  # in 32 bits
+    s = (torch.where(bad, 0, top) * sixth).view(torch.int32) >> 18 << 18
     s = s.view(torch.float32)
     if t == torch.float16:
         s = (s.double() * 2.0 ** 23).floor().float() * 2.0 ** -23
@@ -97,6 +98,9 @@ def test_pack_borders_and_ends_of_the_range(t):
     W[10, 5], W[10, 40] = math.nan, 2.0
     W[11, 5], W[11, 40] = math.inf, 2.0
     W[12, 5], W[12, 40] = -math.inf, 2.0
+    # a sixth of it falls just short of six bits, and its product with the
+    # 32-bit number nearest to 1/6 on them
+    W[13, 0], W[13, 1] = 0.11132811754941940, 0.05
     W = W.to(TYPES[t]).to(DEV)
     for group in (32, 64):
         P = nv.svm_pack_weights(W, group)
@@ -104,6 +108,8 @@ def test_pack_borders_and_ends_of_the_range(t):
         want = held(W, group)[0]
         assert same_values(got, want)
         assert got[10:13, :32].isnan().all()
+        if t == "f32":
+            assert float(got[13, 0]) == 6 * 0.0185546875
         if group == 32:  # the next group is untouched
             assert got[10:13, 40].eq(2.0).logical_or(
                 (got[10:13, 40] - 2.0).abs() < 0.07).all()

@@ -215,7 +215,8 @@ GROUPS = [dict(positions=0), dict(positions=-3), dict(positions=4),
     dict(act=6), dict(act=-1), dict(Y=arr(5, 4, at=2 << 20)),
     dict(Y=arr(6, 4, at=(1 << 20) + 4)), dict(Y=arr(6, 4, ld=5)),
     dict(w=arr(1, 4, at=2 << 20)), dict(b=arr(1, 4, at=2 << 20)),
-    dict(mean=18), dict(rstd=17), dict(device=-1), dict(work=24),
+    dict(mean=18), dict(rstd=17), dict(mean=32, rstd=32), dict(device=-1),
+    dict(work=24),
     # chunks of few large samples need a workspace
     dict(X=arr(1 << 20, 4, at=1 << 30), positions=1 << 20,
          Y=arr(1 << 20, 4, at=2 << 30), work=None)])

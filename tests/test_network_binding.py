@@ -85,6 +85,7 @@ def test_refusals_of_the_binding(late):  # noqa: F811
     X, st = torch.ones(4, 6), torch.ones(4, 2)
     for call in (lambda: nv.svm_group_norm(X[0], 2),
                  lambda: nv.svm_group_norm_backward(X, X[:3], 2, st, st),
+                 lambda: nv.svm_group_norm_backward(X, X, 2, st, st[:3]),
                  lambda: nv.svm_linear_packed(X, X),
                  lambda: nv.svm_unpack_weights(X),
                  lambda: nv.svm_grad_norm([]),
