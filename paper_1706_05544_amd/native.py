@@ -9,6 +9,7 @@ built, loading fails loudly instead of falling back to anything else.
 from __future__ import annotations
 
 import ctypes as ct
+import functools
 import os
 import struct
 from typing import Optional
@@ -1070,6 +1071,16 @@ def _positions(X) -> int:
     return max(n, 1)
 
 
+@functools.lru_cache(maxsize=256)
+def _group_norm_bytes(backward: bool, *sizes) -> int:
+    """Workspace of a group norm: a matter of its sizes alone."""
+    lib, size = load(), ct.c_int64()
+    f = (lib.svm_group_norm_backward_workspace if backward
+         else lib.svm_group_norm_workspace)
+    _check(f(*sizes, ct.byref(size)))
+    return size.value
+
+
 def svm_group_norm(X, groups: int, weight=None, bias=None, eps: float = 1e-5,
                    act="none", save: bool = False, out=None, stream=None):
     """Group norm with an activation over X (samples, any positions,
@@ -1083,10 +1094,8 @@ def svm_group_norm(X, groups: int, weight=None, bias=None, eps: float = 1e-5,
     a, per = c.arr(X, "X"), _positions(X)
     Y = out if out is not None else X.new_empty(X.shape)
     mean = rstd = None
-    size = ct.c_int64()
-    _check(lib.svm_group_norm_workspace(a.rows, per, a.cols, groups, a.dtype,
-                                        ct.byref(size)))
-    ws = c.work(size.value)
+    size = _group_norm_bytes(False, a.rows, per, a.cols, groups, a.dtype)
+    ws = c.work(size)
     if save:
         mean = c.empty((X.shape[0], groups), torch.float32)
         rstd = c.empty((X.shape[0], groups), torch.float32)
@@ -1096,7 +1105,7 @@ def svm_group_norm(X, groups: int, weight=None, bias=None, eps: float = 1e-5,
     c.ready()
     _check(lib.svm_group_norm(ct.byref(a), per, groups, _ref(w), _ref(b), eps,
                               _act(act), ct.byref(c.arr(Y, "out", True)),
-                              _ptr(mean), _ptr(rstd), ws, size.value, c.index,
+                              _ptr(mean), _ptr(rstd), ws, size, c.index,
                               c.handle))
     c.done()
     if out is not None:
@@ -1124,10 +1133,8 @@ def svm_group_norm_backward(dY, X, groups: int, mean, rstd, weight=None,
     dX = dY.new_empty(X.shape) if need[0] else None
     dw = dY.new_empty(g.cols) if need[1] else None
     db = dY.new_empty(g.cols) if need[2] else None
-    size = ct.c_int64()
-    _check(lib.svm_group_norm_backward_workspace(
-        g.rows, per, g.cols, groups, g.dtype, ct.byref(size)))
-    ws = c.work(size.value)
+    size = _group_norm_bytes(True, g.rows, per, g.cols, groups, g.dtype)
+    ws = c.work(size)
     w, b, r = (c.arr(weight, "weight"), c.arr(bias, "bias"),
                c.arr(residual, "residual"))
     c.ready()
@@ -1135,7 +1142,7 @@ def svm_group_norm_backward(dY, X, groups: int, mean, rstd, weight=None,
         ct.byref(g), ct.byref(a), per, groups, mp, rp, _ref(w), _ref(b),
         _act(act), _ref(r), _ref(c.arr(dX, "dX", True)),
         _ref(c.arr(dw, "dweight", True)), _ref(c.arr(db, "dbias", True)), ws,
-        size.value, c.index, c.handle))
+        size, c.index, c.handle))
     c.done()
     return dX, dw, db
 

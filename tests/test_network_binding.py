@@ -8,6 +8,13 @@ from paper_1706_05544_amd import native as nv
 from test_layers_binding import late  # noqa: F401 (a fixture)
 
 
+@pytest.fixture(autouse=True)
+def sizes_forgotten():
+    # (workspace sizes that the stand-in library gave are not to stay)
+    yield
+    nv._group_norm_bytes.cache_clear()
+
+
 def rows(m, n):
     return torch.randn(n, m).t()
 
