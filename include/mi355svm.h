@@ -539,8 +539,8 @@ svm_status svm_adamw_state(const int8_t *m, const uint8_t *v,
  *   rstd = 1 / sqrt(mean of (x - mean)^2 + eps).
  * rows a multiple of positions (>= 1), cols of groups.  weight and bias
  * (1 x cols) are nullable (1 and 0).  mean and rstd (samples x groups floats
- * each, nullable) receive the statistics that the gradient needs.  Y may be X
- * itself (same data and ld). */
+ * each, nullable) receive the statistics that the gradient needs, and overlap
+ * nothing.  Y may be X itself (same data and ld). */
 svm_status svm_group_norm(const svm_array *X, int64_t positions,
                           int64_t groups, const svm_array *weight,
                           const svm_array *bias, double eps, int32_t act,

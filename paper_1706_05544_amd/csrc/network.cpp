@@ -299,8 +299,13 @@ svm_status svm_group_norm(const svm_array* X, int64_t positions,
     if (!same(Y, X)) CHECK(check_apart(Y, "Y", {X}));
     CHECK(check_float(mean, "mean"));
     CHECK(check_float(rstd, "rstd"));
-    if (mean && mean == rstd)
-        return fail(SVM_E_INVALID, "mean and rstd are the same");
+    const int64_t stats = m / positions * groups;
+    const svm_array M{mean, 1, stats, stats, SVM_F32, 1};
+    const svm_array R{rstd, 1, stats, stats, SVM_F32, 1};
+    if (stats) {
+        CHECK(check_apart(&M, "mean", {&R, X, Y, weight, bias}));
+        CHECK(check_apart(&R, "rstd", {X, Y, weight, bias}));
+    }
     GroupCall a{*X,  or_none(weight), or_none(bias), *Y,
                 positions, groups, (float)eps, act, mean, rstd};
     Pieces count;

@@ -216,6 +216,11 @@ GROUPS = [dict(positions=0), dict(positions=-3), dict(positions=4),
     dict(Y=arr(6, 4, at=(1 << 20) + 4)), dict(Y=arr(6, 4, ld=5)),
     dict(w=arr(1, 4, at=2 << 20)), dict(b=arr(1, 4, at=2 << 20)),
     dict(mean=18), dict(rstd=17), dict(mean=32, rstd=32), dict(device=-1),
+    # statistics (2 samples of 2 groups: 16 bytes each) in one another, in the
+    # values before them and in the outputs
+    dict(mean=32, rstd=44), dict(mean=44, rstd=32),
+    dict(mean=(1 << 20) + 92), dict(rstd=(2 << 20) - 12),
+    dict(rstd=4 << 20, w=arr(1, 4, at=4 << 20)),
     dict(work=24),
     # chunks of few large samples need a workspace
     dict(X=arr(1 << 20, 4, at=1 << 30), positions=1 << 20,
