@@ -489,6 +489,9 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
         const int64_t rows = kThreads[i] / p.lanes;
         const int64_t deep = most < 8 ? most : 8;
         // chunks enough for two blocks to a CU, but no longer than fits
+        // (gradients of 6 x 3977 x 231, f16: 512 units 39.9 us, 384 39.6, 256
+        // 41.3, 1024 46.3, 2048 54.2; of 1 x 3977 x 231 27.8, with 256 24.6;
+        // of 4 x 2000 x 512, bf16: 25.9, with 256 29.1)
         int64_t chunk = up(positions * samples * p.slices, 512);
         if (chunk < rows) chunk = rows;
         if (chunk > rows * deep) chunk = rows * deep;
