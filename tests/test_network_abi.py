@@ -105,14 +105,14 @@ BAD_PACKED = [packed(rows=0), packed(cols=0), packed(rows=(1 << 21) + 1),
               packed(cols=(1 << 21) + 1), packed(group=16), packed(group=96),
               packed(group=0), packed(dtype=3), packed(dtype=-1),
               packed(at=None), packed(at=(1 << 28) + 8),
-              # 3 tiles of 16 x 128: 3072 bytes of codes, 4 * 48 scales
+              # 3 tiles of 16 x 128: 1024 bytes of codes each, 4 * 48 scales
               packed(nbytes=3 * 1024 + 4 * 48 * 4 - 1), packed(nbytes=-1)]
 
 
 def test_pack4_bytes():
     lib, n = nv.load(), ct.c_int64(-1)
-    for args, want in (((40, 100, 32, 0), 3072 + 4 * 48 * 4),
-                       ((40, 100, 128, 1), 3072 + 48 * 2),
+    for args, want in (((40, 100, 32, 0), 3 * 1024 + 4 * 48 * 4),
+                       ((40, 100, 128, 1), 3 * 1024 + 48 * 2),
                        ((1, 1, 64, 2), 1024 + 2 * 16 * 2),
                        ((1 << 21, 1 << 21, 128, 0), (1 << 41) + (1 << 37))):
         assert lib.svm_pack_weights_bytes(*args, ct.byref(n)) == 0
@@ -139,7 +139,7 @@ def test_pack4_refusals(fn):
     for W in (arr(40, 99), arr(39, 100), arr(40, 100, dtype=1),
               arr(40, 100, ld=99), arr(40, 100, at=None),
               arr(40, 100, at=(1 << 20) + 2), arr(40, 100, at=1 << 28),
-              arr(40, 100, at=(1 << 28) + 3072)):
+              arr(40, 100, at=(1 << 28) + 3 * 1024)):
         assert pack(W=W, fn=fn) == INV
     assert pack(W=arr(40, 100, dev=0), fn=fn) == UNS
     assert pack(device=-1, fn=fn) == INV
