@@ -105,9 +105,14 @@ void k_group_grad(GroupArgs a)
         load_slab<DT, IT>(g, a.dY, (u.row + at.row) * a.ldg + at.first(),
                           p.rows * a.ldg, last * a.ldg + at.first(), any,
                           at.count, a.endg);
-        // (a slab without a unit takes the last sample's; it adds nothing)
+        // (a slab without a unit: statistics of 0, so that its xh are 0 and add
+        // nothing; with any sample's they may be infinite, and 0 times them NaN)
         float mu[kK], rs[kK];
         load_stats<EVEN>(a, at, u.n < a.samples ? u.n : a.samples - 1, mu, rs);
+        if (kSlabs<T> > 1 && u.rows == 0) {
+#pragma unroll
+            for (int k = 0; k < kK; ++k) mu[k] = rs[k] = 0.0f;
+        }
         float w[8], b[8];
         w8.values(w);
         b8.values(b);
