@@ -556,7 +556,8 @@ svm_status svm_group_norm_workspace(int64_t rows, int64_t positions,
  *   dX = rstd (a - mean(a) - xh mean(a xh)) + residual,
  *   dweight = sum over rows of dZ xh,  dbias = sum over rows of dZ.
  * residual (rows x cols, nullable): the gradient that reaches X past the
- * norm.  dX, dweight and dbias are nullable; dX may be dY or the residual
+ * norm.  dX, dweight and dbias are nullable and overlap neither each other
+ * nor any input, mean and rstd among them, but dX may be dY or the residual
  * itself.  With no rows dweight and dbias are set to 0. */
 svm_status svm_group_norm_backward(
     const svm_array *dY, const svm_array *X, int64_t positions,

@@ -382,6 +382,16 @@ svm_status svm_group_norm_backward(
         CHECK(check_array(dbias, "dbias", 1, n, t));
         CHECK(check_apart(dbias, "dbias", {dY, X, weight, bias, residual}));
     }
+    const int64_t stats = m / positions * groups;
+    if (stats) {  // other blocks read them while the outputs are written
+        const svm_array M{const_cast<float*>(mean), 1, stats, stats, SVM_F32,
+                          1};
+        const svm_array R{const_cast<float*>(rstd), 1, stats, stats, SVM_F32,
+                          1};
+        CHECK(check_apart(dX, "dX", {&M, &R}));
+        CHECK(check_apart(dweight, "dweight", {&M, &R}));
+        CHECK(check_apart(dbias, "dbias", {&M, &R}));
+    }
     GroupGradCall a{*dY,          *X,
                     or_none(weight),   or_none(bias),
                     or_none(residual), or_none(dX),
