@@ -419,6 +419,7 @@ Plan plan_of(int64_t samples, int64_t positions, int64_t channels,
              int64_t groups, int32_t dtype, bool grad)
 {
     Plan p{};
+    if (samples == 0) positions = 1;  // (there may be any number of them)
     p.each = channels / groups;
     p.parts_across = p.each > kWideCols ? up(p.each, kWideCols) : 1;
     p.even = p.each % 8 == 0;
