@@ -594,12 +594,25 @@ svm_status svm_grad_norm_workspace(const svm_grad *grads, int32_t n_grads,
 /* svm_adamw_step on clipped gradients: g = (grad_scale *factor) grad, with
  * the factor (one float, from svm_grad_norm) read on the device as the step
  * runs.  Where it is not finite nothing is written: the step is left out.
- * factor NULL: svm_adamw_step. */
+ * params->step counts it all the same (svm_adamw_step_counted does not).
+ * factor NULL: svm_adamw_step.  It lies in nothing that the step writes. */
 svm_status svm_adamw_step_clipped(const svm_adamw_tensor *tensors,
                                   int32_t n_tensors,
                                   const svm_adamw_params *params,
                                   const float *factor, int32_t device,
                                   void *stream);
+
+/* svm_adamw_step_clipped that counts the steps left out, in *left_out on the
+ * device (0 to begin with): the bias corrections are those of step
+ * params->step - *left_out, so that the steps after one that was left out are
+ * as if it had never been asked for.  Where this step is left out, *left_out
+ * goes up by one (given a value to step).  factor and left_out overlap neither
+ * each other nor what the step writes; left_out NULL: svm_adamw_step_clipped. */
+svm_status svm_adamw_step_counted(const svm_adamw_tensor *tensors,
+                                  int32_t n_tensors,
+                                  const svm_adamw_params *params,
+                                  const float *factor, int64_t *left_out,
+                                  int32_t device, void *stream);
 
 /* The weights of a linear layer in 4 bits, rows x cols, with a scale to each
  * `group` (32, 64 or 128) consecutive inputs of an output.  A weight stands

@@ -22,7 +22,8 @@ DEVICE_SOURCES = ["kernels.hip", "rows.hip", "lockstep.hip", "select.hip",
                   "resident.hip", "linear.hip", "matmul.hip", "norm.hip", "hinge.hip",
                   "adamw.hip", "gradnorm.hip", "linear4.hip",
                   "groupnorm.hip", "groupgrad.hip"]
-HOST_SOURCES = ["solver.cpp", "api.cpp", "layers.cpp", "network.cpp"]
+HOST_SOURCES = ["solver.cpp", "api.cpp", "layers.cpp", "network.cpp",
+                "steps.cpp"]
 
 # Packed fp32 instructions are disabled for every compilation that has a
 # device pass (hipcc runs one for the .cpp sources too).

@@ -33,7 +33,32 @@ struct AdamConst {
     float root;            // 1 / sqrt(1 - b2^t)
     float eps, gscale;
     const float* factor;   // nullable: multiplies gscale
+    // nullable: how many of the steps before this one were left out.  Where
+    // there are any, rate and root are made again from these.
+    int64_t* left_out;
+    bool count;            // this launch counts the step if it is left out
+    int64_t step;
+    double lr, beta1, beta2;
 };
+
+// b^t by squares: exact for t = 1, and good to t 2^-53 of itself.
+__device__ __forceinline__ double power(double b, int64_t t)
+{
+    double r = 1.0;
+    for (; t > 0; t >>= 1, b *= b)
+        if (t & 1) r *= b;
+    return r;
+}
+
+// The corrections of the step that this is when those left out are not
+// counted (1 at the least, however the count was set).
+__device__ __forceinline__ void correct(AdamConst& k, int64_t left_out)
+{
+    const int64_t t =
+        left_out < 0 ? k.step : left_out < k.step ? k.step - left_out : 1;
+    k.rate = (float)(k.lr / (1.0 - power(k.beta1, t)));
+    k.root = (float)(1.0 / sqrt(1.0 - power(k.beta2, t)));
+}
 
 constexpr float kTiny = 1e-30f;
 
@@ -177,8 +202,16 @@ __global__ __launch_bounds__(256) void k_adamw(AdamTable t, AdamConst k)
     }
     if (k.factor) {
         const float f = *k.factor;
-        if (!(fabsf(f) <= kMost)) return;  // the step is left out
+        if (!(fabsf(f) <= kMost)) {  // the step is left out
+            // (and no wave reads the count)
+            if (k.left_out && k.count && blk == 0 && lane == 0) ++*k.left_out;
+            return;
+        }
         k.gscale *= f;
+    }
+    if (k.left_out) {
+        const int64_t c = *k.left_out;
+        if (c) correct(k, c);
     }
     using P = Elem<PT>;
     using G = Elem<GT>;
@@ -331,8 +364,21 @@ void adamw_step_clipped(const svm_adamw_tensor* t, int32_t n,
                         const svm_adamw_params& p, const float* factor,
                         hipStream_t s)
 {
+    adamw_step_counted(t, n, p, factor, nullptr, s);
+}
+
+void adamw_step_counted(const svm_adamw_tensor* t, int32_t n,
+                        const svm_adamw_params& p, const float* factor,
+                        int64_t* left_out, hipStream_t s)
+{
     AdamConst k;
     k.factor = factor;
+    k.left_out = left_out;
+    k.count = true;
+    k.step = p.step;
+    k.lr = p.lr;
+    k.beta1 = p.beta1;
+    k.beta2 = p.beta2;
     k.b1 = (float)p.beta1;
     k.c1 = (float)(1.0 - p.beta1);
     k.b2 = (float)p.beta2;
@@ -369,6 +415,7 @@ void adamw_step_clipped(const svm_adamw_tensor* t, int32_t n,
                         launch_group<SVM_F16, SVM_F32>(tab, k, p.bits, master,
                                                        s);
                     tab.count = 0;
+                    k.count = false;
                 };
                 // values of a tensor in one launch (block numbers are int32)
                 constexpr int64_t kMost = (int64_t)kAdamBlock << 24;

@@ -71,6 +71,11 @@ void adamw_step(const svm_adamw_tensor* t, int32_t n,
 void adamw_step_clipped(const svm_adamw_tensor* t, int32_t n,
                         const svm_adamw_params& p, const float* factor,
                         hipStream_t s);
+// ... and that counts the steps left out, on the device (nullable): the
+// corrections are those of the steps that were not.
+void adamw_step_counted(const svm_adamw_tensor* t, int32_t n,
+                        const svm_adamw_params& p, const float* factor,
+                        int64_t* left_out, hipStream_t s);
 void adamw_state(const int8_t* m, const uint8_t* v, const float* ms,
                  const float* vs, int64_t n, float* mo, float* vo,
                  hipStream_t s);

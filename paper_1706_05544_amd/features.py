@@ -97,7 +97,9 @@ class FeatureNet(_Network):
                            + self.head)
         self.states = nv.svm_adamw_states(
             self.parameters, bits=bits, master=dtype != torch.float32)
-        self.steps = 0
+        self.steps = 0       # asked for
+        # of them, those whose gradients were not finite (on the device)
+        self.left_out = torch.zeros((), dtype=torch.int64, device=device)
         self.norm = None  # of the last clipped step's gradients
 
     @staticmethod
@@ -150,7 +152,8 @@ class FeatureNet(_Network):
         """One step on a batch -> its loss (a tensor on the device).  With
         ``clip`` the gradients' norm is brought down to it, and kept in
         ``norm`` (on the device); a step whose gradients are not finite
-        changes nothing."""
+        changes nothing but ``left_out``, and the steps after it are as if it
+        had never been."""
         loss, _, grads = self.gradients(X, labels)
         self.steps += 1
         factor = None
@@ -158,7 +161,7 @@ class FeatureNet(_Network):
             self.norm, factor = nv.svm_grad_norm(grads, clip)
         nv.svm_adamw_step(self.parameters, grads, *self.states, lr=lr,
                           weight_decay=weight_decay, step=self.steps,
-                          factor=factor)
+                          factor=factor, left_out=self.left_out)
         return loss
 
 

@@ -56,7 +56,7 @@ EXPORTS = [
     "svm_adamw_step_clipped", "svm_pack_weights", "svm_pack_weights_bytes",
     "svm_unpack_weights", "svm_linear_packed", "svm_linear_packed_workspace",
     "svm_group_norm", "svm_group_norm_workspace", "svm_group_norm_backward",
-    "svm_group_norm_backward_workspace",
+    "svm_group_norm_backward_workspace", "svm_adamw_step_counted",
 ]
 
 
@@ -242,6 +242,8 @@ def load(path: Optional[str] = None):
     lib.svm_grad_norm_workspace.argtypes = [vp, i32, P(i64)]
     lib.svm_adamw_step_clipped.argtypes = [vp, i32, P(svm_adamw_params), vp,
                                            i32, vp]
+    lib.svm_adamw_step_counted.argtypes = [vp, i32, P(svm_adamw_params), vp,
+                                           vp, i32, vp]
     p4 = P(svm_packed)
     lib.svm_pack_weights.argtypes = [pa, p4, i32, vp]
     lib.svm_pack_weights_bytes.argtypes = [i64, i64, i32, i32, P(i64)]
@@ -911,14 +913,17 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
                    master=None, lr: float = 1e-3, beta1: float = 0.9,
                    beta2: float = 0.999, eps: float = 1e-8,
                    weight_decay: float = 0.01, step: int = 1,
-                   grad_scale: float = 1.0, factor=None, stream=None):
+                   grad_scale: float = 1.0, factor=None, stream=None,
+                   left_out=None):
     """One AdamW step over the tensors `params` (contiguous, updated in
     place, no two of them overlapping) with the gradients `grads`.  The states
     are flat tensors as svm_adamw_states makes them: m and v in float32, or
     int8 and uint8 with float32 scales, and optionally the master weights.
     `factor`: the clipping factor of svm_grad_norm, a float32 scalar on the
     device that multiplies the gradients; where it is not finite the step is
-    left out and nothing changes."""
+    left out and nothing changes but `left_out`, where there is one: an int64
+    scalar on the device that counts such steps (0 to begin with).  The bias
+    corrections are those of step - left_out."""
     import torch
     if len(params) != len(grads):
         raise SvmError(SVM_E_INVALID, "params and grads differ in number")
@@ -979,8 +984,19 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
     h = svm_adamw_params(lr, beta1, beta2, eps, weight_decay, grad_scale,
                          step, bits)
     fp = None if factor is None else c.floats(factor, 1, "factor")
+    if left_out is not None:
+        if not _is_torch(left_out) or left_out.dtype != torch.int64 or \
+                left_out.numel() != 1 or left_out.device != c.device:
+            raise SvmError(SVM_E_INVALID, "left_out must be an int64 scalar "
+                           "on the parameters' device")
+        c.keep.append(left_out)
+        written.append(left_out)
     c.ready()
-    if fp is None:
+    if left_out is not None:
+        _check(lib.svm_adamw_step_counted(
+            _np_ptr(tab), len(params), ct.byref(h), fp, left_out.data_ptr(),
+            c.index, c.handle))
+    elif fp is None:
         _check(lib.svm_adamw_step(_np_ptr(tab), len(params), ct.byref(h),
                                   c.index, c.handle))
     else:
