@@ -913,7 +913,7 @@ def svm_adamw_step(params, grads, m, v, m_scale=None, v_scale=None,
                    master=None, lr: float = 1e-3, beta1: float = 0.9,
                    beta2: float = 0.999, eps: float = 1e-8,
                    weight_decay: float = 0.01, step: int = 1,
-                   grad_scale: float = 1.0, factor=None, stream=None,
+                   grad_scale: float = 1.0, stream=None, factor=None,
                    left_out=None):
     """One AdamW step over the tensors `params` (contiguous, updated in
     place, no two of them overlapping) with the gradients `grads`.  The states

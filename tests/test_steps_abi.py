@@ -1,6 +1,7 @@
 """The AdamW step that counts the steps left out: argument checks, binding and
 host side, without a GPU (no pointer is followed)."""
 import ctypes as ct
+import inspect
 import os
 
 import pytest
@@ -74,3 +75,13 @@ def test_binding(late):  # noqa: F811
         with pytest.raises(nv.SvmError) as e:
             nv.svm_adamw_step(p, g, *st, left_out=bad)
         assert e.value.status == INV
+
+
+def test_arguments_by_place(late):  # noqa: F811
+    # the stream is the fifteenth, as before there was a factor
+    p = [torch.ones(3)]
+    st = nv.svm_adamw_states(p)
+    nv.svm_adamw_step(p, [torch.ones(3)], *st, 1e-3, 0.9, 0.999, 1e-8, 0.01, 1,
+                      1.0, None, torch.ones(()))
+    assert list(inspect.signature(nv.svm_adamw_step).parameters)[12:] == [
+        "step", "grad_scale", "stream", "factor", "left_out"]
