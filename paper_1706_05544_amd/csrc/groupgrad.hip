@@ -146,9 +146,12 @@ void k_group_grad(GroupArgs a)
             settle(v[1]);
         }
         if (!PARTS && !a.out) continue;
-        group_sums<T, 2, EVEN>(
-            p, at, t, v, buf, stat,
-            [&](int, float s) { return PARTS ? s : s * over; });
+        group_sums<T, 2, EVEN>(p, at, t, v, buf,
+                               [&](int q, const float (&s)[2]) {
+                                   stat[q] = PARTS ? s[0] : s[0] * over;
+                                   stat[kStat<T> + q] =
+                                       PARTS ? s[1] : s[1] * over;
+                               });
         if (PARTS) {
             if (u.rows > 0)
                 for (int q = t; q < at.ng; q += T) {

@@ -1,16 +1,40 @@
 // Group norm with an activation: the forward pass (groupnorm.hpp says how it
 // is cut up).  Bound by memory and, nearly as much, by the vector instructions
 // (28 a value): 512 x 196 x 512 in bf16 with silu 47 us, 4.4 TB/s (a
-// large copy: 5.0); 100000 x 64 in 32 bits, eight threads a sample, 15.1 us,
-// 3.4 TB/s.  Groups of a width that is no multiple of 8 take more of them:
+// large copy: 5.0); 100000 x 64 in 32 bits, eight threads a sample, 15.4 us,
+// 3.3 TB/s.  Groups of a width that is no multiple of 8 take more of them:
 // 4000 x 30 x 120 in f16, groups of 15, 31 us, 1.9 TB/s.  Mean and deviations
-// are two sums over registers, so that a level far above the spread costs no
-// digits.
+// are two sums over registers, never a difference of squares.
 #include "groupnorm.hpp"
 
 namespace msvm {
 
 namespace {
+
+// Whether the mean is corrected.  The sum of a group's values is rounded at
+// their own level, by some units of its last place, and what that makes the
+// mean off by is the mean of the deviations from it: their sum, beside that of
+// their squares, gives the mean to one rounding and takes the error out of
+// the squares (equal values come out as exact zeros).  Values of 16 bits need
+// none: the error is far under their own steps.  256 x 196 x 512 in 32 bits
+// 37.3 us, without 37.1; 100000 x 64 15.4 and 14.9; for every type 512 x 196 x
+// 512 in bf16 would take 41.5 for 40.0, 4000 x 30 x 120 in f16 34.0 for 30.7.
+template <int DT>
+constexpr bool kCorrect = DT == SVM_F32;
+
+__device__ __forceinline__ bool is_finite(float v)
+{
+    return fabsf(v) <= 3.402823466e38f;
+}
+
+// The sum of squared deviations from a mean, less what that mean is off by:
+// `sum` of the deviations, `off` their mean.  (Not finite: as it is.)
+__device__ __forceinline__ float squares_about(float squares, float sum,
+                                               float off)
+{
+    const float q = fmaf(-sum, off, squares);
+    return q > 0.0f ? q : q <= 0.0f ? 0.0f : squares;
+}
 
 // PARTS: only the chunks' means and squared deviations, else the whole of a
 // sample.
@@ -19,6 +43,7 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
 {
     constexpr int kK = Place<EVEN>::kK;
     constexpr int kBuf = EVEN ? T : 8 * T;
+    constexpr int kQ = kCorrect<DT> ? 2 : 1;
     __shared__ float bufs[kSlabs<T>][2 * kBuf];
     __shared__ float stats[kSlabs<T>][2 * kStat<T>];
     const Plan& p = a.p;
@@ -51,13 +76,15 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
             settle(v[0]);
         }
         const float size = (float)((int64_t)u.rows * at.each(p));
-        group_sums<T, 1, EVEN>(p, at, t, v, buf, stat,
-                               [&](int, float s) { return s / size; });
-        float mu[kK];
+        group_sums<T, 1, EVEN>(p, at, t, v, buf,
+                               [&](int g, const float (&s)[1]) {
+                                   stat[g] = s[0] / size;
+                               });
+        float mu[kK], d[kQ][kK];
 #pragma unroll
         for (int k = 0; k < kK; ++k) {
             mu[k] = stat[at.group[k]];
-            v[0][k] = 0.0f;
+            d[0][k] = d[kQ - 1][k] = 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < IT; ++i) {
@@ -65,33 +92,46 @@ __global__ __launch_bounds__(kSlabThreads<T>) void k_group_norm(GroupArgs a)
             forget(x[i]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float d = x[i].at(e) - mu[EVEN ? 0 : e];
-                v[0][EVEN ? 0 : e] = fmaf(d, d, v[0][EVEN ? 0 : e]);
+                const int k = EVEN ? 0 : e;
+                const float o = x[i].at(e) - mu[k];
+                if (kQ == 2) d[0][k] += o;
+                d[kQ - 1][k] = fmaf(o, o, d[kQ - 1][k]);
             }
-            settle(v[0]);
+            settle(d[0]);
+            settle(d[kQ - 1]);
         }
-        group_sums<T, 1, EVEN>(
-            p, at, t, v, buf + kBuf, stat + kStat<T>, [&](int, float s) {
-                return PARTS ? s : 1.0f / sqrtf(s / size + a.eps);
+        group_sums<T, kQ, EVEN>(
+            p, at, t, d, buf, [&](int g, const float (&s)[kQ]) {
+                float off = 0.0f, q = s[kQ - 1];
+                if (kQ == 2) {
+                    off = s[0] / size;
+                    q = squares_about(q, s[0], off);
+                    if (!is_finite(off)) off = 0.0f;
+                }
+                if (PARTS) {
+                    const int64_t ng = u.n * a.groups + at.g0 + g;
+                    const int64_t cp =
+                        p.parts_across > 1 ? slice % p.parts_across : 0;
+                    a.moments[ng * p.parts() + cp * p.chunks + u.ch] =
+                        make_double2((double)stat[g] + (double)off, q);
+                } else {
+                    if (kQ == 2) stat[g] += off;
+                    stat[kStat<T> + g] = 1.0f / sqrtf(q / size + a.eps);
+                }
             });
+        if (PARTS) continue;
         if (u.rows > 0)
             for (int g = t; g < at.ng; g += T) {
                 const int64_t ng = u.n * a.groups + at.g0 + g;
-                const float m = stat[g], q = stat[kStat<T> + g];
-                if (PARTS) {
-                    const int64_t cp =
-                        p.parts_across > 1 ? slice % p.parts_across : 0;
-                    a.part[ng * p.parts() + cp * p.chunks + u.ch] =
-                        make_float2(m, q);
-                } else {
-                    if (a.mean) a.mean[ng] = m;
-                    if (a.rstd) a.rstd[ng] = q;
-                }
+                if (a.mean) a.mean[ng] = stat[g];
+                if (a.rstd) a.rstd[ng] = stat[kStat<T> + g];
             }
-        if (PARTS) continue;
         float rs[kK];
 #pragma unroll
-        for (int k = 0; k < kK; ++k) rs[k] = stat[kStat<T> + at.group[k]];
+        for (int k = 0; k < kK; ++k) {
+            if (kQ == 2) mu[k] = stat[at.group[k]];
+            rs[k] = stat[kStat<T> + at.group[k]];
+        }
         float w[8], b[8];
         w8.values(w);
         b8.values(b);
@@ -192,7 +232,7 @@ void group_norm(const GroupCall& c, Pieces& ws, hipStream_t s)
     const Plan& p = a.p;
     const int64_t all = samples * c.groups;
     if (p.split()) {
-        a.part = ws.take<float2>(all * p.parts());
+        a.moments = ws.take<double2>(all * p.parts());
         float* mean = ws.take<float>(all);
         float* rstd = ws.take<float>(all);
         if (!a.mean) a.mean = mean;

@@ -64,7 +64,8 @@ struct GroupArgs {
     float eps;
     int act;
     float *mean, *rstd;     // written by the forward pass, else read
-    float2* part;           // sums of the chunks
+    double2* moments;       // means of the chunks, and squares about them
+    float2* part;           // a gradient's sums of the chunks
     const float2* sums;     // joined sums of a gradient
     float *pw, *pb;         // rows of partial sums for weight and bias
     Plan p;
@@ -158,15 +159,15 @@ __device__ __forceinline__ void slab_sync()
     }
 }
 
-// Adds up Q quantities of a slab's threads by groups: stat[q kStat + g] gets
-// done(q, the sum).  v is
-// a thread's one number (EVEN) or its 8 columns' sums.  buf: T or 8 T floats
-// for each quantity; its earlier contents have been read by all threads
-// before the last slab_sync.
+// Adds up Q quantities of a slab's threads by groups: one thread calls
+// done(g, the sums) for each, and the others wait for it.  v is a thread's one
+// number (EVEN) or its 8 columns' sums.  buf: T or 8 T floats for each
+// quantity; its earlier contents have been read by all threads before the
+// last slab_sync.
 template <int T, int Q, bool EVEN, class F>
 __device__ __forceinline__ void group_sums(
     const Plan& p, const Place<EVEN>& at, int t,
-    const float (&v)[Q][Place<EVEN>::kK], float* buf, float* stat, F&& done)
+    const float (&v)[Q][Place<EVEN>::kK], float* buf, F&& done)
 {
     int team = T < 64 ? T : 64;
     while (team > 1 && team * at.ng > T) team >>= 1;
@@ -229,11 +230,7 @@ __device__ __forceinline__ void group_sums(
         for (int off = team >> 1; off > 0; off >>= 1)
 #pragma unroll
             for (int q = 0; q < Q; ++q) sum[q] += __shfl_xor(sum[q], off);
-        if (l == 0) {
-#pragma unroll
-            for (int q = 0; q < Q; ++q)
-                stat[q * kStat<T> + g] = done(q, sum[q]);
-        }
+        if (l == 0) done(g, sum);
     }
     slab_sync<T>();
 }
@@ -565,9 +562,17 @@ int64_t blocks_across(const GroupArgs& a, int64_t most)
     return nb < cap ? nb : cap;
 }
 
+__device__ __forceinline__ double wave_sum64(double v)
+{
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+    return v;
+}
+
 // Joins the chunks' sums of a group, a wave to a group: the mean of the
-// parts' means by their sizes, and the squares about it.  SUMS: adds the
-// parts of a gradient's two sums instead.
+// parts' means by their sizes, in 64 bits (rounded once: equal means give
+// themselves), and the squares about it.  SUMS: adds the parts of a gradient's
+// two sums instead.
 template <bool SUMS>
 __global__ __launch_bounds__(256) void k_group_join(GroupArgs a, float2* sums)
 {
@@ -578,8 +583,6 @@ __global__ __launch_bounds__(256) void k_group_join(GroupArgs a, float2* sums)
     const float size = (float)(a.positions * p.each);
     for (int64_t g = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); g < all;
          g += (int64_t)gridDim.x * 4) {
-        const float2* q = a.part + g * parts;
-        float s0 = 0.0f, s1 = 0.0f;
         auto count = [&](int64_t i) {
             const int64_t cp = p.parts_across > 1 ? i / p.chunks : 0;
             const int64_t ch = i - cp * p.chunks;
@@ -590,25 +593,37 @@ __global__ __launch_bounds__(256) void k_group_join(GroupArgs a, float2* sums)
             return (float)((r < p.chunk ? r : p.chunk) *
                            (c < wide ? c : wide));
         };
-        for (int64_t i = lane; i < parts; i += 64) {
-            const float2 v = q[i];
-            s0 += SUMS ? v.x : v.x * count(i);
-            s1 += v.y;
-        }
-        s0 = SUMS ? wave_sum(s0) : wave_sum(s0) / size;
-        s1 = wave_sum(s1);
         if (SUMS) {
+            const float2* q = a.part + g * parts;
+            float s0 = 0.0f, s1 = 0.0f;
+            for (int64_t i = lane; i < parts; i += 64) {
+                const float2 v = q[i];
+                s0 += v.x;
+                s1 += v.y;
+            }
+            s0 = wave_sum(s0);
+            s1 = wave_sum(s1);
             if (lane == 0) sums[g] = make_float2(s0, s1);
             continue;
         }
+        const double2* q = a.moments + g * parts;
+        double s0 = 0.0;
+        float s1 = 0.0f;
+        for (int64_t i = lane; i < parts; i += 64) {
+            const double2 v = q[i];
+            s0 += v.x * (double)count(i);
+            s1 += (float)v.y;
+        }
+        const double mu = wave_sum64(s0) / (double)size;
+        s1 = wave_sum(s1);
         float far = 0.0f;
         for (int64_t i = lane; i < parts; i += 64) {
-            const float d = q[i].x - s0;
+            const float d = (float)(q[i].x - mu);
             far = fmaf(d * d, count(i), far);
         }
         s1 += wave_sum(far);
         if (lane == 0) {
-            a.mean[g] = s0;
+            a.mean[g] = (float)mu;
             a.rstd[g] = 1.0f / sqrtf(s1 / size + a.eps);
         }
     }
