@@ -646,7 +646,8 @@ svm_status svm_unpack_weights(const svm_packed *packed, const svm_array *W,
 /* One layer on packed weights: Y = act(X W^T + bias) + residual, arrays as in
  * svm_linear.  No weight is rounded further: sums of X times codes over a
  * group's inputs are held in 32 bits and multiplied by the group's scale there
- * (so that |X| up to 4e35 stays in range).  Made for few rows, whose time is
+ * (and formed again, smaller by a power of two, where they would leave 32 bits
+ * before the scale).  Made for few rows, whose time is
  * that of reading the weights; many go through svm_linear's products on the
  * unpacked weights, in the workspace.  residual may be Y itself. */
 svm_status svm_linear_packed(const svm_array *X, const svm_packed *W,

@@ -128,20 +128,21 @@ __device__ __forceinline__ floatx2 two32(uint32_t d)
     return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(d, 1.0f, SEL);
 }
 
+// ... times `by`, a power of two, as 16-bit ones.
 template <int DT>
-__device__ __forceinline__ short8v eight16(uint32_t d)
+__device__ __forceinline__ short8v eight16(uint32_t d, float by)
 {
     if constexpr (DT == SVM_F16) {
-        half2v v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, 1.0f, 0),
-                       __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, 1.0f, 1),
-                       __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, 1.0f, 2),
-                       __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, 1.0f, 3)};
+        half2v v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, by, 0),
+                       __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, by, 1),
+                       __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, by, 2),
+                       __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, by, 3)};
         return __builtin_bit_cast(short8v, v);
     } else {
-        bf16x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, 1.0f, 0),
-                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, 1.0f, 1),
-                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, 1.0f, 2),
-                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, 1.0f, 3)};
+        bf16x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, by, 0),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, by, 1),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, by, 2),
+                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(d, by, 3)};
         return __builtin_bit_cast(short8v, v);
     }
 }
@@ -275,10 +276,11 @@ struct Stage {
         }
     }
 
-    // acc += this chunk's products.  A group's are added up by the matrix
-    // instruction and multiplied by its scale once.
+    // acc += this chunk's products, times `by`.  A group's are added up by the
+    // matrix instruction and multiplied by its scale once.
     template <int REGS>
-    __device__ __forceinline__ void add(float (&acc)[NT][REGS]) const
+    __device__ __forceinline__ void add(float (&acc)[NT][REGS],
+                                        float by = 1.0f) const
     {
         constexpr int kSteps = 4 / GPC;
 #pragma unroll
@@ -290,7 +292,7 @@ struct Stage {
             for (int s = q * kSteps; s < (q + 1) * kSteps; ++s) {
                 short8v w[NT];
 #pragma unroll
-                for (int b = 0; b < NT; ++b) w[b] = eight16<DT>(code[b][s]);
+                for (int b = 0; b < NT; ++b) w[b] = eight16<DT>(code[b][s], by);
                 Factor8<DT> f;
                 f.from(x[s]);
 #pragma unroll
@@ -308,6 +310,37 @@ struct Stage {
         }
     }
 };
+
+// A group's sum of inputs times codes may leave 32 bits where its scale would
+// bring it back (from |X| = 4e35 on; in f16 never).  A wave with a sum that is
+// not finite forms a tile's sums again, of codes times kDown, and puts them in
+// the place of those that were not.  Seldom: a tile and a chunk at a time, and
+// nothing of it is made ahead, so that it takes no registers from the rest.
+constexpr float kDown = 1.0f / 4096.0f;
+
+template <int DT, int GPC, bool FEW>
+__device__ __forceinline__ void sums_again(const Linear4Args& p, int64_t tile,
+                                           int64_t row, int wave, float* red,
+                                           int pad)
+{
+    constexpr int kRegs = FEW ? 1 : 4;
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    float acc[1][kRegs] = {};
+    const int64_t t[1] = {tile};
+#pragma clang loop unroll(disable)
+    for (int64_t c = wave; c < p.chunks; c += kWaves) {
+        Stage<DT, 1, GPC> now;
+        now.load(p, t, row, c, lane);
+        now.template add<kRegs>(acc, kDown);
+    }
+    const int i = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int v = 0; v < kRegs; ++v) {
+        float& sum = red[(FEW ? g : g * 4 + v) * pad + i];
+        if (!(fabsf(sum) <= kMost)) sum = acc[0][v] * (1.0f / kDown);
+    }
+}
 
 // Few rows: 16 NT outputs to a block and 16 rows, the inputs in chunks of 128
 // taken in turn by its waves, whose sums are joined at the end in a fixed
@@ -347,11 +380,20 @@ __global__ __launch_bounds__(64 * kWaves) void k_linear4(Linear4Args p)
         if (c + kWaves < p.chunks) next.load(p, t, row, c + kWaves, lane);
         now.template add<kRegs>(acc);
     }
+    float all = 0.0f;  // NaN where one of them is not finite
 #pragma unroll
     for (int b = 0; b < NT; ++b)
 #pragma unroll
-        for (int v = 0; v < kRegs; ++v)
+        for (int v = 0; v < kRegs; ++v) {
             red[wave][FEW ? g : g * 4 + v][b * 16 + i] = acc[b][v];
+            all = fmaf(acc[b][v], 0.0f, all);
+        }
+    if (DT != SVM_F16 && __any(all != 0.0f)) {
+#pragma clang loop unroll(disable)
+        for (int b = 0; b < NT; ++b)
+            sums_again<DT, GPC, FEW>(p, t0 + b < tiles ? t0 + b : tiles - 1,
+                                     row, wave, &red[wave][0][b * 16], kPad);
+    }
     __syncthreads();
     // a thread to eight outputs
     static_assert(kRows * NT * 2 <= 64 * kWaves, "one turn");
