@@ -61,7 +61,7 @@ __device__ __forceinline__ uint32_t code_of(float w, float s)
 
 struct PackArgs {
     const void* W;
-    int64_t ldw, n, k, chunks, groups, all;
+    int64_t ldw, n, k, chunks, all;
     unsigned char* codes;
     void* scales;
 };
@@ -150,7 +150,7 @@ __device__ __forceinline__ short8v eight16(uint32_t d, float by)
 struct UnpackArgs {
     const unsigned char* codes;
     const void* scales;
-    int64_t n, k, chunks, groups, all;
+    int64_t n, k, chunks, all;
     int gshift;
     void* W;
     int64_t ldw;
@@ -440,8 +440,8 @@ void launch_unpack(const svm_packed& w, int64_t cols, void* to, int64_t ld,
 {
     const Shape4 sh(w);
     const UnpackArgs a{(const unsigned char*)w.data, scales_of(w), w.rows,
-                       cols, sh.chunks, sh.groups, sh.tiles * sh.chunks,
-                       sh.gshift, to, ld};
+                       cols, sh.chunks, sh.tiles * sh.chunks, sh.gshift, to,
+                       ld};
     for_dtype(w.dtype, [&]<int DT>() {
         hipLaunchKernelGGL((k_unpack4<DT>), dim3(tile_blocks(a.all)),
                            dim3(256), 0, s, a);
@@ -464,7 +464,7 @@ bool few_rows4(int64_t m, int64_t n, int64_t k)
 void pack4(const svm_array& W, const svm_packed& to, hipStream_t s)
 {
     const Shape4 sh(to);
-    const PackArgs a{W.data, W.ld, to.rows, to.cols, sh.chunks, sh.groups,
+    const PackArgs a{W.data, W.ld, to.rows, to.cols, sh.chunks,
                      sh.tiles * sh.chunks, (unsigned char*)to.data,
                      const_cast<void*>(scales_of(to))};
     const dim3 grid(tile_blocks(a.all)), block(256);
