@@ -1,6 +1,8 @@
 """How group norm cuts up a call (csrc/groupnorm.hpp), on the CPU: the host's
 part of it compiled for this machine, with UndefinedBehaviorSanitizer."""
+import math
 import os
+import random
 import subprocess
 
 import pytest
@@ -58,3 +60,38 @@ def test_the_kernels_assumptions_hold_for_every_plan(plans):
                 cases += [(n, p, c, groups, t, grad) for t in range(3)
                           for grad in (0, 1)]
     plans(cases)
+
+
+def test_every_variant_is_compared_with_64_bits(plans):
+    # of 40000 drawn calls, none takes a variant that no size of the GPU tests
+    # takes (what is compiled differs between 32-bit and 16-bit types, not
+    # between the two 16-bit ones)
+    import test_gpu_groupnorm as a
+    import test_gpu_groupnorm_variants as v
+
+    def variants(sizes):
+        cases = [s + (t, grad) for s in sizes for t in (0, 1)
+                 for grad in (0, 1)]
+        return {c[4:] + x: c for c, x in zip(cases, plans(cases))}
+
+    rng = random.Random(5)
+    log = lambda lo, hi: round(math.exp(rng.uniform(  # noqa: E731
+        math.log(lo), math.log(hi))))
+    drawn = []
+    while len(drawn) < 40000:
+        n, p = log(1, 200000), log(1, 100000)
+        groups, each = log(1, 256), log(1, 9000)
+        if rng.random() < 0.5:
+            each = max(8, each // 8 * 8)
+        if n * p * groups * each <= 6e7 and groups * each <= 1 << 21:
+            drawn.append((n, p, groups * each, groups))
+    sizes = [s for f in (a.test_group_norm_and_gradients, a.test_acts,
+                         a.test_large, v.test_every_variant)
+             for m in f.pytestmark
+             if m.name == "parametrize" and m.args[0] == "n,p,c,groups"
+             for s in m.args[1]]
+    assert len(sizes) > 50
+    have, reached = variants(sizes), variants(drawn)
+    assert len(reached) > 120
+    missing = {k: reached[k] for k in set(reached) - set(have)}
+    assert not missing, missing
