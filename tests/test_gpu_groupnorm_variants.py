@@ -3,8 +3,10 @@ kernels that a call can reach: threads and pieces of a slab, groups of whole
 eights of channels and others, whole samples and chunks.  test_group_plan.py
 asks the plan which variant each size takes, and that none is missing."""
 import pytest
+import torch
 
-from test_gpu_groupnorm import TYPES, check, gen, rnd
+from paper_1706_05544_amd import native as nv
+from test_gpu_groupnorm import DEV, EPS, TYPES, Ref, check, gen, rnd
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +30,17 @@ def test_every_variant(n, p, c, groups, t):
     w, b = (1 + rnd(g, c, by=0.2)).to(TYPES[t]), rnd(g, c, by=0.3, t=t)
     dY, R = rnd(g, n, p, c, t=t), rnd(g, n, p, c, t=t)
     check(X, groups, w, b, "gelu", t, R, dY)
+
+
+def test_the_last_samples_of_2_6e9_values():
+    n, p, c, groups = 5000, 1024, 512, 32
+    g = gen(16)
+    X = torch.empty(n, p, c, dtype=torch.bfloat16, device=DEV)
+    for i in range(0, n, 50):
+        X[i:i + 50] = rnd(g, 50, p, c, t="bf16") + i / n
+    w, b = rnd(g, c, t="bf16"), rnd(g, c, t="bf16")
+    Y, mean, rstd = nv.svm_group_norm(X, groups, w, b, eps=EPS, act="silu",
+                                      save=True)
+    for i in (0, 2499, n - 1):
+        Ref(X[i:i + 1], groups, w, b, "silu").forward(
+            Y[i:i + 1], mean[i:i + 1], rstd[i:i + 1], "bf16")
