@@ -540,7 +540,9 @@ svm_status svm_adamw_state(const int8_t *m, const uint8_t *v,
  * rows a multiple of positions (>= 1), cols of groups.  weight and bias
  * (1 x cols) are nullable (1 and 0).  mean and rstd (samples x groups floats
  * each, nullable) receive the statistics that the gradient needs, and overlap
- * nothing.  Y may be X itself (same data and ld). */
+ * nothing.  Y may be X itself (same data and ld).  The sum of a group's values
+ * and that of their squared deviations have to stay in 32 bits' range (an
+ * infinite mean makes Y NaN, an infinite sum of squares rstd 0). */
 svm_status svm_group_norm(const svm_array *X, int64_t positions,
                           int64_t groups, const svm_array *weight,
                           const svm_array *bias, double eps, int32_t act,
@@ -583,7 +585,8 @@ typedef struct {
  *   *factor = max_norm / *norm where that is above max_norm, else 1,
  * one float each on the device; factor is nullable.  Squares and sums are
  * held in 64 bits.  Where a gradient is NaN or infinite, *norm is not finite
- * and *factor NaN.  max_norm >= 0, or infinite (a factor of 1 or NaN). */
+ * and *factor NaN.  max_norm >= 0, or infinite (a factor of 1 or NaN).  Both
+ * are written after all gradients have been read. */
 svm_status svm_grad_norm(const svm_grad *grads, int32_t n_grads,
                          double grad_scale, double max_norm, float *norm,
                          float *factor, void *work, int64_t work_bytes,

@@ -69,7 +69,7 @@ struct PackArgs {
 // A wave to a tile: a group's 32 inputs are the four lanes of an output in one
 // step, so its largest magnitude takes two exchanges.  Rounding is done once,
 // when weights are laid out; bound by its division and comparisons: 67 million
-// f16 weights 70 us, 2.4 TB/s.
+// f16 weights 63 to 70 us, 2.4 TB/s and more.
 template <int DT, int GROUP>
 __global__ __launch_bounds__(256) void k_pack4(PackArgs p)
 {
@@ -157,7 +157,8 @@ struct UnpackArgs {
 };
 
 // A wave to a tile.  Exact: scale times code is a value of the type.  Bound by
-// memory: 1.6 million weights to 32 bits 5.2 us.
+// memory: 67 million f16 weights 32.2 us, 5.3 TB/s; 1.6 million to 32 bits 4.5
+// us, of which a launch is 2.
 template <int DT>
 __global__ __launch_bounds__(256) void k_unpack4(UnpackArgs p)
 {
@@ -350,10 +351,10 @@ __device__ __forceinline__ void sums_again(const Linear4Args& p, int64_t tile,
 // FEW: up to 4 rows, every fourth of the 16 that the matrix instruction takes,
 // so that a lane has one sum to scale and not four.
 // Bound by the read of the codes where they are many: 1 x 4096 over 16384 in
-// f16 8.4 us in a row of calls, 4.3 TB/s; by latency where they are few: 1 x
-// 784 over 1024 4.0 us, of which an empty launch is 2; and for more rows by
-// what is read of X from the caches, again for every 16 NT outputs: 32 x 4096
-// over 4096 in bf16 7.6 us, 128 rows 13.4.
+// f16 7.3 us in a row of calls, 8.4 by the trace, 4.3 TB/s; by latency where
+// they are few: 1 x 784 over 1024 4.4 us, of which an empty launch is 2; and
+// for more rows by what is read of X from the caches, again for every 16 NT
+// outputs: 32 x 4096 over 4096 in bf16 7.2 us, 128 rows 12.9.
 template <int DT, int NT, int GPC, bool FEW>
 __global__ __launch_bounds__(64 * kWaves) void k_linear4(Linear4Args p)
 {

@@ -759,7 +759,7 @@ struct Split {
 // instructions) and the LDS traffic of three parts take the rest.
 // NARROW: B's values are those of bf16, so that h' is all of them: three
 // products, of which each reads a part of A's.  Unpacked 4-bit weights: 5000 x
-// 2048 over 784 97 us, with the six 138; 16384 x 2048 over 2048 397 and 645.
+// 2048 over 784 97 us, with the six 138; 16384 x 2048 over 2048 373 and 645.
 template <int BM, int BN, int WGM, int WGN, bool AALONG, bool BALONG,
           bool NARROW>
 __global__ __launch_bounds__(64 * WGM * WGN) void k_product32(Args p)
@@ -1216,6 +1216,11 @@ struct TileCost {
 constexpr TileCost kCost16[3] = {{256, 256, 1.65, 1.65, 5.0},
                                  {128, 128, 0.57, 0.57, 4.0},
                                  {64, 64, 0.26, 0.23, 1.5}};
+// (Those in 32 bits are of six matrix products.  Narrow factors take three in
+// the tile that is best with six: 16384 x 2048 over 2048 373 us in the largest,
+// 487 and 599 in the others; 4000 x 1000 over 500 29.2 in tiles of 128 columns,
+// 36 in either other; but 5000 x 2048 over 784 97 in tiles of 128, 92.5 in the
+// largest, and 1100 x 130 over 20000 64 in tiles of 64, 53 in the largest.)
 constexpr TileCost kCost32[3] = {{256, 128, 2.50, 2.50, 10.0},
                                  {128, 128, 1.45, 1.42, 7.0},
                                  {64, 64, 0.65, 0.48, 2.0}};
